@@ -7,6 +7,9 @@
  *   -> gather of the kept variate tokens                       (vardrop_gather)
  *   -> multi-head scaled dot-product attention over the kept tokens, forward and
  *      backward                                               (vardrop_attn_fwd / _bwd).
+ * What turns that block into a layer that trains comes with it: the norms before and after a block with its gate and
+ * residual scale (vardrop_block_norm_fwd / _bwd), the global norm and clipping of all gradients (vardrop_grad_norm,
+ * vardrop_clip_grads) and the update of the weights (vardrop_adamw).
  *
  * General rules
  *   - Every pointer is a DEVICE pointer owned by the caller unless its name ends in
@@ -98,6 +101,12 @@ enum {
   VARDROP_K_GEMM_DWE,        /* dWe = z^T dxs (K slices)                                    */
   VARDROP_K_SDPA_BWD_DQKV,   /* bf16, n > 128, few workgroups: dQ, dK, dV in one launch (GEMM_DO then forms rowsum(dO * O)) */
   VARDROP_K_EMBED_FUSED,     /* kept windows gathered, standardised and embedded in one launch (bf16: short windows always, longer ones by size) */
+  VARDROP_K_BLOCK_NORM_FWD,  /* norms around a block, gate and residual, forward            */
+  VARDROP_K_BLOCK_NORM_BWD,  /* their gradients, column sums of every range of rows         */
+  VARDROP_K_BLOCK_NORM_VECTORS, /* weight, bias and gate gradients from those sums          */
+  VARDROP_K_GRAD_NORM,       /* global norm of a tensor list's gradients                    */
+  VARDROP_K_CLIP,            /* gradients scaled to a norm                                  */
+  VARDROP_K_ADAMW,           /* AdamW step of a tensor list                                 */
   VARDROP_K_COUNT
 };
 int vardrop_profile_select(vardrop_ctx* ctx, int kernel_id);
@@ -372,6 +381,120 @@ int vardrop_attn_bwd_dev(vardrop_ctx* ctx, const void* dy, const void* xs,
                          void* dxs, float* dWq, float* dWk, float* dWv, float* dWo,
                          float* dbq, float* dbk, float* dbv, float* dbo,
                          void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * Norms before and after a block, fused with the block's gate and the residual scale -- what joins the blocks of the
+ * backbone (Sec. 4.1) of which the attention above is one.  For every token, over its d channels:
+ *
+ *   u = post(f)                        f: the block's output;  post: LayerNorm or RMSNorm with weight wp, bias bp, or nothing
+ *   r = alpha x + beta g * u           x: the residual stream;  g: the block's gate (a learned scale of every channel)
+ *   h = pre(r)                         the next block's input;  pre: LayerNorm or RMSNorm with weight w, bias b, or nothing
+ *
+ * LayerNorm: (v - mean) / sqrt(var + eps) with the population variance; RMSNorm: v / sqrt(mean(v^2) + eps).  The first
+ * block's input needs f == NULL (r = alpha x); add-and-norm is post = NONE without a gate; norms on both sides of a
+ * block are post and pre together.
+ *
+ *   x, r, dr, dx   [B][n][d], element type `res_dtype`        f, h, dh, df  [B][n][d], element type `dtype`
+ *                  (the residual stream may be VARDROP_F32 beside VARDROP_BF16 blocks, not the other way round)
+ *   w, b, wp, bp   [d], `dtype`; NULL = ones (w, wp), zeros (b, bp); NULL where the norm is NONE
+ *   gate           [gates][d], `dtype`: gates = 1 one row for all tokens, gates = B one row for each window (gate of a
+ *                  condition); NULL with gates = 0: ones
+ *   r              NULL = not wanted;  h NULL exactly when pre is NONE.  r may be x, h may be f, and r may be f or h may be x
+ *                  where the element types agree
+ *   stats          fp32 [B*n][4], 16-byte aligned: mean and 1/deviation of post, mean and 1/deviation of pre (0 and 1
+ *                  where there is no norm, mean 0 for RMSNorm), taken from r before it is rounded; written by fwd (NULL =
+ *                  not wanted), read by bwd (may be NULL there when neither norm is)
+ * Backward, from the gradients dr and dh of r and h (dr NULL = zero; dh NULL exactly when pre is NONE):
+ *   dx, df         NULL = not wanted; dx may be dr, df may be dh, and dx may be dh or df may be dr where the element types agree
+ *   r, f           as the forward had them (r: needed with pre, x itself where f was NULL and alpha 1; f: needed with
+ *                  post or a gate, NULL otherwise)
+ *   dw, db, dwp, dbp   fp32 [d], dgate fp32 [gates][d]; overwritten, NULL = skip
+ *   ws             vardrop_block_norm_workspace_bytes, 256-byte aligned; may be NULL when no vector gradient is wanted
+ * All arithmetic and sums are fp32, deviations are taken about the mean; sums run in an order that does not depend on
+ * scheduling.  Rows need element alignment only.  1 <= d <= 8192, B*n < 2^31 and gates <= 65000 (EUNSUPPORTED above);
+ * eps > 0.  B*n == 0 is a no-op (vector gradients zero-filled).  The _dev forms read n on the device (see the general
+ * rules); the same n_max has to be given to the size query and the backward.
+ */
+enum { VARDROP_NORM_NONE = 0, VARDROP_NORM_LAYER = 1, VARDROP_NORM_RMS = 2 };
+size_t vardrop_block_norm_workspace_bytes(int B, int n, int d, int gates);
+int vardrop_block_norm_fwd(vardrop_ctx* ctx, const void* x, const void* f, int B, int n, int d, int res_dtype, int dtype,
+                           int post, const void* wp, const void* bp, const void* gate, int gates, float alpha, float beta,
+                           int pre, const void* w, const void* b, float eps,
+                           void* r, void* h, float* stats, void* stream);
+int vardrop_block_norm_bwd(vardrop_ctx* ctx, const void* dr, const void* dh, const void* r, const void* f, const float* stats,
+                           int B, int n, int d, int res_dtype, int dtype,
+                           int post, const void* wp, const void* bp, const void* gate, int gates, float alpha, float beta,
+                           int pre, const void* w,
+                           void* dx, void* df, float* dw, float* db, float* dwp, float* dbp, float* dgate,
+                           void* ws, size_t ws_bytes, void* stream);
+int vardrop_block_norm_fwd_dev(vardrop_ctx* ctx, const void* x, const void* f, int B, const int32_t* n_dev, int n_max,
+                               int32_t* status, int d, int res_dtype, int dtype,
+                               int post, const void* wp, const void* bp, const void* gate, int gates, float alpha, float beta,
+                               int pre, const void* w, const void* b, float eps,
+                               void* r, void* h, float* stats, void* stream);
+int vardrop_block_norm_bwd_dev(vardrop_ctx* ctx, const void* dr, const void* dh, const void* r, const void* f,
+                               const float* stats, int B, const int32_t* n_dev, int n_max, int32_t* status,
+                               int d, int res_dtype, int dtype,
+                               int post, const void* wp, const void* bp, const void* gate, int gates, float alpha, float beta,
+                               int pre, const void* w,
+                               void* dx, void* df, float* dw, float* db, float* dwp, float* dbp, float* dgate,
+                               void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * Lists of tensors: the gradients of a model, and the weights and moments they update.  A list is laid out once, in
+ * `table` (device memory of the caller, vardrop_tensor_list_bytes, 256-byte aligned), and used every step as long as the
+ * tensors stay where they are; the calls below then take one launch each, however many tensors there are.  The struct is
+ * host memory of the caller, filled by vardrop_tensor_list_build; copies of it are the same list.  The *_host arrays are read
+ * during the call only (it enqueues one launch for every 48 tensors, and needs a stream that is not being captured).
+ *
+ *   numel_host        elements of each tensor (0 is allowed: its pointers are not looked at)
+ *   grad_host         gradients, grad_dtype_host[i] VARDROP_F32 or VARDROP_BF16 (NULL = all F32)
+ *   clip_host         where vardrop_clip_grads writes the clipped gradients, clip_dtype_host[i] (NULL = all F32);
+ *                     clip_host NULL = in place
+ *   param, m, v       fp32 weights and moments of vardrop_adamw (all three, or NULL for a list that is not updated)
+ *   weight_host       bf16 copies of the weights that vardrop_adamw writes beside them; NULL, or NULL entries = none
+ *   decay_host        weight decay of each tensor; NULL = 0
+ * Tensors need element alignment only, and must not overlap.  The table also holds the calls' partial sums: calls that use one list
+ * must be ordered by their streams.
+ */
+typedef struct vardrop_tensor_list {
+  void* table;
+  size_t table_bytes;
+  int64_t numel;      /* elements in all */
+  int32_t tensors, chunks;
+  uint32_t has, built;
+} vardrop_tensor_list;
+size_t vardrop_tensor_list_bytes(int tensors, const int64_t* numel_host);
+int vardrop_tensor_list_build(vardrop_ctx* ctx, int tensors, const int64_t* numel_host,
+                              void* const* grad_host, const int32_t* grad_dtype_host,
+                              void* const* clip_host, const int32_t* clip_dtype_host,
+                              float* const* param_host, float* const* m_host, float* const* v_host,
+                              void* const* weight_host, const float* decay_host,
+                              void* table, size_t table_bytes, vardrop_tensor_list* list_host, void* stream);
+
+/* Global norm of all gradients of a list, norm = sqrt(sum g^2) (device fp32 [1]; 0 for an empty list).  Squares and sums are
+ * fp64, in an order that does not depend on scheduling: a finite set of gradients has a finite norm unless the result itself
+ * exceeds fp32. */
+int vardrop_grad_norm(vardrop_ctx* ctx, const vardrop_tensor_list* list, float* norm, void* stream);
+/* Clipping to a global norm: out = g * min(1, max_norm / (norm + 1e-6)), rounded once to the type of `out` (the gradients
+ * themselves for a list without clip tensors).  `norm` is read on the device, max_norm > 0.  When it is not finite nothing is written
+ * and *status (device int32, optional, never cleared by the library) is set to 1. */
+int vardrop_clip_grads(vardrop_ctx* ctx, const vardrop_tensor_list* list, const float* norm, float max_norm,
+                       int32_t* status, void* stream);
+/* One AdamW step (decoupled weight decay) of every tensor of a list, in place, all in fp32; with s the clipping factor above
+ * (norm NULL or max_norm 0: s = 1), so that clipped gradients are never written:
+ *   m = beta1 m + (1 - beta1) s g,   v = beta2 v + (1 - beta2) (s g)^2
+ *   param = param (1 - lr decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps),   weight = bf16(param)
+ * step >= 1 counts this step; 0 <= beta1, beta2 < 1, eps > 0.  When `norm` is given and not finite the step is skipped: nothing
+ * is written (nor is the step counted, below) and *status is set to 1.
+ * vardrop_adamw_dev reads the rate from lr_dev (fp32 [1]) and the number of steps already done from step_dev (int64 [1],
+ * 8-byte aligned), and with advance != 0 stores that number + 1 once the step is done, so that a recorded launch makes the next
+ * step at every replay.  Calls that share a step_dev must be ordered by their streams. */
+int vardrop_adamw(vardrop_ctx* ctx, const vardrop_tensor_list* list, double lr, double beta1, double beta2, double eps,
+                  int64_t step, const float* norm, float max_norm, int32_t* status, void* stream);
+int vardrop_adamw_dev(vardrop_ctx* ctx, const vardrop_tensor_list* list, const float* lr_dev, double beta1, double beta2,
+                      double eps, int64_t* step_dev, int advance, const float* norm, float max_norm,
+                      int32_t* status, void* stream);
 
 #ifdef __cplusplus
 }

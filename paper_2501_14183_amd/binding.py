@@ -11,6 +11,9 @@ import torch
 
 F32 = 0
 BF16 = 1
+NORM_NONE = 0
+NORM_LAYER = 1
+NORM_RMS = 2
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
 
@@ -19,7 +22,13 @@ _c_i64 = ctypes.c_int64
 _c_u32 = ctypes.c_uint32
 _c_u64 = ctypes.c_uint64
 _c_size = ctypes.c_size_t
+_c_float = ctypes.c_float
+_c_double = ctypes.c_double
 _ptr = ctypes.c_void_p
+
+# post, wp, bp, gate, gates, alpha, beta, pre, w, then b, eps, r, h, stats or the gradients and the workspace; stream
+_BLOCK_NORM_FWD = [_c_int, _ptr, _ptr, _ptr, _c_int, _c_float, _c_float, _c_int, _ptr] + [_ptr, _c_float] + [_ptr] * 4
+_BLOCK_NORM_BWD = [_c_int, _ptr, _ptr, _ptr, _c_int, _c_float, _c_float, _c_int, _ptr] + [_ptr] * 8 + [_c_size, _ptr]
 
 _SIGNATURES = {
     "vardrop_create": (_c_int, [ctypes.POINTER(_ptr), _c_int]),
@@ -75,6 +84,17 @@ _SIGNATURES = {
                                     [_ptr] * 8 + [_ptr, _ptr, _ptr, _ptr, _c_size, _ptr]),
     "vardrop_attn_bwd_dev": (_c_int, [_ptr, _ptr, _ptr, _c_int, _ptr, _c_int, _ptr, _c_int, _c_int, _c_int] + [_ptr] * 4 +
                              [_ptr] + [_ptr] * 9 + [_ptr, _c_size, _ptr]),
+    "vardrop_block_norm_workspace_bytes": (_c_size, [_c_int] * 4),
+    "vardrop_block_norm_fwd": (_c_int, [_ptr, _ptr, _ptr, _c_int, _c_int, _c_int, _c_int, _c_int] + _BLOCK_NORM_FWD),
+    "vardrop_block_norm_fwd_dev": (_c_int, [_ptr, _ptr, _ptr, _c_int, _ptr, _c_int, _ptr, _c_int, _c_int, _c_int] + _BLOCK_NORM_FWD),
+    "vardrop_block_norm_bwd": (_c_int, [_ptr] * 6 + [_c_int, _c_int, _c_int, _c_int, _c_int] + _BLOCK_NORM_BWD),
+    "vardrop_block_norm_bwd_dev": (_c_int, [_ptr] * 6 + [_c_int, _ptr, _c_int, _ptr, _c_int, _c_int, _c_int] + _BLOCK_NORM_BWD),
+    "vardrop_tensor_list_bytes": (_c_size, [_c_int, _ptr]),
+    "vardrop_tensor_list_build": (_c_int, [_ptr, _c_int] + [_ptr] * 10 + [_ptr, _c_size, _ptr, _ptr]),
+    "vardrop_grad_norm": (_c_int, [_ptr, _ptr, _ptr, _ptr]),
+    "vardrop_clip_grads": (_c_int, [_ptr, _ptr, _ptr, _c_float, _ptr, _ptr]),
+    "vardrop_adamw": (_c_int, [_ptr, _ptr, _c_double, _c_double, _c_double, _c_double, _c_i64, _ptr, _c_float, _ptr, _ptr]),
+    "vardrop_adamw_dev": (_c_int, [_ptr, _ptr, _ptr, _c_double, _c_double, _c_double, _ptr, _c_int, _ptr, _c_float, _ptr, _ptr]),
 }
 
 
@@ -485,3 +505,216 @@ def vardrop_embed_bwd_dev(ctx, dxs, n_dev, n_max, L, saved, ws, out, stream=None
                                         _p(dWe), _p(dbe), _p(ws), ws.numel(), _stream(dxs, stream))
     ctx.check(rc, "vardrop_embed_bwd_dev")
     return dWe, dbe
+
+
+# ---------------------------------------------------------------- norms before and after a block
+def _block_dtype(res, *others):
+    """Element type code of the block's tensors (those given must agree), that of the residual stream where there is none."""
+    code = None
+    for t in others:
+        if t is not None:
+            c = _dtype_code(t)
+            if code is not None and c != code:
+                raise TypeError("the block's output, its norms' weights and its gate must have one element type")
+            code = c
+    return _dtype_code(res) if code is None else code
+
+
+def _check_block_norm(shape, code, res, w, b, wp, bp, gate, **more):
+    """Shapes, element types and layout of a block norm's tensors -> rows of the gate."""
+    B, n, d = shape
+    dt = torch.float32 if code == F32 else torch.bfloat16
+    for name, t in more.items():
+        if t is not None:
+            if t.shape != shape or not t.is_contiguous():
+                raise TypeError("%s must be contiguous %s" % (name, list(shape)))
+            if t.dtype != (dt if name in ("f", "h", "dh", "df") else res.dtype):
+                raise TypeError("%s has element type %s" % (name, t.dtype))
+    if not res.is_contiguous():
+        raise TypeError("tokens must be contiguous [B, n, d]")
+    for name, t in (("w", w), ("b", b), ("wp", wp), ("bp", bp)):
+        if t is not None and (t.numel() != d or not t.is_contiguous()):
+            raise TypeError("%s must hold %d contiguous elements" % (name, d))
+    if gate is None:
+        return 0
+    if not gate.is_contiguous() or gate.shape[-1] != d or gate.numel() not in (d, B * d):
+        raise TypeError("gate must be contiguous [d], [1, d] or [B, d]")
+    return 1 if gate.numel() == d else B
+
+
+def vardrop_block_norm_workspace_bytes(B, n, d, gates):
+    """Bytes of the workspace of vardrop_block_norm_bwd; gates: rows of the gate (0 = none)."""
+    return max(load_library().vardrop_block_norm_workspace_bytes(B, n, d, gates), 256)
+
+
+def vardrop_block_norm_fwd(ctx, x, f=None, pre=NORM_LAYER, w=None, b=None, post=NORM_NONE, wp=None, bp=None, gate=None,
+                           alpha=1.0, beta=1.0, eps=1e-5, want_r=True, want_stats=True, out=None, stream=None,
+                           n_dev=None, status=None):
+    """r = alpha x + beta gate * post(f), h = pre(r): x [B, n, d] the residual stream, f the block's output (None: none).
+
+    -> (r, h, stats): r in x's type, h in the block's, stats float32 [B*n, 4] for the backward.  `out`, when given, is that
+    triple of preallocated tensors; entries that are None are not written (h is None exactly when pre is NORM_NONE).
+    n_dev (int32 [1] on the device): the tensors are buffers for x.shape[1] tokens that hold [B, N', d] packed."""
+    B, n, d = x.shape
+    code = _block_dtype(x, f, w, b, wp, bp, gate)
+    if out is not None:
+        r, h, stats = out
+    else:
+        _own_buffers(stream, "vardrop_block_norm_fwd", out=out)
+        dt = torch.float32 if code == F32 else torch.bfloat16
+        r = torch.empty_like(x) if want_r or pre == NORM_NONE else None
+        h = torch.empty((B, n, d), dtype=dt, device=x.device) if pre != NORM_NONE else None
+        stats = torch.empty((B * n, 4), dtype=torch.float32, device=x.device) if want_stats else None
+    gates = _check_block_norm(x.shape, code, x, w, b, wp, bp, gate, r=r, f=f, h=h)
+    if stats is not None and (stats.dtype != torch.float32 or stats.numel() < 4 * B * n or not stats.is_contiguous()):
+        raise TypeError("stats must be contiguous float32 [B * n, 4]")
+    args = (post, _p(wp), _p(bp), _p(gate), gates, alpha, beta, pre, _p(w), _p(b), eps, _p(r), _p(h), _p(stats),
+            _stream(x, stream))
+    res = _dtype_code(x)
+    if n_dev is None:
+        rc = ctx._lib.vardrop_block_norm_fwd(ctx.handle, _p(x), _p(f), B, n, d, res, code, *args)
+    else:
+        rc = ctx._lib.vardrop_block_norm_fwd_dev(ctx.handle, _p(x), _p(f), B, _p(n_dev), n, _p(status), d, res, code, *args)
+    if rc:
+        ctx.check(rc, "vardrop_block_norm_fwd")
+    return r, h, stats
+
+
+def vardrop_block_norm_bwd(ctx, dr, dh, r, f, stats, pre=NORM_LAYER, w=None, post=NORM_NONE, wp=None, bp=None, gate=None,
+                           alpha=1.0, beta=1.0, bias_grads=False, ws=None, out=None, stream=None, n_dev=None, status=None):
+    """Gradients of vardrop_block_norm_fwd from dr and dh, those of r and h (dr may be None; dh is None exactly when pre
+    is NORM_NONE); r, f, stats as the forward had them.
+
+    -> (dx, df, dw, db, dwp, dbp, dgate): dx in the residual's type, df in the block's, the rest float32.  Without `out`, df is
+    made when f is given, the vectors' gradients for the vectors given (db, dbp with bias_grads).  `out`, when given, is that
+    tuple of preallocated tensors; entries that are None are skipped."""
+    like = dr if dr is not None else r
+    B, n, d = like.shape
+    code = _block_dtype(like, dh, f, w, wp, bp, gate)
+    if out is not None:
+        dx, df, dw, db, dwp, dbp, dgate = out
+    else:
+        _own_buffers(stream, "vardrop_block_norm_bwd", out=out)
+
+        def vector(wanted, *shape):
+            return torch.empty(shape, dtype=torch.float32, device=like.device) if wanted else None
+
+        dx = torch.empty_like(like)
+        df = None if f is None else torch.empty_like(f)
+        dw, db = vector(w is not None, d), vector(bias_grads and pre != NORM_NONE, d)
+        dwp, dbp = vector(wp is not None, d), vector(bias_grads and post != NORM_NONE, d)
+        dgate = None if gate is None else vector(True, *gate.shape)
+    gates = _check_block_norm(like.shape, code, like, w, None, wp, bp, gate, dr=dr, dh=dh, r=r, f=f, dx=dx, df=df)
+    if stats is not None and (stats.dtype != torch.float32 or stats.numel() < 4 * B * n or not stats.is_contiguous()):
+        raise TypeError("stats must be contiguous float32 [B * n, 4]")
+    for name, t, count in (("dw", dw, d), ("db", db, d), ("dwp", dwp, d), ("dbp", dbp, d), ("dgate", dgate, gates * d)):
+        if t is not None and (t.dtype != torch.float32 or t.numel() != count or not t.is_contiguous()):
+            raise TypeError("%s must be contiguous float32 of %d elements" % (name, count))
+    if ws is None and (dw is not None or db is not None or dwp is not None or dbp is not None or dgate is not None):
+        _own_buffers(stream, "vardrop_block_norm_bwd", ws=ws)
+        ws = torch.empty(vardrop_block_norm_workspace_bytes(B, n, d, gates), dtype=torch.uint8, device=like.device)
+    args = (post, _p(wp), _p(bp), _p(gate), gates, alpha, beta, pre, _p(w), _p(dx), _p(df), _p(dw), _p(db), _p(dwp), _p(dbp),
+            _p(dgate), _p(ws), 0 if ws is None else ws.numel(), _stream(like, stream))
+    res = _dtype_code(like)
+    if n_dev is None:
+        rc = ctx._lib.vardrop_block_norm_bwd(ctx.handle, _p(dr), _p(dh), _p(r), _p(f), _p(stats), B, n, d, res, code, *args)
+    else:
+        rc = ctx._lib.vardrop_block_norm_bwd_dev(ctx.handle, _p(dr), _p(dh), _p(r), _p(f), _p(stats), B, _p(n_dev), n,
+                                                 _p(status), d, res, code, *args)
+    if rc:
+        ctx.check(rc, "vardrop_block_norm_bwd")
+    return dx, df, dw, db, dwp, dbp, dgate
+
+
+# ---------------------------------------------------------------- tensor lists: gradient norm, clipping, AdamW
+class _TensorListStruct(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("table_bytes", ctypes.c_size_t), ("numel", ctypes.c_int64),
+                ("tensors", ctypes.c_int32), ("chunks", ctypes.c_int32), ("has", ctypes.c_uint32), ("built", ctypes.c_uint32)]
+
+
+class TensorList:
+    """A vardrop_tensor_list with its table and the tensors it names, which it keeps alive.
+
+    grads: float32 or bfloat16 tensors on one device, contiguous; clipped: where vardrop_clip_grads writes (None: in place);
+    params, exp_avg, exp_avg_sq: float32, for vardrop_adamw; weights: bfloat16 copies of the weights, entries may be None;
+    decay: weight decay of each tensor.  Building it enqueues work on torch's current stream."""
+
+    def __init__(self, ctx, grads, clipped=None, params=None, exp_avg=None, exp_avg_sq=None, weights=None, decay=None):
+        grads = list(grads)
+        count = len(grads)
+        numel = [t.numel() for t in grads]
+
+        def pointers(what, tensors, dtypes, may_miss=False):
+            if tensors is None:
+                return None, None
+            tensors = list(tensors)
+            if len(tensors) != count:
+                raise TypeError("%s: %d tensors for %d gradients" % (what, len(tensors), count))
+            for t, k in zip(tensors, numel):
+                if t is None and may_miss:
+                    continue
+                if t is None or t.dtype not in dtypes or t.numel() != k or not t.is_contiguous() or t.device != ctx.device:
+                    raise TypeError("%s: contiguous tensors of the gradients' sizes on %s wanted, in %s"
+                                    % (what, ctx.device, " or ".join(str(d) for d in dtypes)))
+            return tensors, (ctypes.c_void_p * max(count, 1))(*[None if t is None else t.data_ptr() for t in tensors])
+
+        both, fp32 = (torch.float32, torch.bfloat16), (torch.float32,)
+
+        def codes(tensors):
+            return None if tensors is None else (ctypes.c_int32 * max(count, 1))(*[_dtype_code(t) for t in tensors])
+
+        grads, g = pointers("grads", grads, both)
+        clipped, c = pointers("clipped", clipped, both)
+        params, p = pointers("params", params, fp32)
+        exp_avg, m = pointers("exp_avg", exp_avg, fp32)
+        exp_avg_sq, v = pointers("exp_avg_sq", exp_avg_sq, fp32)
+        weights, w = pointers("weights", weights, (torch.bfloat16,), may_miss=True)
+        if decay is not None and len(decay) != count:
+            raise TypeError("decay: %d values for %d gradients" % (len(decay), count))
+        rates = None if decay is None else (ctypes.c_float * max(count, 1))(*decay)
+        sizes = (ctypes.c_int64 * max(count, 1))(*numel)
+        self.tensors = (grads, clipped, params, exp_avg, exp_avg_sq, weights)
+        nbytes = ctx._lib.vardrop_tensor_list_bytes(count, sizes)
+        if nbytes == 0:
+            raise VarDropError(-1, "vardrop_tensor_list_bytes")
+        self.table = torch.empty(nbytes, dtype=torch.uint8, device=ctx.device)
+        self.struct = _TensorListStruct()
+        self.pointer = ctypes.addressof(self.struct)
+        rc = ctx._lib.vardrop_tensor_list_build(ctx.handle, count, sizes, g, codes(grads), c, codes(clipped), p, m, v, w, rates,
+                                                self.table.data_ptr(), nbytes, self.pointer, _stream(self.table, None))
+        ctx.check(rc, "vardrop_tensor_list_build")
+
+
+def vardrop_grad_norm(ctx, tensors, out=None, stream=None):
+    """Global norm of a TensorList's gradients -> float32 [1] on the device (`out` when given)."""
+    if out is None:
+        _own_buffers(stream, "vardrop_grad_norm", out=out)
+        out = torch.empty(1, dtype=torch.float32, device=ctx.device)
+    rc = ctx._lib.vardrop_grad_norm(ctx.handle, tensors.pointer, out.data_ptr(), _stream(tensors.table, stream))
+    if rc:
+        ctx.check(rc, "vardrop_grad_norm")
+    return out
+
+
+def vardrop_clip_grads(ctx, tensors, norm, max_norm, status=None, stream=None):
+    """Gradients times min(1, max_norm / (norm + 1e-6)) into the list's `clipped` tensors (in place without them)."""
+    rc = ctx._lib.vardrop_clip_grads(ctx.handle, tensors.pointer, _p(norm), max_norm, _p(status), _stream(tensors.table, stream))
+    if rc:
+        ctx.check(rc, "vardrop_clip_grads")
+
+
+def vardrop_adamw(ctx, tensors, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, norm=None, max_norm=0.0, status=None, stream=None):
+    """AdamW step number `step` (from 1) of a TensorList with params; with `norm` and max_norm the gradients are clipped in it."""
+    rc = ctx._lib.vardrop_adamw(ctx.handle, tensors.pointer, lr, beta1, beta2, eps, step, _p(norm), max_norm, _p(status),
+                                _stream(tensors.table, stream))
+    if rc:
+        ctx.check(rc, "vardrop_adamw")
+
+
+def vardrop_adamw_dev(ctx, tensors, lr_dev, step_dev, beta1=0.9, beta2=0.999, eps=1e-8, norm=None, max_norm=0.0, advance=True,
+                      status=None, stream=None):
+    """vardrop_adamw with the rate (float32 [1]) and the number of steps done (int64 [1], advanced) in device memory."""
+    rc = ctx._lib.vardrop_adamw_dev(ctx.handle, tensors.pointer, _p(lr_dev), beta1, beta2, eps, _p(step_dev), 1 if advance else 0,
+                                    _p(norm), max_norm, _p(status), _stream(tensors.table, stream))
+    if rc:
+        ctx.check(rc, "vardrop_adamw_dev")
