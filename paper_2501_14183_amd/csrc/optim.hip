@@ -5,7 +5,7 @@
 //   AdamW:  m' = b1 m + (1 - b1) s g,  v' = b2 v + (1 - b2) (s g)^2,
 //           p' = p (1 - lr decay) - lr m' / (1 - b1^t) / (sqrt(v' / (1 - b2^t)) + eps)
 //
-// A tensor list is laid out once in the caller's memory: all tensors cut into chunks of at most kChunk elements, 64 bytes of
+// A tensor list is laid out once in the caller's memory: all tensors cut into chunks, 64 bytes of
 // addresses each, so that a launch walks over chunks whatever the number and the sizes of the tensors.  All three calls are
 // bound by memory.
 #include "common.h"
@@ -14,12 +14,14 @@
 
 namespace {
 
-constexpr int kChunk = 4096;                 // elements per chunk
 constexpr int kThreads = 256;
-constexpr int kUnits = kChunk / (4 * kThreads);
 constexpr int kMaxParts = 2048;              // workgroups of the norm, one partial sum each
+constexpr int kTicket = 32;                  // workgroups that share a counter
 constexpr int kRecords = 48;                 // tensors per launch of the layout kernel (its arguments hold them)
 constexpr uint32_t kBuilt = 0x56445431u;
+
+constexpr int U = 4;                         // fours of a thread
+constexpr int kChunk = 4 * U * kThreads;     // elements of a chunk
 
 struct Chunk {
   void* grad;
@@ -36,10 +38,15 @@ struct Chunk {
 static_assert(sizeof(Chunk) == 64, "");
 enum { kGradBf16 = 1, kClipBf16 = 2 };
 
-// Head of the table: counters of finished workgroups (zero between launches), then the norm's partial sums, then the chunks.
+// Counters of finished workgroups, zero between launches.  Increments of one address follow each other at about 12 ns, so kTicket
+// workgroups share a counter and the last of them counts for all at the top (a line of memory each).
+struct Tickets {
+  uint32_t group[kMaxParts / kTicket][32];
+  uint32_t top[32];
+};
+// Head of the table; the chunks follow.
 struct Head {
-  uint32_t norm_done, step_done;
-  uint32_t pad[62];
+  Tickets norm, step;
   double part[kMaxParts];
 };
 
@@ -57,10 +64,8 @@ struct Records {
 static_assert(sizeof(Records) <= 3800, "kernel arguments");
 
 __global__ __launch_bounds__(256) void list_kernel(Records a, Head* head, Chunk* chunks, int clear) {
-  if (clear && blockIdx.x == 0 && threadIdx.x == 0) {
-    head->norm_done = 0;
-    head->step_done = 0;
-  }
+  if (clear && blockIdx.x == 0)
+    for (int i = threadIdx.x; i < (int)(2 * sizeof(Tickets) / 4); i += blockDim.x) ((uint32_t*)head)[i] = 0;
   const Record r = a.r[blockIdx.x];
   const long long n = (r.numel + kChunk - 1) / kChunk;
   for (long long i = threadIdx.x; i < n; i += blockDim.x) {
@@ -80,55 +85,47 @@ __global__ __launch_bounds__(256) void list_kernel(Records a, Head* head, Chunk*
   }
 }
 
-// Four neighbouring elements; tensors need no more than element alignment.
-typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(2)));
-__device__ inline void load4(const float* p, int left, float (&v)[4]) {
-  if (left >= 4) {
-    const f32x4u t = *reinterpret_cast<const f32x4u*>(p);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = t[e];
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = e < left ? p[e] : 0.f;
-  }
+// Four neighbouring elements of a tensor; tensors need no more than element alignment.  (The addresses come from the table: the
+// address space has to be named, or the compiler takes them for addresses that may be LDS.)
+template <typename T> using gptr = __attribute__((address_space(1))) T*;
+template <typename T> struct Four;
+template <> struct Four<float> {
+  typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
+  __device__ static float get(const vec& t, int e) { return t[e]; }
+  __device__ static vec put(const float (&v)[4]) { return vec{v[0], v[1], v[2], v[3]}; }
+  __device__ static float one(float t) { return t; }
+  __device__ static float round(float t) { return t; }
+};
+template <> struct Four<bf16_t> {
+  typedef uint32_t vec __attribute__((ext_vector_type(2), aligned(2)));
+  __device__ static float get(const vec& t, int e) { return __uint_as_float(e & 1 ? t[e >> 1] & 0xffff0000u : t[e >> 1] << 16); }
+  __device__ static vec put(const float (&v)[4]) { return vec{pack2(v[0], v[1]), pack2(v[2], v[3])}; }
+  __device__ static float one(bf16_t t) { return bf2f(t); }
+  __device__ static bf16_t round(float t) { return f2bf(t); }
+};
+// kOnce: data that no kernel reads again soon, not kept in the caches.
+template <typename T, bool kOnce = false> __device__ inline typename Four<T>::vec load4(const void* p, int at) {
+  const auto q = (gptr<const typename Four<T>::vec>)((gptr<const T>)(const T*)p + at);
+  return kOnce ? __builtin_nontemporal_load(q) : *q;
 }
-__device__ inline void load4(const bf16_t* p, int left, float (&v)[4]) {
-  if (left >= 4) {
-    const u32x2u t = *reinterpret_cast<const u32x2u*>(p);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(e & 1 ? t[e >> 1] & 0xffff0000u : t[e >> 1] << 16);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = e < left ? bf2f(p[e]) : 0.f;
-  }
+template <typename T, bool kOnce = false> __device__ inline void store4(void* p, int at, const float (&v)[4]) {
+  const auto q = (gptr<typename Four<T>::vec>)((gptr<T>)(T*)p + at);
+  if (kOnce) __builtin_nontemporal_store(Four<T>::put(v), q);
+  else *q = Four<T>::put(v);
 }
-__device__ inline void store4(float* p, int left, const float (&v)[4]) {
-  if (left >= 4) {
-    *reinterpret_cast<f32x4u*>(p) = f32x4u{v[0], v[1], v[2], v[3]};
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e < left) p[e] = v[e];
-  }
-}
-__device__ inline void store4(bf16_t* p, int left, const float (&v)[4]) {
-  if (left >= 4) {
-    *reinterpret_cast<u32x2u*>(p) = u32x2u{pack2(v[0], v[1]), pack2(v[2], v[3])};
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e < left) p[e] = f2bf(v[e]);
-  }
-}
-__device__ inline void load_grads(const Chunk& c, float (&g)[kUnits][4]) {
-#pragma unroll
-  for (int u = 0; u < kUnits; ++u) {
-    const int at = (u * kThreads + threadIdx.x) * 4;
-    if (c.flags & kGradBf16) load4((const bf16_t*)c.grad + at, c.count - at, g[u]);
-    else load4((const float*)c.grad + at, c.count - at, g[u]);
-  }
-}
+template <typename T> __device__ inline float load1(const void* p, int at) { return Four<T>::one(((gptr<const T>)(const T*)p)[at]); }
+template <typename T> __device__ inline void store1(void* p, int at, float v) { ((gptr<T>)(T*)p)[at] = Four<T>::round(v); }
+
+// A chunk of `count` elements: thread t of a workgroup has the fours at 4 (u kThreads + t), u < U, as far as they are whole
+// ones, and the first three threads one each of the elements behind the last whole four.
+struct Places {
+  int count;
+  __device__ explicit Places(int n) : count(n) {}
+  __device__ int at(int u) const { return (u * kThreads + threadIdx.x) * 4; }
+  __device__ bool whole(int u) const { return at(u) + 4 <= count; }
+  __device__ int rest() const { return (count & ~3) + threadIdx.x; }
+  __device__ bool has_rest() const { return rest() < count; }
+};
 
 __device__ inline double wave_sum(double v) {
 #pragma unroll
@@ -147,28 +144,56 @@ __device__ inline double block_sum(double v, double* red) {
   return v;
 }
 
+// True in the one workgroup of the grid (at most kMaxParts) that comes last.  By one thread, which has waited for what the
+// others' reads and writes before this call have to be done with.
+__device__ inline bool comes_last(Tickets* t) {
+  auto count = [](uint32_t* p) { return __hip_atomic_fetch_add(p, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+  auto reset = [](uint32_t* p) { __hip_atomic_store(p, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+  const uint32_t group = blockIdx.x / kTicket, groups = (gridDim.x + kTicket - 1) / kTicket;
+  if (count(t->group[group]) != min((uint32_t)kTicket, gridDim.x - group * kTicket) - 1) return false;
+  reset(t->group[group]);
+  if (count(t->top) != groups - 1) return false;
+  reset(t->top);
+  return true;
+}
+
 // Squares are formed and added in 64 bits: no gradient is too large or too small for its square, and the sum keeps every digit the
 // result has.  The workgroup that finishes last adds the partial sums in their order, so the result does not depend on which it was.
 __global__ __launch_bounds__(kThreads) void grad_norm_kernel(Head* head, const Chunk* __restrict__ chunks, int n, float* norm) {
   __shared__ double red[kThreads / 64];
   __shared__ bool last;
   double s[4] = {0.0, 0.0, 0.0, 0.0};
+  auto add = [&](float v, int e) { s[e] = fma((double)v, (double)v, s[e]); };
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const Chunk c = chunks[i];
-    float g[kUnits][4];
-    load_grads(c, g);
+    const Places at(c.count);
+    auto sum = [&](auto type) {
+      typedef decltype(type) T;
+      typename Four<T>::vec g[U];
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const double x = (double)g[u][e];
-        s[e] = fma(x, x, s[e]);
+      for (int u = 0; u < U; ++u) {
+        g[u] = typename Four<T>::vec{};
+        if (at.whole(u)) g[u] = load4<T>(c.grad, at.at(u));
       }
+      float one = 0.f;
+      if (at.has_rest()) one = load1<T>(c.grad, at.rest());
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) add(Four<T>::get(g[u], e), e);
+      add(one, 0);
+    };
+    if (c.flags & kGradBf16) sum(bf16_t{});
+    else sum(float{});
   }
   const double mine = block_sum((s[0] + s[1]) + (s[2] + s[3]), red);
   if (threadIdx.x == 0) {
     __hip_atomic_store(&head->part[blockIdx.x], mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    last = __hip_atomic_fetch_add(&head->norm_done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+    // The store and the later loads of the partial sums are atomic, so they bypass what this die caches; with the wait in
+    // between the sum is in memory before it is counted, and no cache has to be written back (a release by every workgroup
+    // made this kernel 58 us instead of 32 at 10.5 million gradients).
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    last = comes_last(&head->norm);
   }
   __syncthreads();
   if (!last) return;
@@ -176,10 +201,7 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(Head* head, const C
   for (int i = threadIdx.x; i < (int)gridDim.x; i += kThreads)
     t += __hip_atomic_load(&head->part[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   t = block_sum(t, red);
-  if (threadIdx.x == 0) {
-    *norm = (float)sqrt(t);
-    __hip_atomic_store(&head->norm_done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
+  if (threadIdx.x == 0) *norm = (float)sqrt(t);
 }
 
 // Factor of the gradients; false when the norm is not finite.
@@ -202,17 +224,28 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(const Chunk* __restrict_
     const Chunk c = chunks[i];
     void* out = c.clip ? c.clip : c.grad;
     if (out == c.grad && s == 1.f) continue;          // in place and short enough: nothing changes
-    const bool bf16 = c.flags & (c.clip ? kClipBf16 : kGradBf16);
-    float g[kUnits][4];
-    load_grads(c, g);
+    const Places at(c.count);
+    auto scale = [&](auto from, auto to) {
+      typedef decltype(from) T;
+      typedef decltype(to) R;
+      typename Four<T>::vec g[U];
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const int at = (u * kThreads + threadIdx.x) * 4;
+      for (int u = 0; u < U; ++u)
+        if (at.whole(u)) g[u] = load4<T>(c.grad, at.at(u));
+      float one = 0.f;
+      if (at.has_rest()) one = load1<T>(c.grad, at.rest());
 #pragma unroll
-      for (int e = 0; e < 4; ++e) g[u][e] *= s;
-      if (bf16) store4((bf16_t*)out + at, c.count - at, g[u]);
-      else store4((float*)out + at, c.count - at, g[u]);
-    }
+      for (int u = 0; u < U; ++u) {
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = s * Four<T>::get(g[u], e);
+        if (at.whole(u)) store4<R>(out, at.at(u), v);
+      }
+      if (at.has_rest()) store1<R>(out, at.rest(), s * one);
+    };
+    const bool from = c.flags & kGradBf16, to = c.flags & (c.clip ? kClipBf16 : kGradBf16);
+    if (from) to ? scale(bf16_t{}, bf16_t{}) : scale(bf16_t{}, float{});
+    else to ? scale(float{}, bf16_t{}) : scale(float{}, float{});
   }
 }
 
@@ -228,54 +261,79 @@ struct Adam {
   int32_t* status;
 };
 
+template <bool kOnce>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(Head* head, const Chunk* __restrict__ chunks, int n, Adam a) {
-  float s;
-  if (!clip_factor(a.norm, a.max_norm, s)) {
-    if (a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = 1;
-    return;
-  }
+  float s = 1.f;
   int64_t t = 0;
-  if (a.step_dev) {                    // (the host has filled `rate` and `root` in otherwise)
-    t = *a.step_dev + 1;
-    a.lr = *a.lr_dev;
-    a.rate = (float)((double)a.lr / -expm1((double)t * a.log_b1));
-    a.root = (float)(1.0 / sqrt(-expm1((double)t * a.log_b2)));
-  }
-  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+  bool ready = false, sound = true;
+  // What the whole step shares, asked for when the first chunk is on its way.
+  auto prepare = [&]() {
+    ready = true;
+    sound = clip_factor(a.norm, a.max_norm, s);
+    if (!sound && a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = 1;
+    if (a.step_dev) {                  // (the host has filled `rate` and `root` in otherwise)
+      t = *a.step_dev + 1;
+      a.lr = *a.lr_dev;
+      a.rate = (float)((double)a.lr / -expm1((double)t * a.log_b1));
+      a.root = (float)(1.0 / sqrt(-expm1((double)t * a.log_b2)));
+    }
+  };
+  for (int i = blockIdx.x; i < n && sound; i += gridDim.x) {
     const Chunk c = chunks[i];
-    float g[kUnits][4], p[kUnits][4], m[kUnits][4], v[kUnits][4];
-    load_grads(c, g);
+    const Places at(c.count);
+    auto move = [&](float g, float& p, float& m, float& v) {
+      const float x = s * g;
+      m = fmaf(a.b1, m, a.c1 * x);
+      v = fmaf(a.b2, v, a.c2 * x * x);
+      p = fmaf(-a.rate, m / fmaf(sqrtf(v), a.root, a.eps), (1.f - a.lr * c.decay) * p);
+    };
+    auto update = [&](auto type) {
+      typedef decltype(type) T;
+      typename Four<T>::vec g[U];
+      Four<float>::vec p[U], m[U], v[U];
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const int at = (u * kThreads + threadIdx.x) * 4, left = c.count - at;
-      load4(c.param + at, left, p[u]);
-      load4(c.m + at, left, m[u]);
-      load4(c.v + at, left, v[u]);
-    }
-    const float keep = 1.f - a.lr * c.decay;
+      for (int u = 0; u < U; ++u)
+        if (at.whole(u)) {
+          g[u] = load4<T, kOnce>(c.grad, at.at(u));
+          p[u] = load4<float, kOnce>(c.param, at.at(u));
+          m[u] = load4<float, kOnce>(c.m, at.at(u));
+          v[u] = load4<float, kOnce>(c.v, at.at(u));
+        }
+      if (!ready) prepare();
+      if (!sound) return;
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const int at = (u * kThreads + threadIdx.x) * 4, left = c.count - at;
+      for (int u = 0; u < U; ++u)
+        if (at.whole(u)) {
+          float np[4], nm[4], nv[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = s * g[u][e];
-        m[u][e] = fmaf(a.b1, m[u][e], a.c1 * x);
-        v[u][e] = fmaf(a.b2, v[u][e], a.c2 * x * x);
-        p[u][e] = fmaf(-a.rate, m[u][e] / fmaf(sqrtf(v[u][e]), a.root, a.eps), keep * p[u][e]);
+          for (int e = 0; e < 4; ++e) {
+            np[e] = p[u][e];
+            nm[e] = m[u][e];
+            nv[e] = v[u][e];
+            move(Four<T>::get(g[u], e), np[e], nm[e], nv[e]);
+          }
+          store4<float, kOnce>(c.param, at.at(u), np);
+          store4<float, kOnce>(c.m, at.at(u), nm);
+          store4<float, kOnce>(c.v, at.at(u), nv);
+          if (c.weight) store4<bf16_t>(c.weight, at.at(u), np);
+        }
+      if (at.has_rest()) {
+        const int k = at.rest();
+        float p1 = load1<float>(c.param, k), m1 = load1<float>(c.m, k), v1 = load1<float>(c.v, k);
+        move(load1<T>(c.grad, k), p1, m1, v1);
+        store1<float>(c.param, k, p1);
+        store1<float>(c.m, k, m1);
+        store1<float>(c.v, k, v1);
+        if (c.weight) store1<bf16_t>(c.weight, k, p1);
       }
-      store4(c.param + at, left, p[u]);
-      store4(c.m + at, left, m[u]);
-      store4(c.v + at, left, v[u]);
-      if (c.weight) store4(c.weight + at, left, p[u]);
-    }
+    };
+    if (c.flags & kGradBf16) update(bf16_t{});
+    else update(float{});
   }
   if (a.step_dev && a.advance) {       // whoever finishes last: all others have read the counter
+    if (!ready) prepare();             // (a list without elements)
     __syncthreads();
-    if (threadIdx.x == 0 &&
-        __hip_atomic_fetch_add(&head->step_done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1) {
-      *a.step_dev = t;
-      __hip_atomic_store(&head->step_done, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
+    if (sound && threadIdx.x == 0 && comes_last(&head->step)) *a.step_dev = t;
   }
 }
 
@@ -283,6 +341,12 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Head* head, const Chunk
 Head* head_of(const vardrop_tensor_list* l) { return (Head*)l->table; }
 Chunk* chunks_of(const vardrop_tensor_list* l) { return (Chunk*)((char*)l->table + sizeof(Head)); }
 enum { kHasParams = 1 };
+
+// Weights and moments are next read a step later.  A large model's have left the caches by then, and what they pushed out on their
+// way is written back in the next kernels' time: they pass the caches by.  Norm and step with fp32 gradients, kept ->
+// passed by, us: 4.3 million weights 27.5 -> 30.6, 8.5 61.5 -> 52.2 (one list over and over: 49.9 -> 51.3), 12.7 87.2 -> 74.6 (70.3 ->
+// 74.6), 25 170 -> 143 (167 -> 142), 57 391 -> 333 (395 -> 318).
+constexpr int64_t kOnceAbove = 6000000;
 
 int check_list(const vardrop_ctx* ctx, const vardrop_tensor_list* l) {
   if (!ctx || !l || l->built != kBuilt || !l->table || l->chunks < 0) return VARDROP_EINVAL;
@@ -310,7 +374,9 @@ int adamw(vardrop_ctx* ctx, const vardrop_tensor_list* l, Adam a, double beta1, 
   }
   hipStream_t s = (hipStream_t)stream;
   VdTimer timer(ctx, VARDROP_K_ADAMW, s);
-  VD_KERNEL(ctx, adamw_kernel, dim3(blocks_for(l, 8 * ctx->num_cus)), dim3(kThreads), 0, s, head_of(l), chunks_of(l), l->chunks, a);
+  const dim3 grid(blocks_for(l, kMaxParts)), block(kThreads);
+  if (l->numel > kOnceAbove) VD_KERNEL(ctx, adamw_kernel<true>, grid, block, 0, s, head_of(l), chunks_of(l), l->chunks, a);
+  else VD_KERNEL(ctx, adamw_kernel<false>, grid, block, 0, s, head_of(l), chunks_of(l), l->chunks, a);
   VD_LAUNCH_CHECK(ctx);
   return VARDROP_OK;
 }
@@ -360,6 +426,7 @@ extern "C" int vardrop_tensor_list_build(vardrop_ctx* ctx, int tensors, const in
   l.tensors = tensors;
   l.has = params ? kHasParams : 0;
   l.built = kBuilt;
+  for (int i = 0; i < tensors; ++i) l.numel += numel_host[i];
   hipStream_t s = (hipStream_t)stream;
   int done = 0;
   bool clear = true;
@@ -381,7 +448,6 @@ extern "C" int vardrop_tensor_list_build(vardrop_ctx* ctx, int tensors, const in
       r.flags = (grad_dtype_host && grad_dtype_host[done] == VARDROP_BF16 ? kGradBf16 : 0) |
                 (clip_host && clip_dtype_host && clip_dtype_host[done] == VARDROP_BF16 ? kClipBf16 : 0);
       l.chunks += (int)((r.numel + kChunk - 1) / kChunk);
-      l.numel += r.numel;
     }
     if (k == 0 && !clear) break;
     hipLaunchKernelGGL(list_kernel, dim3(k ? k : 1), dim3(256), 0, s, a, head_of(&l), chunks_of(&l), clear ? 1 : 0);
@@ -412,7 +478,7 @@ extern "C" int vardrop_clip_grads(vardrop_ctx* ctx, const vardrop_tensor_list* l
   if (list->chunks == 0) return VARDROP_OK;
   hipStream_t s = (hipStream_t)stream;
   VdTimer timer(ctx, VARDROP_K_CLIP, s);
-  VD_KERNEL(ctx, clip_kernel, dim3(blocks_for(list, 8 * ctx->num_cus)), dim3(kThreads), 0, s, chunks_of(list), list->chunks, norm,
+  VD_KERNEL(ctx, clip_kernel, dim3(blocks_for(list, kMaxParts)), dim3(kThreads), 0, s, chunks_of(list), list->chunks, norm,
             max_norm, status);
   VD_LAUNCH_CHECK(ctx);
   return VARDROP_OK;
