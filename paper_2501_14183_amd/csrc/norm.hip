@@ -17,76 +17,101 @@
 #include "common.h"
 #include "bf16_mfma.h"
 #include <initializer_list>
+#include <type_traits>
 
 namespace {
 
 constexpr int kVec = 4;                  // neighbouring elements of a row that a lane holds per chunk
 constexpr int kMaxD = 8192;
 
-// A row of d elements belongs to LPR lanes with CH chunks each: element ((c * LPR + lane) * kVec + e).  Rows need no
-// alignment: global loads and stores take any element-aligned address.
+// A row of d elements belongs to LPR lanes with CH chunks each: element ((c * LPR + lane) * kVec + e).  All chunks but the last
+// are whole; how the last one ends (End) is part of a kernel's type: d is a multiple of what the lanes hold; of kVec only; not of
+// kVec; less than kVec.
+enum End { kWhole, kCut, kRagged, kTiny };
+
+// All tensors are reached through buffer descriptors that begin at the wavefront's row: what is not there (a tensor that was
+// not given, lanes past the end of a row, rows past the last) lies outside a descriptor's range, where loads give zero and
+// stores are dropped.  So a row's loads and stores stand without branches, and the wait for the loads of the next row need
+// not wait for the stores of this one: with branches the compiler cannot count the stores behind the loads (backward of 39 062 x 640
+// bf16 93 us instead of 66).  Rows need element alignment only.
+typedef __amdgpu_buffer_rsrc_t Window;
+constexpr int kRange = 1 << 28, kOutside = 1 << 28;      // bytes; elements, of two bytes or more
+template <typename T> __device__ inline Window window(const void* tensor, long long first) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)((const T*)tensor + first), 0, tensor ? kRange : 0, 0x00020000);
+}
+
+typedef uint32_t raw4 __attribute__((ext_vector_type(4)));
+typedef uint32_t raw2 __attribute__((ext_vector_type(2)));
 template <typename T> struct Unit;
 template <> struct Unit<float> {
-  typedef float vec __attribute__((ext_vector_type(4), aligned(4)));
-  float v[4];
-  __device__ float get(int e) const { return v[e]; }
-  __device__ void load(const float* p) {
-    const vec t = *reinterpret_cast<const vec*>(p);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = t[e];
+  raw4 v;
+  __device__ float get(int e) const { return __uint_as_float(v[e]); }
+  __device__ void load(Window w, int at) { v = __builtin_amdgcn_raw_buffer_load_b128(w, at * 4, 0, 0); }
+  __device__ void load1(Window w, int at, int e) { v[e] = __builtin_amdgcn_raw_buffer_load_b32(w, at * 4, 0, 0); }
+  __device__ void fill(float f) { v = __float_as_uint(f); }
+  // the elements from the k-th on, k < 4, zeros behind them
+  __device__ void drop(int k) {
+    if (k & 1) v = raw4{v[1], v[2], v[3], 0};
+    if (k & 2) v = raw4{v[2], v[3], 0, 0};
   }
-  __device__ void load1(const float* p, int e) { v[e] = p[e]; }
-  __device__ void zero() { v[0] = v[1] = v[2] = v[3] = 0.f; }
-  __device__ static void store(float* p, const float (&t)[4]) { *reinterpret_cast<vec*>(p) = vec{t[0], t[1], t[2], t[3]}; }
-  __device__ static void store1(float* p, float t) { *p = t; }
+  template <int kCache> __device__ static void store(Window w, int at, const float (&t)[4]) {
+    __builtin_amdgcn_raw_buffer_store_b128(raw4{__float_as_uint(t[0]), __float_as_uint(t[1]), __float_as_uint(t[2]), __float_as_uint(t[3])}, w, at * 4, 0, kCache);
+  }
+  __device__ static void store1(Window w, int at, float t) { __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(t), w, at * 4, 0, 0); }
 };
 template <> struct Unit<bf16_t> {
-  typedef uint32_t vec __attribute__((ext_vector_type(2), aligned(2)));
-  uint32_t v[2];
+  raw2 v;
   __device__ float get(int e) const { return __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16); }
-  __device__ void load(const bf16_t* p) {
-    const vec t = *reinterpret_cast<const vec*>(p);
-    v[0] = t.x;
-    v[1] = t.y;
+  __device__ void load(Window w, int at) { v = __builtin_amdgcn_raw_buffer_load_b64(w, at * 2, 0, 0); }
+  __device__ void load1(Window w, int at, int e) {
+    const uint32_t t = __builtin_amdgcn_raw_buffer_load_b16(w, at * 2, 0, 0);
+    v[e >> 1] = e & 1 ? v[e >> 1] | t << 16 : t;
   }
-  __device__ void load1(const bf16_t* p, int e) { v[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1)); }
-  __device__ void zero() { v[0] = v[1] = 0; }
-  __device__ static void store(bf16_t* p, const float (&t)[4]) { *reinterpret_cast<vec*>(p) = vec{pack2(t[0], t[1]), pack2(t[2], t[3])}; }
-  __device__ static void store1(bf16_t* p, float t) { *p = f2bf(t); }
+  __device__ void fill(float f) { v = f2bf(f) * 0x10001u; }
+  __device__ void drop(int k) {
+    const uint64_t t = ((uint64_t)v[1] << 32 | v[0]) >> (16 * k);
+    v = raw2{(uint32_t)t, (uint32_t)(t >> 32)};
+  }
+  template <int kCache> __device__ static void store(Window w, int at, const float (&t)[4]) {
+    __builtin_amdgcn_raw_buffer_store_b64(raw2{pack2(t[0], t[1]), pack2(t[2], t[3])}, w, at * 2, 0, kCache);
+  }
+  __device__ static void store1(Window w, int at, float t) { __builtin_amdgcn_raw_buffer_store_b16(f2bf(t), w, at * 2, 0, 0); }
 };
 
-// the chunk that begins at element `at` of a row of d; elements past its end are zero
-template <typename T> __device__ inline Unit<T> load_unit(const T* row, int at, int d) {
-  Unit<T> u;
-  if (at + kVec <= d) {
-    u.load(row + at);
-  } else {
-    u.zero();
-    for (int e = 0; e < kVec; ++e)
-      if (at + e < d) u.load1(row + at, e);
-  }
-  return u;
-}
-template <typename T> __device__ inline void store_unit(T* row, int at, int d, const float (&t)[4]) {
-  if (at + kVec <= d) {
-    Unit<T>::store(row + at, t);
-  } else {
+// Where a lane's chunk lies in a window whose rows are d apart: `sub` rows behind the window's first, nowhere unless `active`.
+template <End kEnd> struct Spot {
+  int at, d, base;
+  bool active;
+  __device__ Spot(int at_, int d_, int sub, bool active_) : at(at_), d(d_), base(sub * d_), active(active_) {}
+  __device__ int one(int e) const { return active && at + e < d ? base + at + e : kOutside; }
+  template <typename T> __device__ void load(Unit<T>& u, Window w) const {
+    if constexpr (kEnd == kTiny) {
 #pragma unroll
-    for (int e = 0; e < kVec; ++e)
-      if (at + e < d) Unit<T>::store1(row + at + e, t[e]);
+      for (int e = 0; e < kVec; ++e) u.load1(w, one(e), e);
+    } else {
+      // (a ragged chunk is cut from the last four elements of the row, see trim)
+      const int from = kEnd == kRagged ? min(at, d - kVec) : at;
+      u.load(w, active && (kEnd == kWhole || at < d) ? base + from : kOutside);
+    }
   }
-}
-// a vector of parameters; `none` stands for an absent one, 0 for elements past the end
-template <typename T> __device__ inline void load_param(const T* p, int at, int d, float none, float (&out)[4]) {
-  if (!p) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) out[e] = at + e < d ? none : 0.f;
-    return;
+  // after the wait: brings a loaded chunk into place
+  template <typename T> __device__ void trim(Unit<T>& u) const {
+    if constexpr (kEnd == kRagged) u.drop(at < d ? max(0, at - (d - kVec)) : 0);
   }
-  const Unit<T> u = load_unit(p, at, d);
+  // past: no copy is left in the caches (see kPastCaches)
+  template <typename T, bool kPast = false> __device__ void store(Window w, const float (&t)[4]) const {
+    constexpr int kNontemporal = 2;
+    if constexpr (kEnd != kTiny) {
+      const int to = active && (kEnd == kWhole || at + kVec <= d) ? base + at : kOutside;
+      Unit<T>::template store<kPast ? kNontemporal : 0>(w, to, t);
+    }
+    if constexpr (kEnd == kRagged || kEnd == kTiny) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) out[e] = u.get(e);
-}
+      for (int e = 0; e < kVec - 1; ++e) Unit<T>::store1(w, at + kVec > d ? one(e) : kOutside, t[e]);
+    }
+  }
+  __device__ bool has(int e) const { return kEnd == kWhole || at + e < d; }
+};
 
 template <int CTRL> __device__ inline float dpp_add(float v) {
   return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
@@ -137,6 +162,7 @@ struct NormArgs {
   float* stats;                            // [rows][4]: mean and rstd of post, mean and rstd of pre
   float* part;                             // backward: [segments * pieces][4][d] of T0, T1, S0, S1
   int B, n, d, gates, pre, post, pieces;
+  bool past;                               // forward: h is written past the caches
   float alpha, beta, eps;
   const int32_t* n_dev;
   int32_t* status;
@@ -144,107 +170,125 @@ struct NormArgs {
 
 template <int LPR> constexpr int threads_of() { return LPR > 256 ? LPR : 256; }
 
-// One row per group of LPR lanes.  The statistics are taken from fp32 values before r is rounded, deviations about the mean.
-template <typename TR, typename TB, int LPR, int CH>
+// Calls body(c, spot) for every chunk.
+template <int LPR, int CH, End kEnd, typename F> __device__ inline void for_chunks(int d, int sub, bool active, F body) {
+  const int lane = threadIdx.x % LPR;
+#pragma unroll
+  for (int c = 0; c < CH - 1; ++c) body(c, Spot<kWhole>((c * LPR + lane) * kVec, d, sub, active));
+  body(CH - 1, Spot<kEnd>(((CH - 1) * LPR + lane) * kVec, d, sub, active));
+}
+// A wavefront's first group of lanes, the same in all its lanes, and a lane's group behind that.
+template <int LPR> __device__ inline int first_group() {
+  return LPR <= 64 ? __builtin_amdgcn_readfirstlane((int)(threadIdx.x / 64)) * (64 / LPR) : 0;
+}
+template <int LPR> __device__ inline int sub_group() { return LPR < 64 ? (int)(threadIdx.x % 64) / LPR : 0; }
+
+// One row per group of LPR lanes.  Everything a row needs is asked for at once.  The statistics are taken from fp32 values before
+// r is rounded, deviations about the mean.
+template <typename TR, typename TB, int LPR, int CH, End kEnd>
 __global__ __launch_bounds__(threads_of<LPR>()) void block_norm_fwd_kernel(NormArgs a) {
   constexpr int T = threads_of<LPR>();
   __shared__ float red[LPR > 64 ? 2 * LPR / 64 : 1][1];
   int n;
   if (!vd_count(a.n_dev, a.n, n, a.status)) return;
   const long long rows = (long long)a.B * n;
-  const int lane = threadIdx.x % LPR, d = a.d;
+  const int d = a.d, sub = sub_group<LPR>();
   const float inv_d = 1.f / (float)d;
   int turn = 0;
-  for (long long row = (long long)blockIdx.x * (T / LPR) + threadIdx.x / LPR; row < rows; row += (long long)gridDim.x * (T / LPR)) {
-    const long long off = row * d;
-    const TB* gate = a.gate ? (const TB*)a.gate + (a.gates > 1 ? (long long)((uint32_t)row / (uint32_t)n) * d : 0) : nullptr;
-
-    Unit<TR> xr[CH];
-    Unit<TB> fr[CH];
-  #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int at = (c * LPR + lane) * kVec;
-      xr[c] = load_unit((const TR*)a.x + off, at, d);
-      if (a.f) fr[c] = load_unit((const TB*)a.f + off, at, d);
+  for (long long row = (long long)blockIdx.x * (T / LPR) + first_group<LPR>(); row < rows; row += (long long)gridDim.x * (T / LPR)) {
+    const bool active = LPR >= 64 || row + sub < rows;
+    const Window wx = window<TR>(a.x, row * d), wf = window<TB>(a.f, row * d);
+    int gate = 0, sub_gate = 0;
+    if (a.gates > 1) {
+      gate = (int)((uint32_t)row / (uint32_t)n);
+      if (LPR < 64) sub_gate = (int)((uint32_t)(row + sub) / (uint32_t)n) - gate;
     }
+    const Window wg = window<TB>(a.gate, (long long)gate * d), wwp = window<TB>(a.wp, 0), wbp = window<TB>(a.bp, 0),
+                 ww = window<TB>(a.w, 0), wb = window<TB>(a.b, 0);
+
+    Unit<TR> x[CH];
+    Unit<TB> f[CH], g[CH], wp[CH], bp[CH], w[CH], b[CH];
+    for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) {
+      at.load(x[c], wx);
+      at.load(f[c], wf);
+    });
+    for_chunks<LPR, CH, kEnd>(d, sub_gate, active, [&](int c, auto at) { at.load(g[c], wg); });
+    for_chunks<LPR, CH, kEnd>(d, 0, true, [&](int c, auto at) {
+      at.load(wp[c], wwp);
+      at.load(bp[c], wbp);
+      at.load(w[c], ww);
+      at.load(b[c], wb);
+    });
+    for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) {
+      at.trim(x[c]);
+      at.trim(f[c]);
+      at.trim(g[c]);
+      at.trim(wp[c]);
+      at.trim(bp[c]);
+      at.trim(w[c]);
+      at.trim(b[c]);
+      if (!a.gate) g[c].fill(1.f);
+      if (!a.wp) wp[c].fill(1.f);
+      if (!a.w) w[c].fill(1.f);
+    });
     float v[CH][4];
     float mean_p = 0.f, rstd_p = 1.f, mean = 0.f, rstd = 1.f;
     auto moments = [&](int kind, float& m, float& k) {
-      m = 0.f;
-      k = 1.f;
       if (kind == VARDROP_NORM_NONE) return;
       if (kind == VARDROP_NORM_LAYER) {
         float s[1] = {0.f};
-  #pragma unroll
+#pragma unroll
         for (int c = 0; c < CH; ++c)
-  #pragma unroll
+#pragma unroll
           for (int e = 0; e < 4; ++e) s[0] += v[c][e];
         row_sum<LPR>(s, red, turn);
         m = s[0] * inv_d;
       }
       float q[1] = {0.f};
-  #pragma unroll
-      for (int c = 0; c < CH; ++c)
-  #pragma unroll
+      for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) {
+#pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float t = (c * LPR + lane) * kVec + e < d ? v[c][e] - m : 0.f;
+          const float t = at.has(e) ? v[c][e] - m : 0.f;
           q[0] = fmaf(t, t, q[0]);
         }
+      });
       row_sum<LPR>(q, red, turn);
       k = 1.f / sqrtf(q[0] * inv_d + a.eps);
     };
-    if (a.f) {
-  #pragma unroll
-      for (int c = 0; c < CH; ++c)
-  #pragma unroll
-        for (int e = 0; e < 4; ++e) v[c][e] = fr[c].get(e);
-      moments(a.post, mean_p, rstd_p);
-  #pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        const int at = (c * LPR + lane) * kVec;
-        float wp[4], bp[4], g[4];
-        load_param((const TB*)a.wp, at, d, 1.f, wp);
-        load_param((const TB*)a.bp, at, d, 0.f, bp);
-        load_param(gate, at, d, 1.f, g);
-  #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float u = fmaf((v[c][e] - mean_p) * rstd_p, wp[e], bp[e]);
-          v[c][e] = fmaf(a.beta * g[e], u, a.alpha * xr[c].get(e));
-        }
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[c][e] = f[c].get(e);
+    moments(a.post, mean_p, rstd_p);
+    for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float u = fmaf((v[c][e] - mean_p) * rstd_p, wp[c].get(e), bp[c].get(e));
+        v[c][e] = at.has(e) ? fmaf(a.beta * g[c].get(e), u, a.alpha * x[c].get(e)) : 0.f;
       }
-    } else {
-  #pragma unroll
-      for (int c = 0; c < CH; ++c)
-  #pragma unroll
-        for (int e = 0; e < 4; ++e) v[c][e] = a.alpha * xr[c].get(e);
-    }
-    if (a.r)
-  #pragma unroll
-      for (int c = 0; c < CH; ++c) store_unit((TR*)a.r + off, (c * LPR + lane) * kVec, d, v[c]);
+    });
+    const Window wr = window<TR>(a.r, row * d), wh = window<TB>(a.h, row * d);
+    for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) { at.template store<TR, true>(wr, v[c]); });
     moments(a.pre, mean, rstd);
-    if (a.h) {
-  #pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        const int at = (c * LPR + lane) * kVec;
-        float w[4], b[4], o[4];
-        load_param((const TB*)a.w, at, d, 1.f, w);
-        load_param((const TB*)a.b, at, d, 0.f, b);
-  #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = fmaf((v[c][e] - mean) * rstd, w[e], b[e]);
-        store_unit((TB*)a.h + off, at, d, o);
-      }
-    }
-    if (a.stats && lane == 0) *reinterpret_cast<float4*>(a.stats + 4 * row) = make_float4(mean_p, rstd_p, mean, rstd);
+    for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) {
+      float o[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf((v[c][e] - mean) * rstd, w[c].get(e), b[c].get(e));
+      if (a.past) at.template store<TB, true>(wh, o);
+      else at.template store<TB>(wh, o);
+    });
+    if (a.stats && active && threadIdx.x % LPR == 0)
+      *reinterpret_cast<float4*>(a.stats + 4 * (row + sub)) = make_float4(mean_p, rstd_p, mean, rstd);
   }
 }
 
 // Rows of one segment (the tokens of a gate row) in `pieces` ranges, one workgroup each; its groups walk the range in
 // turn and keep their column sums in registers, the next row on its way while this one is worked on.
-template <typename TR, typename TB, int LPR, int CH>
+template <typename TR, typename TB, int LPR, int CH, End kEnd>
 __global__ __launch_bounds__(threads_of<LPR>()) void block_norm_bwd_kernel(NormArgs a) {
   constexpr int T = threads_of<LPR>(), G = T / LPR;
   __shared__ float red[LPR > 64 ? 2 * LPR / 64 : 1][2];
-  __shared__ float sums[G > 1 ? G : 1][G > 1 ? LPR * CH * 4 : 1];
+  __shared__ float sums[G > 1 ? 4 : 1][G > 1 ? G : 1][G > 1 ? LPR * CH * 4 : 1];
   int n;
   if (!vd_count(a.n_dev, a.n, n, a.status)) return;
   const int segment = blockIdx.x / a.pieces, piece = blockIdx.x - segment * a.pieces, d = a.d;
@@ -252,73 +296,79 @@ __global__ __launch_bounds__(threads_of<LPR>()) void block_norm_bwd_kernel(NormA
   const long long chunk = (seg_rows + a.pieces - 1) / a.pieces;
   const long long first = segment * seg_rows;
   const long long r0 = first + min(seg_rows, piece * chunk), r1 = first + min(seg_rows, (piece + 1) * chunk);
-  const int group = threadIdx.x / LPR, lane = threadIdx.x % LPR;
+  const int sub = sub_group<LPR>();
   const float inv_d = 1.f / (float)d;
-  const bool branch = a.df != nullptr || a.f != nullptr;
-  const float pre_mean = a.pre == VARDROP_NORM_LAYER ? inv_d : 0.f, post_mean = a.post == VARDROP_NORM_LAYER ? inv_d : 0.f;
+  const float pre_mean = a.pre == VARDROP_NORM_LAYER ? inv_d : 0.f;
+  const float post_mean = a.post == VARDROP_NORM_LAYER ? inv_d : 0.f, post_hat = a.post == VARDROP_NORM_NONE ? 0.f : inv_d;
   int turn = 0;
-
-  float w[CH][4], gq[CH][4];               // weight of pre; beta g wp
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    const int at = (c * LPR + lane) * kVec;
-    load_param((const TB*)a.w, at, d, 1.f, w[c]);
-    float wp[4], g[4];
-    load_param((const TB*)a.wp, at, d, 1.f, wp);
-    load_param(a.gate ? (const TB*)a.gate + (long long)segment * d : nullptr, at, d, 1.f, g);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) gq[c][e] = a.beta * g[e] * wp[e];
-  }
-  float t0[CH][4] = {}, t1[CH][4] = {}, s0[CH][4] = {}, s1[CH][4] = {};
 
   Unit<TR> dr[CH], r[CH];
   Unit<TB> dh[CH], f[CH];
-  float4 st = make_float4(0.f, 1.f, 0.f, 1.f);
+  raw4 st;
   auto fetch = [&](long long row) {
-    const long long off = row * d;
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int at = (c * LPR + lane) * kVec;
-      if (a.dr) dr[c] = load_unit((const TR*)a.dr + off, at, d);
-      if (a.dh) {
-        dh[c] = load_unit((const TB*)a.dh + off, at, d);
-        r[c] = load_unit((const TR*)a.r_in + off, at, d);
-      }
-      if (a.f) f[c] = load_unit((const TB*)a.f + off, at, d);
-    }
-    if (a.stats) st = *reinterpret_cast<const float4*>(a.stats + 4 * row);
+    const bool active = LPR >= 64 || row + sub < r1;
+    const Window wdr = window<TR>(a.dr, row * d), wr = window<TR>(a.r_in, row * d), wdh = window<TB>(a.dh, row * d),
+                 wf = window<TB>(a.f, row * d), ws = window<float>(a.stats, row * 4);
+    st = __builtin_amdgcn_raw_buffer_load_b128(ws, active ? 16 * sub : kOutside, 0, 0);
+    for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) {
+      at.load(dr[c], wdr);
+      at.load(dh[c], wdh);
+      at.load(r[c], wr);
+      at.load(f[c], wf);
+    });
   };
+  float w[CH][4], gq[CH][4];               // weight of pre; beta g wp
+  long long row = r0 + first_group<LPR>();
+  {
+    const Window ww = window<TB>(a.w, 0), wwp = window<TB>(a.wp, 0), wg = window<TB>(a.gate, a.gates > 1 ? (long long)segment * d : 0);
+    Unit<TB> uw[CH], up[CH], ug[CH];
+    for_chunks<LPR, CH, kEnd>(d, 0, true, [&](int c, auto at) {
+      at.load(uw[c], ww);
+      at.load(up[c], wwp);
+      at.load(ug[c], wg);
+    });
+    if (row < r1) fetch(row);
+    for_chunks<LPR, CH, kEnd>(d, 0, true, [&](int c, auto at) {
+      at.trim(uw[c]);
+      at.trim(up[c]);
+      at.trim(ug[c]);
+      if (!a.w) uw[c].fill(1.f);
+      if (!a.wp) up[c].fill(1.f);
+      if (!a.gate) ug[c].fill(1.f);
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    dr[c].zero();
-    r[c].zero();
-    dh[c].zero();
-    f[c].zero();
+      for (int e = 0; e < 4; ++e) {
+        w[c][e] = uw[c].get(e);
+        gq[c][e] = at.has(e) ? a.beta * ug[c].get(e) * up[c].get(e) : 0.f;
+      }
+    });
   }
-  long long row = r0 + group;
-  // (rows of several wavefronts: one group, so that all threads meet at the barriers)
-  if (row < r1) fetch(row);
+  float t0[CH][4] = {}, t1[CH][4] = {}, s0[CH][4] = {}, s1[CH][4] = {};
   for (; row < r1; row += G) {
-    const long long off = row * d;
-    const float mean_p = st.x, rstd_p = st.y, mean = st.z, rstd = st.w;
+    const bool active = LPR >= 64 || row + sub < r1;
+    const bool there = a.stats != nullptr;
+    const float mean_p = __uint_as_float(st[0]), rstd_p = there ? __uint_as_float(st[1]) : 1.f, mean = __uint_as_float(st[2]),
+                rstd = __uint_as_float(st[3]);
     float D[CH][4], fh[CH][4];
     {
       float hat[CH][4], t[CH][4], s[2] = {0.f, 0.f};
+      for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) {
+        at.trim(dr[c]);
+        at.trim(dh[c]);
+        at.trim(r[c]);
+        at.trim(f[c]);
 #pragma unroll
-      for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const bool in = (c * LPR + lane) * kVec + e < d;      // (past the end all of these are zero)
+        for (int e = 0; e < 4; ++e) {            // (past the end all of these are zero)
           const float g = dh[c].get(e);
           D[c][e] = dr[c].get(e);
-          fh[c][e] = in ? (f[c].get(e) - mean_p) * rstd_p : 0.f;
-          hat[c][e] = in ? (r[c].get(e) - mean) * rstd : 0.f;
+          fh[c][e] = at.has(e) ? (f[c].get(e) - mean_p) * rstd_p : 0.f;
+          hat[c][e] = at.has(e) ? (r[c].get(e) - mean) * rstd : 0.f;
           t[c][e] = w[c][e] * g;
           s[0] += t[c][e];
           s[1] = fmaf(t[c][e], hat[c][e], s[1]);
           t0[c][e] += g;
           t1[c][e] = fmaf(g, hat[c][e], t1[c][e]);
         }
+      });
       if (row + G < r1) fetch(row + G);
       if (a.dh) {
         row_sum<LPR>(s, red, turn);
@@ -329,76 +379,74 @@ __global__ __launch_bounds__(threads_of<LPR>()) void block_norm_bwd_kernel(NormA
           for (int e = 0; e < 4; ++e) D[c][e] = fmaf(rstd, t[c][e] - m0 - hat[c][e] * m1, D[c][e]);
       }
     }
-    if (a.dx)
+    const Window wdx = window<TR>(a.dx, row * d), wdf = window<TB>(a.df, row * d);
+    float q[2] = {0.f, 0.f};
+    for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) {
+      float o[4];
 #pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        float o[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = a.alpha * D[c][e];
-        store_unit((TR*)a.dx + off, (c * LPR + lane) * kVec, d, o);
+      for (int e = 0; e < 4; ++e) {
+        o[e] = a.alpha * D[c][e];
+        s0[c][e] += D[c][e];
+        s1[c][e] = fmaf(D[c][e], fh[c][e], s1[c][e]);
+        D[c][e] = at.has(e) ? D[c][e] * gq[c][e] : 0.f;
+        q[0] += D[c][e];
+        q[1] = fmaf(D[c][e], fh[c][e], q[1]);
       }
-    if (branch) {
-      float q[2] = {0.f, 0.f};
+      at.template store<TR, true>(wdx, o);
+    });
+    if (a.post != VARDROP_NORM_NONE) row_sum<LPR>(q, red, turn);
+    const float m0 = q[0] * post_mean, m1 = q[1] * post_hat;
+    for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) {
+      float o[4];
 #pragma unroll
-      for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s0[c][e] += D[c][e];
-          s1[c][e] = fmaf(D[c][e], fh[c][e], s1[c][e]);
-          D[c][e] = (c * LPR + lane) * kVec + e < d ? D[c][e] * gq[c][e] : 0.f;
-          q[0] += D[c][e];
-          q[1] = fmaf(D[c][e], fh[c][e], q[1]);
-        }
-      if (a.post != VARDROP_NORM_NONE) row_sum<LPR>(q, red, turn);
-      const float m0 = a.post == VARDROP_NORM_NONE ? 0.f : q[0] * post_mean, m1 = a.post == VARDROP_NORM_NONE ? 0.f : q[1] * inv_d;
-      if (a.df)
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-          float o[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] = rstd_p * (D[c][e] - m0 - fh[c][e] * m1);
-          store_unit((TB*)a.df + off, (c * LPR + lane) * kVec, d, o);
-        }
-    }
+      for (int e = 0; e < 4; ++e) o[e] = rstd_p * (D[c][e] - m0 - fh[c][e] * m1);
+      at.template store<TB>(wdf, o);
+    });
   }
+  if (!a.part) return;
   // column sums of the groups, in their order
   float* part = a.part + (long long)blockIdx.x * 4 * d;
-  auto flush = [&](float (&v)[CH][4], float* out) {
+  auto leave = [&](int which, float (&v)[CH][4]) {
     if (G == 1) {
+      const Window wp = window<float>(part, (long long)which * d);
+      for_chunks<LPR, CH, kEnd>(d, 0, true, [&](int c, auto at) { at.template store<float>(wp, v[c]); });
+    } else {
 #pragma unroll
-      for (int c = 0; c < CH; ++c) store_unit(out, (c * LPR + lane) * kVec, d, v[c]);
-      return;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sums[group][(c * LPR + lane) * kVec + e] = v[c][e];
-    __syncthreads();
-    for (int i = threadIdx.x; i < d; i += T) {
-      float s = 0.f;
-#pragma unroll
-      for (int g = 0; g < G; ++g) s += sums[g][i];
-      out[i] = s;
+      for (int c = 0; c < CH; ++c)
+        *reinterpret_cast<float4*>(&sums[which][threadIdx.x / LPR][(c * LPR + threadIdx.x % LPR) * kVec]) =
+            make_float4(v[c][0], v[c][1], v[c][2], v[c][3]);
     }
   };
-  if (!a.part) return;
-  flush(t0, part);
-  flush(t1, part + d);
-  flush(s0, part + 2 * d);
-  flush(s1, part + 3 * d);
+  leave(0, t0);
+  leave(1, t1);
+  leave(2, s0);
+  leave(3, s1);
+  if (G == 1) return;
+  __syncthreads();
+  for (int i = threadIdx.x; i < 4 * d; i += T) {
+    const int which = i / d, col = i - which * d;
+    float s = 0.f;
+#pragma unroll
+    for (int g = 0; g < G; ++g) s += sums[which][g][col];
+    part[i] = s;
+  }
 }
 
-// The vector gradients from the pieces' column sums.  A workgroup takes 64 columns; blockIdx.y 0: db, dw; 1: dbp, dwp (every
-// piece weighted with its gate row); 2 + g: gate row g.
+// The vector gradients from the pieces' column sums.  A workgroup takes 16 columns (64 bytes of a sum) and 64 pieces at a time, so
+// that it has all it reads under way after one or two rounds; blockIdx.y 0: db, dw; 1: dbp, dwp (every piece weighted with its
+// gate row); 2 + g: gate row g.
+constexpr int kVectorCols = 16;
+__device__ inline float to_float(float v) { return v; }
+__device__ inline float to_float(bf16_t v) { return bf2f(v); }
 template <typename TB>
 __global__ __launch_bounds__(1024) void block_norm_vectors_kernel(NormArgs a, float* dw, float* db, float* dwp, float* dbp,
                                                                   float* dgate, int segments) {
-  __shared__ float red[16][64][2];
+  constexpr int R = 1024 / kVectorCols, N = 6;     // pieces side by side; rounds in flight
+  __shared__ float red[2][R][kVectorCols + 1];
   int n;
   if (!vd_count(a.n_dev, a.n, n)) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, what = blockIdx.y, d = a.d;
-  const int col = blockIdx.x * 64 + lane, c = min(col, d - 1);
+  const int j = threadIdx.x % kVectorCols, k = threadIdx.x / kVectorCols, what = blockIdx.y, d = a.d;
+  const int col = blockIdx.x * kVectorCols + j, c = min(col, d - 1);
   int p0 = 0, p1 = segments * a.pieces;
   if (what >= 2 && a.gates > 1) {
     p0 = (what - 2) * a.pieces;
@@ -406,83 +454,85 @@ __global__ __launch_bounds__(1024) void block_norm_vectors_kernel(NormArgs a, fl
   }
   const bool weighted = what == 1 && a.gates > 1;
   const float* src = a.part + (what == 0 ? 0 : 2 * d) + c;
-  float s0 = 0.f, s1 = 0.f;
-  for (int p = p0 + wave; p < p1; p += 16 * 8) {
-    float v0[8], v1[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float* q = src + (long long)min(p + 16 * i, p1 - 1) * 4 * d;
-      v0[i] = q[0];
-      v1[i] = q[d];
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int at = p + 16 * i;
-      if (at >= p1) break;
-      float g = 1.f;
-      if (weighted) {
-        const TB* row = (const TB*)a.gate + (long long)(at / a.pieces) * d + c;
-        Unit<TB> u;
-        u.zero();
-        u.load1(row, 0);
-        g = u.get(0);
-      }
-      s0 = fmaf(g, v0[i], s0);
-      s1 = fmaf(g, v1[i], s1);
-    }
-  }
-  red[wave][lane][0] = s0;
-  red[wave][lane][1] = s1;
-  __syncthreads();
-  if (wave != 0 || col >= d) return;
-  s0 = s1 = 0.f;
-#pragma unroll
-  for (int w = 0; w < 16; ++w) {
-    s0 += red[w][lane][0];
-    s1 += red[w][lane][1];
-  }
-  auto param = [&](const void* p, float none) {
-    if (!p) return none;
-    Unit<TB> u;
-    u.zero();
-    u.load1((const TB*)p + col, 0);
-    return u.get(0);
+  auto param = [&](const void* p, long long at, float none) {
+    return p ? to_float(((const TB*)p)[at]) : none;
   };
+  float s0 = 0.f, s1 = 0.f;
+  for (int p = p0 + k; p < p1; p += N * R) {
+    float v0[N], v1[N], g[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = min(p + i * R, p1 - 1);
+      v0[i] = src[(long long)at * 4 * d];
+      v1[i] = src[(long long)at * 4 * d + d];
+      g[i] = weighted ? param(a.gate, (long long)(at / a.pieces) * d + c, 1.f) : 1.f;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float t = p + i * R < p1 ? g[i] : 0.f;
+      s0 = p + i * R < p1 ? fmaf(t, v0[i], s0) : s0;
+      s1 = p + i * R < p1 ? fmaf(t, v1[i], s1) : s1;
+    }
+  }
+  // 64 sums of a column: sixteen threads take four each, then one adds those
+  red[0][k][j] = s0;
+  red[1][k][j] = s1;
+  __syncthreads();
+  if (k < 16) {
+#pragma unroll
+    for (int i = 1; i < R / 16; ++i) {
+      s0 += red[0][k + 16 * i][j];
+      s1 += red[1][k + 16 * i][j];
+    }
+    red[0][k][j] = s0;
+    red[1][k][j] = s1;
+  }
+  __syncthreads();
+  if (k != 0 || col >= d) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) {
+    s0 += red[0][i][j];
+    s1 += red[1][i][j];
+  }
   if (what == 0) {
     if (db) db[col] = s0;
     if (dw) dw[col] = s1;
   } else if (what == 1) {
-    const float k = a.beta * (a.gates == 1 ? param(a.gate, 1.f) : 1.f);
-    if (dbp) dbp[col] = k * s0;
-    if (dwp) dwp[col] = k * s1;
+    const float f = a.beta * (a.gates == 1 ? param(a.gate, col, 1.f) : 1.f);
+    if (dbp) dbp[col] = f * s0;
+    if (dwp) dwp[col] = f * s1;
   } else {
-    dgate[(long long)(what - 2) * d + col] = a.beta * fmaf(param(a.wp, 1.f), s1, param(a.bp, 0.f) * s0);
+    dgate[(long long)(what - 2) * d + col] = a.beta * fmaf(param(a.wp, col, 1.f), s1, param(a.bp, col, 0.f) * s0);
   }
 }
 
 // ---------------------------------------------------------------- host side
 struct Shape {
   int lanes, chunks;
+  End end;
 };
 // Lanes and chunks of a row of d elements: as many lanes as hold it with one chunk each, up to a wavefront; then up to four chunks;
-// then several wavefronts.
+// then several wavefronts.  All chunks but the last are whole.
 Shape shape_of(int d) {
-  if (d <= 64) return {16, 1};
-  if (d <= 128) return {32, 1};
-  if (d <= 1024) return {64, vd_ceil_div(d, 256)};
-  if (d <= 4096) return {256, d <= 2048 ? 2 : 4};
-  return {512, 4};
+  const int lanes = d <= 64 ? 16 : d <= 128 ? 32 : d <= 1024 ? 64 : d <= 4096 ? 256 : 512;
+  const int chunks = vd_ceil_div(d, lanes * kVec);
+  return {lanes, chunks, d < kVec ? kTiny : d % kVec ? kRagged : d == lanes * kVec * chunks ? kWhole : kCut};
 }
-#define VD_NORM_SHAPES(X) X(16, 1) X(32, 1) X(64, 1) X(64, 2) X(64, 3) X(64, 4) X(256, 2) X(256, 4) X(512, 4)
+#define VD_NORM_SHAPES(X) \
+  X(16, 1) X(32, 1) X(64, 1) X(64, 2) X(64, 3) X(64, 4) X(256, 2) X(256, 3) X(256, 4) X(512, 3) X(512, 4)
 
-// Workgroups per segment of the backward.
+// Ranges of rows per segment: two workgroups a compute unit, one for wide rows, whose column sums (32 d bytes a range, written and read
+// again) weigh more; at least eight rows, two for every group of lanes.  Backward with 256 / 512 / 1024 ranges in all, us: 390 625 x 64 bf16 84 / 64 / 68,
+// 97 656 x 256 82 / 64 / 69, 48 828 x 512 64.4 / 65.5 / 67.4, 32 552 x 768 66.8 / 66.4 / 67.0, 24 414 x 1024 67.4 / 67.9 / 68.6, fp32 129 / 127 / 128;
+// 12 207 x 2048 67.5 / 72.1 / 81.9, 6103 x 4096 71.8 / 81.7 / 89.9; 2784 x 512 with 174, 348, 696 ranges 15.8 / 14.8 / 17.0 (an earlier kernel).
 int pieces_of(int B, int n, int d, int gates) {
   const int segments = gates > 1 ? gates : 1;
   const Shape s = shape_of(d);
   const int groups = (s.lanes > 256 ? s.lanes : 256) / s.lanes;
   const long long rows = gates > 1 ? n : (long long)B * n;
-  long long p = vd_ceil_div(768, segments);
-  const long long most = (rows + groups - 1) / groups;
+  const int least = 2 * groups > 8 ? 2 * groups : 8;
+  const long long most = (rows + least - 1) / least;
+  long long p = vd_ceil_div(d > 1024 ? 256 : 512, segments);
   if (p > most) p = most;
   return p < 1 ? 1 : (int)p;
 }
@@ -497,14 +547,17 @@ template <bool kBackward, typename TR, typename TB>
 int launch(vardrop_ctx* ctx, const NormArgs& a, long long groups_of_rows, hipStream_t s) {
   const Shape sh = shape_of(a.d);
   VdTimer timer(ctx, kBackward ? VARDROP_K_BLOCK_NORM_BWD : VARDROP_K_BLOCK_NORM_FWD, s);
-#define VD_CASE(L, C)                                                                                              \
-  if (sh.lanes == L && sh.chunks == C) {                                                                           \
+#define VD_CASE_END(L, C, F)                                                                                       \
+  if (sh.lanes == L && sh.chunks == C && sh.end == F) {                                                            \
     constexpr int T = threads_of<L>();                                                                             \
-    if (kBackward) VD_KERNEL(ctx, (block_norm_bwd_kernel<TR, TB, L, C>), dim3((unsigned)groups_of_rows), dim3(T), 0, s, a); \
-    else VD_KERNEL(ctx, (block_norm_fwd_kernel<TR, TB, L, C>), dim3(blocks_of(groups_of_rows, T / L)), dim3(T), 0, s, a); \
+    if (kBackward) VD_KERNEL(ctx, (block_norm_bwd_kernel<TR, TB, L, C, F>), dim3((unsigned)groups_of_rows), dim3(T), 0, s, a); \
+    else VD_KERNEL(ctx, (block_norm_fwd_kernel<TR, TB, L, C, F>), dim3(blocks_of(groups_of_rows, T / L)), dim3(T), 0, s, a); \
   }
+#define VD_CASE(L, C) VD_CASE_END(L, C, kWhole) VD_CASE_END(L, C, kCut) VD_CASE_END(L, C, kRagged)
   VD_NORM_SHAPES(VD_CASE)
+  VD_CASE_END(16, 1, kTiny)
 #undef VD_CASE
+#undef VD_CASE_END
   VD_LAUNCH_CHECK(ctx);
   return VARDROP_OK;
 }
@@ -515,6 +568,14 @@ int launch_types(vardrop_ctx* ctx, const NormArgs& a, int res_dtype, int dtype, 
   if (res_dtype == VARDROP_F32) return launch<kBackward, float, bf16_t>(ctx, a, count, s);
   return launch<kBackward, bf16_t, bf16_t>(ctx, a, count, s);
 }
+
+// What is read again only after the block between (r, dx) is written past the caches: as dirty lines of the L2s it is written back
+// at the kernel's end, when nothing else runs.  h and df are what the next kernel reads; h goes past from this size on.  us, all
+// kept -> r and dx past -> all past: forward of 27 584 x 512 (fp32 residual, 28 MB of h) 35.0 -> 33.6 -> 30.7, backward of 2002 x 2048 fp32 27.3 -> 24.5
+// -> 22.8, of 65 536 x 768 131.3 -> 130.1 -> 129.6; norm, attention and back, 32 x 862 tokens of 512 545 each, 8 x 2000 of 768 778 -> 778 -> 780, 32 x 87
+// of 512 66.3 -> 65.6 -> 65.6, but 32 x 321 of 512 (10.5 MB) 193 -> 194 -> 198.
+constexpr long long kPastCaches = 16 << 20;
+bool is_past(int B, int n, int d, int dtype) { return (long long)B * n * d * (dtype == VARDROP_F32 ? 4 : 2) >= kPastCaches; }
 
 bool is_kind(int k) { return k == VARDROP_NORM_NONE || k == VARDROP_NORM_LAYER || k == VARDROP_NORM_RMS; }
 bool is_finite(float v) { return v - v == 0.f; }
@@ -552,6 +613,7 @@ int forward(vardrop_ctx* ctx, const void* x, const void* f, int B, int n, int d,
   NormArgs a = {};
   a.x = x; a.f = f; a.w = w; a.b = b; a.wp = wp; a.bp = bp; a.gate = gate; a.r = r; a.h = h; a.stats = stats;
   a.B = B; a.n = n; a.d = d; a.gates = gates; a.pre = pre; a.post = post;
+  a.past = is_past(B, n, d, dtype);
   a.alpha = alpha; a.beta = beta; a.eps = eps;
   a.n_dev = dn.dev; a.status = dn.status;
   return launch_types<false>(ctx, a, res_dtype, dtype, (long long)B * n, (hipStream_t)stream);
@@ -590,7 +652,7 @@ int backward(vardrop_ctx* ctx, const void* dr, const void* dh, const void* r, co
   hipStream_t s = (hipStream_t)stream;
   const int rb = launch_types<true>(ctx, a, res_dtype, dtype, (long long)segments * a.pieces, s);
   if (rb || !vectors) return rb;
-  const dim3 grid((unsigned)vd_ceil_div(d, 64), (unsigned)(dgate ? 2 + gates : (dwp || dbp) ? 2 : 1));
+  const dim3 grid((unsigned)vd_ceil_div(d, kVectorCols), (unsigned)(dgate ? 2 + gates : (dwp || dbp) ? 2 : 1));
   VdTimer timer(ctx, VARDROP_K_BLOCK_NORM_VECTORS, s);
   if (dtype == VARDROP_F32) VD_KERNEL(ctx, block_norm_vectors_kernel<float>, grid, dim3(1024), 0, s, a, dw, db, dwp, dbp, dgate, segments);
   else VD_KERNEL(ctx, block_norm_vectors_kernel<bf16_t>, grid, dim3(1024), 0, s, a, dw, db, dwp, dbp, dgate, segments);
