@@ -697,8 +697,11 @@ class TensorList:
         grads = list(grads)
         count = len(grads)
         numel = [t.numel() for t in grads]
+        device = ctx.device.index or 0
+        room = max(count, 1)
 
-        def pointers(what, tensors, dtypes, may_miss=False):
+        def addresses(what, tensors, dtypes, may_miss=False):
+            """The list of tensors and a C array of their addresses."""
             if tensors is None:
                 return None, None
             tensors = list(tensors)
@@ -707,26 +710,29 @@ class TensorList:
             for t, k in zip(tensors, numel):
                 if t is None and may_miss:
                     continue
-                if t is None or t.dtype not in dtypes or t.numel() != k or not t.is_contiguous() or t.device != ctx.device:
+                if t is None or t.numel() != k or t.dtype not in dtypes or not t.is_contiguous() or t.get_device() != device:
                     raise TypeError("%s: contiguous tensors of the gradients' sizes on %s wanted, in %s"
                                     % (what, ctx.device, " or ".join(str(d) for d in dtypes)))
-            return tensors, (ctypes.c_void_p * max(count, 1))(*[None if t is None else t.data_ptr() for t in tensors])
+            return tensors, (ctypes.c_void_p * room)(*[None if t is None else t.data_ptr() for t in tensors])
 
         both, fp32 = (torch.float32, torch.bfloat16), (torch.float32,)
 
         def codes(tensors):
-            return None if tensors is None else (ctypes.c_int32 * max(count, 1))(*[_dtype_code(t) for t in tensors])
+            """C array of the element types; None where all are float32, which the library takes for that."""
+            if tensors is None or all(t.dtype is torch.float32 for t in tensors):
+                return None
+            return (ctypes.c_int32 * room)(*[_CODES[t.dtype] for t in tensors])
 
-        grads, g = pointers("grads", grads, both)
-        clipped, c = pointers("clipped", clipped, both)
-        params, p = pointers("params", params, fp32)
-        exp_avg, m = pointers("exp_avg", exp_avg, fp32)
-        exp_avg_sq, v = pointers("exp_avg_sq", exp_avg_sq, fp32)
-        weights, w = pointers("weights", weights, (torch.bfloat16,), may_miss=True)
+        grads, g = addresses("grads", grads, both)
+        clipped, c = addresses("clipped", clipped, both)
+        params, p = addresses("params", params, fp32)
+        exp_avg, m = addresses("exp_avg", exp_avg, fp32)
+        exp_avg_sq, v = addresses("exp_avg_sq", exp_avg_sq, fp32)
+        weights, w = addresses("weights", weights, (torch.bfloat16,), may_miss=True)
         if decay is not None and len(decay) != count:
             raise TypeError("decay: %d values for %d gradients" % (len(decay), count))
-        rates = None if decay is None else (ctypes.c_float * max(count, 1))(*decay)
-        sizes = (ctypes.c_int64 * max(count, 1))(*numel)
+        rates = None if decay is None else (ctypes.c_float * room)(*decay)
+        sizes = (ctypes.c_int64 * room)(*numel)
         self.tensors = (grads, clipped, params, exp_avg, exp_avg_sq, weights)
         nbytes = ctx._lib.vardrop_tensor_list_bytes(count, sizes)
         if nbytes == 0:

@@ -16,7 +16,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxParts = 2048;              // workgroups of the norm, one partial sum each
-constexpr int kTicket = 32;                  // workgroups that share a counter
 constexpr int kRecords = 48;                 // tensors per launch of the layout kernel (its arguments hold them)
 constexpr uint32_t kBuilt = 0x56445431u;
 
@@ -38,16 +37,17 @@ struct Chunk {
 static_assert(sizeof(Chunk) == 64, "");
 enum { kGradBf16 = 1, kClipBf16 = 2 };
 
-// Counters of finished workgroups, zero between launches.  Increments of one address follow each other at about 12 ns, so kTicket
-// workgroups share a counter and the last of them counts for all at the top (a line of memory each).
+// Counters of finished workgroups, zero between launches.  Increments of one address follow each other at about 12 ns, so
+// workgroups share a counter in groups and the last of a group counts for all at the top (a line of memory each).
+constexpr int kGroups = 64, kGroupLeast = 32;
 struct Tickets {
-  uint32_t group[kMaxParts / kTicket][32];
+  uint32_t group[kGroups][32];
   uint32_t top[32];
 };
 // Head of the table; the chunks follow.
 struct Head {
   Tickets norm, step;
-  double part[kMaxParts];
+  uint64_t part[kMaxParts];          // of doubles
 };
 
 struct Record {
@@ -144,13 +144,14 @@ __device__ inline double block_sum(double v, double* red) {
   return v;
 }
 
-// True in the one workgroup of the grid (at most kMaxParts) that comes last.  By one thread, which has waited for what the
+// True in the one workgroup of the grid that comes last.  By one thread, which has waited for what the
 // others' reads and writes before this call have to be done with.
 __device__ inline bool comes_last(Tickets* t) {
   auto count = [](uint32_t* p) { return __hip_atomic_fetch_add(p, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
   auto reset = [](uint32_t* p) { __hip_atomic_store(p, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
-  const uint32_t group = blockIdx.x / kTicket, groups = (gridDim.x + kTicket - 1) / kTicket;
-  if (count(t->group[group]) != min((uint32_t)kTicket, gridDim.x - group * kTicket) - 1) return false;
+  const uint32_t size = max((uint32_t)kGroupLeast, (gridDim.x + kGroups - 1) / kGroups);
+  const uint32_t group = blockIdx.x / size, groups = (gridDim.x + size - 1) / size;
+  if (count(t->group[group]) != min(size, gridDim.x - group * size) - 1) return false;
   reset(t->group[group]);
   if (count(t->top) != groups - 1) return false;
   reset(t->top);
@@ -188,18 +189,18 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(Head* head, const C
   }
   const double mine = block_sum((s[0] + s[1]) + (s[2] + s[3]), red);
   if (threadIdx.x == 0) {
-    __hip_atomic_store(&head->part[blockIdx.x], mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    // The store and the later loads of the partial sums are atomic, so they bypass what this die caches; with the wait in
-    // between the sum is in memory before it is counted, and no cache has to be written back (a release by every workgroup
-    // made this kernel 58 us instead of 32 at 10.5 million gradients).
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // The sum is exchanged, not stored: when the old value is back the new one is where every die sees it, so it can be
+    // counted without a release, which would write this die's L2 back (10.5 million gradients: 58 us instead of 32).
+    const uint64_t old = __hip_atomic_exchange(&head->part[blockIdx.x], __builtin_bit_cast(uint64_t, mine), __ATOMIC_RELAXED,
+                                               __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("" ::"v"((uint32_t)old) : "memory");
     last = comes_last(&head->norm);
   }
   __syncthreads();
   if (!last) return;
   double t = 0.0;
   for (int i = threadIdx.x; i < (int)gridDim.x; i += kThreads)
-    t += __hip_atomic_load(&head->part[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    t += __builtin_bit_cast(double, __hip_atomic_load(&head->part[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
   t = block_sum(t, red);
   if (threadIdx.x == 0) *norm = (float)sqrt(t);
 }
@@ -353,7 +354,9 @@ int check_list(const vardrop_ctx* ctx, const vardrop_tensor_list* l) {
   return VARDROP_OK;
 }
 
-unsigned blocks_for(const vardrop_tensor_list* l, int most) { return (unsigned)(l->chunks < 1 ? 1 : l->chunks < most ? l->chunks : most); }
+// Workgroups of a launch: one for every chunk (57 million weights: 250 us, with 2048 workgroups that take several chunks each 263); of
+// the norm, as many as are resident together at most, each leaves a partial sum.
+unsigned blocks_for(const vardrop_tensor_list* l, int most = 1 << 20) { return (unsigned)(l->chunks < 1 ? 1 : l->chunks < most ? l->chunks : most); }
 
 int adamw(vardrop_ctx* ctx, const vardrop_tensor_list* l, Adam a, double beta1, double beta2, double eps, int64_t step, void* stream) {
   const int rc = check_list(ctx, l);
@@ -374,7 +377,7 @@ int adamw(vardrop_ctx* ctx, const vardrop_tensor_list* l, Adam a, double beta1, 
   }
   hipStream_t s = (hipStream_t)stream;
   VdTimer timer(ctx, VARDROP_K_ADAMW, s);
-  const dim3 grid(blocks_for(l, kMaxParts)), block(kThreads);
+  const dim3 grid(blocks_for(l)), block(kThreads);
   if (l->numel > kOnceAbove) VD_KERNEL(ctx, adamw_kernel<true>, grid, block, 0, s, head_of(l), chunks_of(l), l->chunks, a);
   else VD_KERNEL(ctx, adamw_kernel<false>, grid, block, 0, s, head_of(l), chunks_of(l), l->chunks, a);
   VD_LAUNCH_CHECK(ctx);
@@ -478,7 +481,7 @@ extern "C" int vardrop_clip_grads(vardrop_ctx* ctx, const vardrop_tensor_list* l
   if (list->chunks == 0) return VARDROP_OK;
   hipStream_t s = (hipStream_t)stream;
   VdTimer timer(ctx, VARDROP_K_CLIP, s);
-  VD_KERNEL(ctx, clip_kernel, dim3(blocks_for(list, kMaxParts)), dim3(kThreads), 0, s, chunks_of(list), list->chunks, norm,
+  VD_KERNEL(ctx, clip_kernel, dim3(blocks_for(list)), dim3(kThreads), 0, s, chunks_of(list), list->chunks, norm,
             max_norm, status);
   VD_LAUNCH_CHECK(ctx);
   return VARDROP_OK;
