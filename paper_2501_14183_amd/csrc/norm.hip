@@ -441,7 +441,7 @@ __device__ inline float to_float(bf16_t v) { return bf2f(v); }
 template <typename TB>
 __global__ __launch_bounds__(1024) void block_norm_vectors_kernel(NormArgs a, float* dw, float* db, float* dwp, float* dbp,
                                                                   float* dgate, int segments) {
-  constexpr int R = 1024 / kVectorCols, N = 6;     // pieces side by side; rounds in flight
+  constexpr int R = 1024 / kVectorCols, N = 8;     // pieces side by side; rounds in flight
   __shared__ float red[2][R][kVectorCols + 1];
   int n;
   if (!vd_count(a.n_dev, a.n, n)) return;

@@ -198,9 +198,16 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(Head* head, const C
   }
   __syncthreads();
   if (!last) return;
+  uint64_t part[kMaxParts / kThreads];               // all asked for before the first is added
+#pragma unroll
+  for (int k = 0; k < kMaxParts / kThreads; ++k) {
+    const int i = min(k * kThreads + (int)threadIdx.x, (int)gridDim.x - 1);
+    part[k] = __hip_atomic_load(&head->part[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
   double t = 0.0;
-  for (int i = threadIdx.x; i < (int)gridDim.x; i += kThreads)
-    t += __builtin_bit_cast(double, __hip_atomic_load(&head->part[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+#pragma unroll
+  for (int k = 0; k < kMaxParts / kThreads; ++k)
+    t += k * kThreads + (int)threadIdx.x < (int)gridDim.x ? __builtin_bit_cast(double, part[k]) : 0.0;
   t = block_sum(t, red);
   if (threadIdx.x == 0) *norm = (float)sqrt(t);
 }

@@ -299,6 +299,83 @@ def test_difference_of_the_kernels_own_forward(vd, ctx):
     assert abs((loss(step) - loss(-step)) / (2 * step) - slope) <= 4e-3 * size
 
 
+@pytest.mark.parametrize("res,dtype", TYPES)
+@pytest.mark.parametrize("B,n,d", [(1, 3, 2), (2, 5, 63), (2, 3, 64), (1, 9, 130), (2, 3, 321), (1, 5, 640), (1, 3, 1500), (1, 2, 4100), (1, 1, 8190)])
+def test_tensors_at_any_element_and_neighbours_untouched(vd, ctx, B, n, d, res, dtype):
+    """Every tensor a slice, at an odd element, of a buffer of sevens that is still there around the results afterwards."""
+    t = make(d, B, n, d, res, dtype, "layer", "rms", "window")
+    td, tr = torch_dtype(dtype), torch_dtype(res)
+    whole = []
+
+    def inside(shape, dt, values=None):
+        count = int(np.prod(shape))
+        flat = torch.full((count + 40,), 7.0, dtype=dt, device="cuda")
+        view = flat[19:19 + count].view(*shape)
+        whole.append((flat, count))
+        if values is not None:
+            view.copy_(to_dev(values, dt))
+        return view
+
+    dev = {k: None if a is None else inside(a.shape, tr if k in ("x", "dr") else td, a) for k, a in t.items()}
+    plain = {k: None if a is None else to_dev(a, tr if k in ("x", "dr") else td) for k, a in t.items()}
+    kw = dict(pre=vd.NORM_LAYER, post=vd.NORM_RMS, alpha=0.9, beta=-0.5)
+    stats = torch.empty(B * n, 4, device="cuda")
+    out = (inside((B, n, d), tr), inside((B, n, d), td), stats)
+    par = lambda v: {k: v[k] for k in ("w", "wp", "bp", "gate")}
+    vd.vardrop_block_norm_fwd(ctx, dev["x"], dev["f"], b=dev["b"], out=out, **par(dev), **kw)
+    want = vd.vardrop_block_norm_fwd(ctx, plain["x"], plain["f"], b=plain["b"], **par(plain), **kw)
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
+    f32 = torch.float32
+    grads = (inside((B, n, d), tr), inside((B, n, d), td)) + tuple(inside((d,), f32) for _ in range(4)) + (inside((B, d), f32),)
+    ws = torch.full((vd.vardrop_block_norm_workspace_bytes(B, n, d, B) + 256,), 9, dtype=torch.uint8, device="cuda")
+    vd.vardrop_block_norm_bwd(ctx, dev["dr"], dev["dh"], out[0], dev["f"], stats, ws=ws[:-256], out=grads, **par(dev), **kw)
+    want = vd.vardrop_block_norm_bwd(ctx, plain["dr"], plain["dh"], want[0], plain["f"], stats, bias_grads=True, **par(plain), **kw)
+    assert all(torch.equal(a, b) for a, b in zip(grads, want))
+    assert bool((ws[-256:] == 9).all())
+    for flat, count in whole:
+        assert bool((flat[:19] == 7.0).all()) and bool((flat[19 + count:] == 7.0).all())
+
+
+def test_recorded_step_follows_the_device_side_count(vd, ctx):
+    """Forward and backward in a graph: every replay, with another count and other data, gives what the calls give."""
+    B, n_max, d = 4, 50, 192
+    g = torch.Generator(device="cuda").manual_seed(1)
+    new = lambda *s: torch.randn(*s, device="cuda", generator=g)
+    x, f, dr, dh = (new(B, n_max, d).to(torch.bfloat16) for _ in range(4))
+    w, wp, gate = new(d).to(torch.bfloat16), new(d).to(torch.bfloat16), new(B, d).to(torch.bfloat16)
+    kw = dict(pre=vd.NORM_LAYER, post=vd.NORM_LAYER, w=w, wp=wp, gate=gate)
+    n_dev = torch.tensor([n_max], dtype=torch.int32, device="cuda")
+    ws = torch.empty(vd.vardrop_block_norm_workspace_bytes(B, n_max, d, B), dtype=torch.uint8, device="cuda")
+
+    def buffers():
+        return ((torch.zeros_like(x), torch.zeros_like(x), torch.zeros(B * n_max, 4, device="cuda")),
+                (torch.zeros_like(x), torch.zeros_like(x), torch.zeros(d, device="cuda"), None, torch.zeros(d, device="cuda"), None,
+                 torch.zeros(B, d, device="cuda")))
+
+    def step(out, grads):
+        vd.vardrop_block_norm_fwd(ctx, x, f, out=out, n_dev=n_dev, **kw)
+        vd.vardrop_block_norm_bwd(ctx, dr, dh, out[0], f, out[2], ws=ws, out=grads, n_dev=n_dev, **kw)
+
+    recorded, called = buffers(), buffers()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(*recorded)
+    for n in (50, 7, 0, 33, 50, 1):
+        n_dev.fill_(n)
+        for t in (x, f, dr, dh):
+            t.copy_(new(B, n_max, d))
+        for t in recorded[0] + recorded[1] + called[0] + called[1]:
+            if t is not None:
+                t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        step(*called)
+        torch.cuda.synchronize()
+        for a, b in zip(recorded[0] + recorded[1], called[0] + called[1]):
+            assert a is None or torch.equal(a, b), n
+
+
 def test_rows_beyond_32_bit_offsets(vd, ctx):
     """2^31 + 1024 elements: the last rows are those of a small batch."""
     d = 512
