@@ -406,6 +406,7 @@ int vardrop_attn_bwd_dev(vardrop_ctx* ctx, const void* dy, const void* xs,
  *                  not wanted), read by bwd (may be NULL there when neither norm is)
  * Backward, from the gradients dr and dh of r and h (dr NULL = zero; dh NULL exactly when pre is NONE):
  *   dx, df         NULL = not wanted; dx may be dr, df may be dh, and dx may be dh or df may be dr where the element types agree
+ *   w, wp, bp, gate as the forward had them (bp: for the gate's gradient)
  *   r, f           as the forward had them (r: needed with pre, x itself where f was NULL and alpha 1; f: needed with
  *                  post or a gate, NULL otherwise)
  *   dw, db, dwp, dbp   fp32 [d], dgate fp32 [gates][d]; overwritten, NULL = skip

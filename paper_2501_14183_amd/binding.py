@@ -141,9 +141,12 @@ def _stream(t, stream=None):
     """Raw hipStream_t: `stream` (an integer handle, e.g. torch.cuda.Stream.cuda_stream) or torch's current one."""
     if stream is not None:
         return stream
+    device = t.get_device()
+    if device < 0:
+        raise TypeError("the tensors must be on the GPU")
     if _current_raw_stream is not None:
-        return _current_raw_stream(t.get_device())
-    return torch.cuda.current_stream(t.device).cuda_stream
+        return _current_raw_stream(device)
+    return torch.cuda.current_stream(device).cuda_stream
 
 
 def _own_buffers(stream, what, **bufs):

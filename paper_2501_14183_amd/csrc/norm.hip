@@ -447,9 +447,10 @@ __global__ __launch_bounds__(1024) void block_norm_vectors_kernel(NormArgs a, fl
                                                                   float* dgate, int segments) {
   constexpr int R = 1024 / kVectorCols, N = 8;     // pieces side by side; rounds in flight
   __shared__ float red[2][R][kVectorCols + 1];
+  const int j = threadIdx.x % kVectorCols, k = threadIdx.x / kVectorCols, what = blockIdx.y, d = a.d;
+  if ((what == 0 && !dw && !db) || (what == 1 && !dwp && !dbp)) return;
   int n;
   if (!vd_count(a.n_dev, a.n, n)) return;
-  const int j = threadIdx.x % kVectorCols, k = threadIdx.x / kVectorCols, what = blockIdx.y, d = a.d;
   const int col = blockIdx.x * kVectorCols + j, c = min(col, d - 1);
   int p0 = 0, p1 = segments * a.pieces;
   if (what >= 2 && a.gates > 1) {
@@ -461,6 +462,9 @@ __global__ __launch_bounds__(1024) void block_norm_vectors_kernel(NormArgs a, fl
   auto param = [&](const void* p, long long at, float none) {
     return p ? to_float(((const TB*)p)[at]) : none;
   };
+  // what the results are multiplied with is asked for before the sums
+  const float gate = what == 1 && a.gates == 1 ? param(a.gate, c, 1.f) : 1.f;
+  const float wp = what >= 2 ? param(a.wp, c, 1.f) : 1.f, bp = what >= 2 ? param(a.bp, c, 0.f) : 0.f;
   float s0 = 0.f, s1 = 0.f;
   for (int p = p0 + k; p < p1; p += N * R) {
     float v0[N], v1[N], g[N];
@@ -502,11 +506,11 @@ __global__ __launch_bounds__(1024) void block_norm_vectors_kernel(NormArgs a, fl
     if (db) db[col] = s0;
     if (dw) dw[col] = s1;
   } else if (what == 1) {
-    const float f = a.beta * (a.gates == 1 ? param(a.gate, col, 1.f) : 1.f);
+    const float f = a.beta * gate;
     if (dbp) dbp[col] = f * s0;
     if (dwp) dwp[col] = f * s1;
   } else {
-    dgate[(long long)(what - 2) * d + col] = a.beta * fmaf(param(a.wp, col, 1.f), s1, param(a.bp, col, 0.f) * s0);
+    dgate[(long long)(what - 2) * d + col] = a.beta * fmaf(wp, s1, bp * s0);
   }
 }
 

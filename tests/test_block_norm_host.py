@@ -62,3 +62,16 @@ def test_kernel_ids_have_names(lib):
     names = [vd.vardrop_kernel_name(k) for k in range(64)]
     for name in ("block_norm_fwd", "block_norm_bwd", "block_norm_vectors", "grad_norm", "clip", "adamw"):
         assert names.count(name) == 1
+
+
+def test_tensors_that_are_not_on_the_gpu_are_refused(lib):
+    import torch
+
+    class Ctx:
+        _lib, handle = lib, None
+
+    x = torch.zeros(2, 3, 8)
+    with pytest.raises(TypeError):
+        vd.vardrop_block_norm_fwd(Ctx, x, x)
+    with pytest.raises(TypeError):
+        vd.vardrop_block_norm_bwd(Ctx, x, x, x, x, torch.zeros(6, 4))
