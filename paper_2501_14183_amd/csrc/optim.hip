@@ -14,13 +14,13 @@
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;                // of the norm and of clipping
+constexpr int kAdamThreads = 512;            // 57 million weights 242 us, with 256 threads of sixteen elements each 250; 1.1 million 10.4, 9.8
 constexpr int kMaxParts = 2048;              // workgroups of the norm, one partial sum each
 constexpr int kRecords = 48;                 // tensors per launch of the layout kernel (its arguments hold them)
 constexpr uint32_t kBuilt = 0x56445431u;
 
-constexpr int U = 4;                         // fours of a thread
-constexpr int kChunk = 4 * U * kThreads;     // elements of a chunk
+constexpr int kChunk = 4096;                 // elements of a chunk
 
 struct Chunk {
   void* grad;
@@ -116,12 +116,12 @@ template <typename T, bool kOnce = false> __device__ inline void store4(void* p,
 template <typename T> __device__ inline float load1(const void* p, int at) { return Four<T>::one(((gptr<const T>)(const T*)p)[at]); }
 template <typename T> __device__ inline void store1(void* p, int at, float v) { ((gptr<T>)(T*)p)[at] = Four<T>::round(v); }
 
-// A chunk of `count` elements: thread t of a workgroup has the fours at 4 (u kThreads + t), u < U, as far as they are whole
-// ones, and the first three threads one each of the elements behind the last whole four.
-struct Places {
+// A chunk of `count` elements among T threads: thread t has the fours at 4 (u T + t), u < kChunk / (4 T), as far as they are
+// whole ones, and the first three threads one each of the elements behind the last whole four.
+template <int T> struct Places {
   int count;
   __device__ explicit Places(int n) : count(n) {}
-  __device__ int at(int u) const { return (u * kThreads + threadIdx.x) * 4; }
+  __device__ int at(int u) const { return (u * T + threadIdx.x) * 4; }
   __device__ bool whole(int u) const { return at(u) + 4 <= count; }
   __device__ int rest() const { return (count & ~3) + threadIdx.x; }
   __device__ bool has_rest() const { return rest() < count; }
@@ -169,7 +169,8 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(Head* head, const C
   auto add = [&](float v, int e) { s[e] = fma((double)v, (double)v, s[e]); };
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const Chunk c = chunks[i];
-    const Places at(c.count);
+    const Places<kThreads> at(c.count);
+    constexpr int U = kChunk / (4 * kThreads);
     auto sum = [&](auto type) {
       typedef decltype(type) T;
       typename Four<T>::vec g[U];
@@ -235,7 +236,8 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(const Chunk* __restrict_
     const Chunk c = chunks[i];
     void* out = c.clip ? c.clip : c.grad;
     if (out == c.grad && s == 1.f) continue;          // in place and short enough: nothing changes
-    const Places at(c.count);
+    const Places<kThreads> at(c.count);
+    constexpr int U = kChunk / (4 * kThreads);
     auto scale = [&](auto from, auto to) {
       typedef decltype(from) T;
       typedef decltype(to) R;
@@ -272,11 +274,11 @@ struct Adam {
   int32_t* status;
 };
 
-// 57 million weights with fp32 gradients and bf16 copies 250 us (6.9 TB/s of 30 bytes each); 5 million with bf16 gradients 22 us (5.9 TB/s);
+// 57 million weights with fp32 gradients and bf16 copies 242 us (7.1 TB/s of 30 bytes each); 5 million with bf16 gradients 21.6 us (6.1 TB/s);
 // 1.1 million 10 us: one round of loads, arithmetic and stores, and the write-back of 16 MB at the kernel's end.  Chunks of 1024
 // elements for small lists: 10.0 us there, 15.1 instead of 11.3 for clipping.
 template <bool kOnce>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(Head* head, const Chunk* __restrict__ chunks, int n, Adam a) {
+__global__ __launch_bounds__(kAdamThreads) void adamw_kernel(Head* head, const Chunk* __restrict__ chunks, int n, Adam a) {
   float s = 1.f;
   int64_t t = 0;
   bool ready = false, sound = true;
@@ -294,7 +296,8 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(Head* head, const Chunk
   };
   for (int i = blockIdx.x; i < n && sound; i += gridDim.x) {
     const Chunk c = chunks[i];
-    const Places at(c.count);
+    const Places<kAdamThreads> at(c.count);
+    constexpr int U = kChunk / (4 * kAdamThreads);
     auto move = [&](float g, float& p, float& m, float& v) {
       const float x = s * g;
       m = fmaf(a.b1, m, a.c1 * x);
@@ -367,7 +370,7 @@ int check_list(const vardrop_ctx* ctx, const vardrop_tensor_list* l) {
   return VARDROP_OK;
 }
 
-// Workgroups of a launch: one for every chunk (57 million weights: 250 us, with 2048 workgroups that take several chunks each 263); of
+// Workgroups of a launch: one for every chunk (57 million weights, 256 threads: 250 us, with 2048 workgroups that take several chunks each 263); of
 // the norm, as many as are resident together at most, each leaves a partial sum.
 unsigned blocks_for(const vardrop_tensor_list* l, int most = 1 << 20) { return (unsigned)(l->chunks < 1 ? 1 : l->chunks < most ? l->chunks : most); }
 
@@ -390,7 +393,7 @@ int adamw(vardrop_ctx* ctx, const vardrop_tensor_list* l, Adam a, double beta1, 
   }
   hipStream_t s = (hipStream_t)stream;
   VdTimer timer(ctx, VARDROP_K_ADAMW, s);
-  const dim3 grid(blocks_for(l)), block(kThreads);
+  const dim3 grid(blocks_for(l)), block(kAdamThreads);
   if (l->numel > kOnceAbove) VD_KERNEL(ctx, adamw_kernel<true>, grid, block, 0, s, head_of(l), chunks_of(l), l->chunks, a);
   else VD_KERNEL(ctx, adamw_kernel<false>, grid, block, 0, s, head_of(l), chunks_of(l), l->chunks, a);
   VD_LAUNCH_CHECK(ctx);
