@@ -183,10 +183,10 @@ template <int LPR> __device__ inline int first_group() {
 }
 template <int LPR> __device__ inline int sub_group() { return LPR < 64 ? (int)(threadIdx.x % 64) / LPR : 0; }
 
-// One row per group of LPR lanes, the least that keeps 16 elements or fewer a lane: 27 584 rows of 512 with a fp32 residual, norms on both
-// sides and a gate for each window 30 us (5.7 TB/s), 2080 rows of 512 bf16 4.6 us (launch and one round of loads; with each vector of
-// weights asked for when it was needed the large one took 46).  Everything a row needs is asked for at once.  The statistics are taken from fp32 values before
-// r is rounded, deviations about the mean.
+// A row has LPR lanes, the least that keeps 16 elements or fewer a lane; a group of lanes takes one row or several, the next one on its way
+// while this one is worked on.  Everything a row needs is asked for at once.  27 584 rows of 512 with a fp32 residual, norms on both sides and a
+// gate for each window 27-28 us (6.1 TB/s; 46 with each vector asked for when it was needed), 2080 rows of 512 bf16 4.6 us (launch and one round
+// of loads).  The statistics are taken from fp32 values before r is rounded, deviations about the mean.
 template <typename TR, typename TB, int LPR, int CH, End kEnd>
 __global__ __launch_bounds__(threads_of<LPR>()) void block_norm_fwd_kernel(NormArgs a) {
   constexpr int T = threads_of<LPR>();
@@ -197,43 +197,60 @@ __global__ __launch_bounds__(threads_of<LPR>()) void block_norm_fwd_kernel(NormA
   const int d = a.d, sub = sub_group<LPR>();
   const float inv_d = 1.f / (float)d;
   int turn = 0;
-  for (long long row = (long long)blockIdx.x * (T / LPR) + first_group<LPR>(); row < rows; row += (long long)gridDim.x * (T / LPR)) {
-    const bool active = LPR >= 64 || row + sub < rows;
-    const Window wx = window<TR>(a.x, row * d), wf = window<TB>(a.f, row * d);
-    int gate = 0, sub_gate = 0;
-    if (a.gates > 1) {
-      gate = (int)((uint32_t)row / (uint32_t)n);
-      if (LPR < 64) sub_gate = (int)((uint32_t)(row + sub) / (uint32_t)n) - gate;
-    }
-    const Window wg = window<TB>(a.gate, (long long)gate * d), wwp = window<TB>(a.wp, 0), wbp = window<TB>(a.bp, 0),
-                 ww = window<TB>(a.w, 0), wb = window<TB>(a.b, 0);
-
-    Unit<TR> x[CH];
-    Unit<TB> f[CH], g[CH], wp[CH], bp[CH], w[CH], b[CH];
-    for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) {
-      at.load(x[c], wx);
-      at.load(f[c], wf);
-    });
-    for_chunks<LPR, CH, kEnd>(d, sub_gate, active, [&](int c, auto at) { at.load(g[c], wg); });
+  Unit<TB> wp[CH], bp[CH], w[CH], b[CH];
+  {
+    const Window wwp = window<TB>(a.wp, 0), wbp = window<TB>(a.bp, 0), ww = window<TB>(a.w, 0), wb = window<TB>(a.b, 0);
     for_chunks<LPR, CH, kEnd>(d, 0, true, [&](int c, auto at) {
       at.load(wp[c], wwp);
       at.load(bp[c], wbp);
       at.load(w[c], ww);
       at.load(b[c], wb);
     });
+  }
+  Unit<TR> x[CH];
+  Unit<TB> f[CH], g[CH];
+  auto fetch = [&](long long row) {
+    const bool active = LPR >= 64 || row + sub < rows;
+    const Window wx = window<TR>(a.x, row * d), wf = window<TB>(a.f, row * d);
+    for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) {
+      at.load(x[c], wx);
+      at.load(f[c], wf);
+    });
+    int gate = 0, sub_gate = 0;
+    if (a.gates > 1) {
+      gate = (int)((uint32_t)row / (uint32_t)n);
+      if (LPR < 64) sub_gate = (int)((uint32_t)(row + sub) / (uint32_t)n) - gate;
+    }
+    const Window wg = window<TB>(a.gate, (long long)gate * d);
+    for_chunks<LPR, CH, kEnd>(d, sub_gate, active, [&](int c, auto at) { at.load(g[c], wg); });
+  };
+  const long long stride = (long long)gridDim.x * (T / LPR);
+  long long row = (long long)blockIdx.x * (T / LPR) + first_group<LPR>();
+  if (row < rows) fetch(row);
+  for_chunks<LPR, CH, kEnd>(d, 0, true, [&](int c, auto at) {
+    at.trim(wp[c]);
+    at.trim(bp[c]);
+    at.trim(w[c]);
+    at.trim(b[c]);
+    if (!a.wp) wp[c].fill(1.f);
+    if (!a.w) w[c].fill(1.f);
+  });
+  for (; row < rows; row += stride) {
+    const bool active = LPR >= 64 || row + sub < rows;
+    float v[CH][4], res[CH][4], scale[CH][4];       // f; alpha x; beta g
     for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) {
       at.trim(x[c]);
       at.trim(f[c]);
       at.trim(g[c]);
-      at.trim(wp[c]);
-      at.trim(bp[c]);
-      at.trim(w[c]);
-      at.trim(b[c]);
       if (!a.gate) g[c].fill(1.f);
-      if (!a.wp) wp[c].fill(1.f);
-      if (!a.w) w[c].fill(1.f);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[c][e] = f[c].get(e);
+        res[c][e] = a.alpha * x[c].get(e);
+        scale[c][e] = a.beta * g[c].get(e);
+      }
     });
-    float v[CH][4];
+    if (row + stride < rows) fetch(row + stride);
     float mean_p = 0.f, rstd_p = 1.f, mean = 0.f, rstd = 1.f;
     auto moments = [&](int kind, float& m, float& k) {
       if (kind == VARDROP_NORM_NONE) return;
@@ -257,16 +274,12 @@ __global__ __launch_bounds__(threads_of<LPR>()) void block_norm_fwd_kernel(NormA
       row_sum<LPR>(q, red, turn);
       k = 1.f / sqrtf(q[0] * inv_d + a.eps);
     };
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[c][e] = f[c].get(e);
     moments(a.post, mean_p, rstd_p);
     for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float u = fmaf((v[c][e] - mean_p) * rstd_p, wp[c].get(e), bp[c].get(e));
-        v[c][e] = at.has(e) ? fmaf(a.beta * g[c].get(e), u, a.alpha * x[c].get(e)) : 0.f;
+        v[c][e] = at.has(e) ? fmaf(scale[c][e], u, res[c][e]) : 0.f;
       }
     });
     const Window wr = window<TR>(a.r, row * d), wh = window<TB>(a.h, row * d);
@@ -545,10 +558,12 @@ int pieces_of(int B, int n, int d, int gates) {
   return p < 1 ? 1 : (int)p;
 }
 
-// Workgroups of the forward: one turn for every row up to half a million of them (a launch holds fewer than 2^32 threads).
+// Workgroups of the forward: 4096 at most, all with the same number of turns but for the last ones; a wavefront with several rows asks for
+// the vectors once and has the next row on its way.  One row for every group of lanes -> up to 1024, 2048, 4096 workgroups, us: 390 625 x 64 bf16
+// 55.4 -> 43.5, 46.7, 41.3; 97 656 x 256 50.1 -> 45.3, 42.8, 40.9; 48 828 x 512 45.7 -> 39.7, 40.1, 38.3; 12 207 x 2048 45.9 -> 39.7, 41.1, 39.5.
 unsigned blocks_of(long long rows, int groups) {
-  const long long b = (rows + groups - 1) / groups;
-  return (unsigned)(b < (1 << 19) ? b : (1 << 19));
+  const long long b = (rows + groups - 1) / groups, turns = (b + 4095) / 4096;
+  return (unsigned)((b + turns - 1) / turns);
 }
 
 template <bool kBackward, typename TR, typename TB>

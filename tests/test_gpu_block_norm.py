@@ -168,6 +168,12 @@ def test_token_counts(vd, ctx, B, n, d, gate):
     run_case(vd, ctx, make(n, B, n, d, "bf16", "bf16", "rms", "layer", gate), "bf16", "bf16", "rms", "layer")
 
 
+@pytest.mark.parametrize("B,n,d,res,dtype", [(5, 14000, 16, "fp32", "bf16"), (3, 6001, 129, "bf16", "bf16"), (2, 2500, 1100, "fp32", "fp32")])
+def test_more_rows_than_groups_of_lanes(vd, ctx, B, n, d, res, dtype):
+    """Groups of lanes take several rows, of several windows."""
+    run_case(vd, ctx, make(n, B, n, d, res, dtype, "layer", "rms", "window"), res, dtype, "layer", "rms")
+
+
 def test_rows_that_do_not_vary_or_lie_far_from_zero(vd, ctx):
     """Constant rows (variance 0), zero rows, a level of 1000 deviations, and one huge channel."""
     t = make(3, 1, 5, 320, "fp32", "fp32", "layer", "layer", "shared")
