@@ -298,11 +298,13 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(Head* head, const C
     const Chunk c = chunks[i];
     const Places<kAdamThreads> at(c.count);
     constexpr int U = kChunk / (4 * kAdamThreads);
+    float shrink = 0.f;                // lr decay
     auto move = [&](float g, float& p, float& m, float& v) {
       const float x = s * g;
       m = fmaf(a.b1, m, a.c1 * x);
       v = fmaf(a.b2, v, a.c2 * x * x);
-      p = fmaf(-a.rate, m / fmaf(sqrtf(v), a.root, a.eps), (1.f - a.lr * c.decay) * p);
+      // (the decay as a difference: 1 - lr decay itself would lose the digits of lr decay that lie below 2^-24)
+      p = fmaf(-a.rate, m / fmaf(sqrtf(v), a.root, a.eps), fmaf(-shrink, p, p));
     };
     auto update = [&](auto type) {
       typedef decltype(type) T;
@@ -318,6 +320,7 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(Head* head, const C
         }
       if (!ready) prepare();
       if (!sound) return;
+      shrink = a.lr * c.decay;
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (at.whole(u)) {

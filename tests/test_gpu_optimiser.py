@@ -266,3 +266,17 @@ def test_refusals(vd, ctx):
     for args in (dict(params=g), dict(weights=[None]), dict(decay=[0.1]), dict(params=g, exp_avg=g, exp_avg_sq=g, decay=[float("nan")])):
         with pytest.raises(vd.VarDropError):
             vd.TensorList(ctx, g, **args)
+
+
+def test_weight_decay_below_the_last_digit_of_one(vd, ctx):
+    """A thousand steps without gradients: weights shrink by (1 - lr decay)^1000 with lr decay = 1e-6, whose rounding beside 1 would
+    be off by up to 3 %.  Every step rounds a weight once (2^-24, in either direction): 1000 of them stay below 1000 * 2^-24 = 6e-5 in
+    all and 2e-6 in the mean of 4096 weights with their roundings in quadrature; 1 % of the decay is 1e-5."""
+    p = torch.rand(4096, device="cuda") + 0.5
+    before = p.double()
+    g, m, v = (torch.zeros_like(p) for _ in range(3))
+    tensors = vd.TensorList(ctx, [g], params=[p], exp_avg=[m], exp_avg_sq=[v], decay=[0.01])
+    for step in range(1, 1001):
+        vd.vardrop_adamw(ctx, tensors, 1e-4, step)
+    shrunk = (p.double() / before).mean()
+    assert abs(float(shrunk) - (1 - 1e-6) ** 1000) <= 1e-5
