@@ -451,7 +451,7 @@ __global__ __launch_bounds__(threads_of<LPR>()) void block_norm_bwd_kernel(NormA
 // The vector gradients from the pieces' column sums.  A workgroup takes 16 columns (64 bytes of a sum) and 64 pieces at a time, so
 // that it has all it reads under way in one round (6.2 us for 512 pieces of 768 columns and eight gate rows, 18.6 with 64 columns a workgroup
 // and three rounds and more; 4.2 us is the least); blockIdx.y 0: db, dw; 1: dbp, dwp (every piece weighted with its
-// gate row); 2 + g: gate row g.
+// gate row) and the gradient of a single gate row; 2 + g: gate row g of several.
 constexpr int kVectorCols = 16;
 __device__ inline float to_float(float v) { return v; }
 __device__ inline float to_float(bf16_t v) { return bf2f(v); }
@@ -461,12 +461,13 @@ __global__ __launch_bounds__(1024) void block_norm_vectors_kernel(NormArgs a, fl
   constexpr int R = 1024 / kVectorCols, N = 8;     // pieces side by side; rounds in flight
   __shared__ float red[2][R][kVectorCols + 1];
   const int j = threadIdx.x % kVectorCols, k = threadIdx.x / kVectorCols, what = blockIdx.y, d = a.d;
-  if ((what == 0 && !dw && !db) || (what == 1 && !dwp && !dbp)) return;
+  const bool one_gate = what == 1 && a.gates == 1 && dgate;
+  if ((what == 0 && !dw && !db) || (what == 1 && !dwp && !dbp && !one_gate)) return;
   int n;
   if (!vd_count(a.n_dev, a.n, n)) return;
   const int col = blockIdx.x * kVectorCols + j, c = min(col, d - 1);
   int p0 = 0, p1 = segments * a.pieces;
-  if (what >= 2 && a.gates > 1) {
+  if (what >= 2) {
     p0 = (what - 2) * a.pieces;
     p1 = p0 + a.pieces;
   }
@@ -477,7 +478,7 @@ __global__ __launch_bounds__(1024) void block_norm_vectors_kernel(NormArgs a, fl
   };
   // what the results are multiplied with is asked for before the sums
   const float gate = what == 1 && a.gates == 1 ? param(a.gate, c, 1.f) : 1.f;
-  const float wp = what >= 2 ? param(a.wp, c, 1.f) : 1.f, bp = what >= 2 ? param(a.bp, c, 0.f) : 0.f;
+  const float wp = what >= 1 ? param(a.wp, c, 1.f) : 1.f, bp = what >= 1 ? param(a.bp, c, 0.f) : 0.f;
   float s0 = 0.f, s1 = 0.f;
   for (int p = p0 + k; p < p1; p += N * R) {
     float v0[N], v1[N], g[N];
@@ -522,9 +523,8 @@ __global__ __launch_bounds__(1024) void block_norm_vectors_kernel(NormArgs a, fl
     const float f = a.beta * gate;
     if (dbp) dbp[col] = f * s0;
     if (dwp) dwp[col] = f * s1;
-  } else {
-    dgate[(long long)(what - 2) * d + col] = a.beta * fmaf(wp, s1, bp * s0);
   }
+  if (what >= 2 || one_gate) dgate[(long long)(what >= 2 ? what - 2 : 0) * d + col] = a.beta * fmaf(wp, s1, bp * s0);
 }
 
 // ---------------------------------------------------------------- host side
@@ -675,7 +675,7 @@ int backward(vardrop_ctx* ctx, const void* dr, const void* dh, const void* r, co
   hipStream_t s = (hipStream_t)stream;
   const int rb = launch_types<true>(ctx, a, res_dtype, dtype, (long long)segments * a.pieces, s);
   if (rb || !vectors) return rb;
-  const dim3 grid((unsigned)vd_ceil_div(d, kVectorCols), (unsigned)(dgate ? 2 + gates : (dwp || dbp) ? 2 : 1));
+  const dim3 grid((unsigned)vd_ceil_div(d, kVectorCols), (unsigned)(dgate && gates > 1 ? 2 + gates : (dgate || dwp || dbp) ? 2 : 1));
   VdTimer timer(ctx, VARDROP_K_BLOCK_NORM_VECTORS, s);
   if (dtype == VARDROP_F32) VD_KERNEL(ctx, block_norm_vectors_kernel<float>, grid, dim3(1024), 0, s, a, dw, db, dwp, dbp, dgate, segments);
   else VD_KERNEL(ctx, block_norm_vectors_kernel<bf16_t>, grid, dim3(1024), 0, s, a, dw, db, dwp, dbp, dgate, segments);
