@@ -314,8 +314,6 @@ __global__ __launch_bounds__(threads_of<LPR>()) void block_norm_bwd_kernel(NormA
   const long long r0 = first + min(seg_rows, piece * chunk), r1 = first + min(seg_rows, (piece + 1) * chunk);
   const int sub = sub_group<LPR>();
   const float inv_d = 1.f / (float)d;
-  const float pre_mean = a.pre == VARDROP_NORM_LAYER ? inv_d : 0.f;
-  const float post_mean = a.post == VARDROP_NORM_LAYER ? inv_d : 0.f, post_hat = a.post == VARDROP_NORM_NONE ? 0.f : inv_d;
   int turn = 0;
 
   Unit<TR> dr[CH], r[CH];
@@ -388,7 +386,7 @@ __global__ __launch_bounds__(threads_of<LPR>()) void block_norm_bwd_kernel(NormA
       if (row + G < r1) fetch(row + G);
       if (a.dh) {
         row_sum<LPR>(s, red, turn);
-        const float m0 = s[0] * pre_mean, m1 = s[1] * inv_d;
+        const float m0 = a.pre == VARDROP_NORM_LAYER ? s[0] * inv_d : 0.f, m1 = s[1] * inv_d;
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -410,14 +408,16 @@ __global__ __launch_bounds__(threads_of<LPR>()) void block_norm_bwd_kernel(NormA
       }
       at.template store<TR, true>(wdx, o);
     });
-    if (a.post != VARDROP_NORM_NONE) row_sum<LPR>(q, red, turn);
-    const float m0 = q[0] * post_mean, m1 = q[1] * post_hat;
-    for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) {
-      float o[4];
+    // Without the norm, beta g D as it is: 0 in the place of a sum would make NaN of the elements beside one that is not finite.
+    if (a.post != VARDROP_NORM_NONE) {
+      row_sum<LPR>(q, red, turn);
+      const float m0 = a.post == VARDROP_NORM_LAYER ? q[0] * inv_d : 0.f, m1 = q[1] * inv_d;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = rstd_p * (D[c][e] - m0 - fh[c][e] * m1);
-      at.template store<TB>(wdf, o);
-    });
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) D[c][e] = rstd_p * (D[c][e] - m0 - fh[c][e] * m1);
+    }
+    for_chunks<LPR, CH, kEnd>(d, sub, active, [&](int c, auto at) { at.template store<TB>(wdf, D[c]); });
   }
   if (!a.part) return;
   // column sums of the groups, in their order

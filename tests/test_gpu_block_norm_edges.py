@@ -1,0 +1,65 @@
+"""Norms around a block where a value, an argument or a buffer is out of the ordinary: non-finite elements, branches that are not
+there, results that overwrite inputs.
+
+Bounds, u = 2^-24: with no norm on either side a gradient is three products (beta g, times wp = 1, times D): 4 u of its value,
+and 2^-8 more where it is rounded to bf16.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block_norm as o
+from test_gpu_block_norm import TYPES, U, make
+from util_gpu import to_dev, torch_dtype
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def vd():
+    import paper_2501_14183_amd as m
+    return m
+
+
+@pytest.fixture(scope="module")
+def ctx(vd):
+    return vd.Context(0)
+
+
+def on_device(t, res, dtype):
+    return {k: None if a is None else to_dev(a, torch_dtype(res if k in ("x", "dr") else dtype)) for k, a in t.items()}
+
+
+def same_but_for_rounding(got, want, what):
+    """Equal where the oracle is not finite, within three products' rounding where it is."""
+    bf16 = got.dtype == torch.bfloat16
+    got = got.double().cpu().numpy().reshape(want.shape)
+    sound = np.isfinite(want)
+    assert np.isfinite(got[sound]).all(), "%s: %d elements are not finite" % (what, (~np.isfinite(got[sound])).sum())
+    assert (np.abs(got[sound] - want[sound]) <= (4 * U + (2.0 ** -8 if bf16 else 0.0)) * np.abs(want[sound]) + 1e-37).all(), what
+    assert np.array_equal(got[~sound], want[~sound], equal_nan=True), what
+
+
+@pytest.mark.parametrize("gate", ["none", "shared", "window"])
+@pytest.mark.parametrize("d", [3, 40, 64, 321, 1100])
+@pytest.mark.parametrize("res,dtype", TYPES)
+def test_a_branch_gradient_does_not_depend_on_the_branch_without_a_post_norm(vd, ctx, res, dtype, d, gate):
+    """df = beta g D whatever f is: an infinite or missing value in f stays out of it."""
+    t = make(1, 2, 5, d, res, dtype, "none", "none", gate)
+    t["f"][0, 1, d // 2], t["f"][1, 2, 0], t["f"][1, 4, d - 1] = np.inf, np.nan, -np.inf
+    dev = on_device(t, res, dtype)
+    dx, df, *_ = vd.vardrop_block_norm_bwd(ctx, dev["dr"], None, dev["x"], dev["f"], None, pre=vd.NORM_NONE, gate=dev["gate"], alpha=0.75,
+                                           beta=-0.5)
+    g = o.gate_rows(t["gate"], 2, d)
+    same_but_for_rounding(dx, 0.75 * t["dr"], "dx")
+    same_but_for_rounding(df, -0.5 * g * t["dr"], "df")
+
+
+@pytest.mark.parametrize("d", [3, 40, 64, 321, 1100])
+def test_an_infinite_gradient_stays_in_its_element_without_norms(vd, ctx, d):
+    t = make(2, 2, 5, d, "fp32", "fp32", "none", "none", "none")
+    t["dr"][0, 1, d // 2], t["dr"][1, 2, 0] = np.inf, -np.inf
+    dev = on_device(t, "fp32", "fp32")
+    dx, df, *_ = vd.vardrop_block_norm_bwd(ctx, dev["dr"], None, dev["x"], dev["f"], None, pre=vd.NORM_NONE, alpha=0.75, beta=0.5)
+    same_but_for_rounding(dx, 0.75 * t["dr"], "dx")
+    same_but_for_rounding(df, 0.5 * t["dr"], "df")
