@@ -524,7 +524,8 @@ __global__ __launch_bounds__(1024) void block_norm_vectors_kernel(NormArgs a, fl
     if (dbp) dbp[col] = f * s0;
     if (dwp) dwp[col] = f * s1;
   }
-  if (what >= 2 || one_gate) dgate[(long long)(what >= 2 ? what - 2 : 0) * d + col] = a.beta * fmaf(wp, s1, bp * s0);
+  // (no product with a bias that is not there: 0 times an infinite S0 is NaN)
+  if (what >= 2 || one_gate) dgate[(long long)(what >= 2 ? what - 2 : 0) * d + col] = a.beta * (a.bp ? fmaf(wp, s1, bp * s0) : wp * s1);
 }
 
 // ---------------------------------------------------------------- host side

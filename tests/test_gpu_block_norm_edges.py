@@ -63,3 +63,21 @@ def test_an_infinite_gradient_stays_in_its_element_without_norms(vd, ctx, d):
     dx, df, *_ = vd.vardrop_block_norm_bwd(ctx, dev["dr"], None, dev["x"], dev["f"], None, pre=vd.NORM_NONE, alpha=0.75, beta=0.5)
     same_but_for_rounding(dx, 0.75 * t["dr"], "dx")
     same_but_for_rounding(df, 0.5 * t["dr"], "df")
+
+
+@pytest.mark.parametrize("gate", ["shared", "window"])
+@pytest.mark.parametrize("post", ["none", "rms"])
+def test_an_infinite_gradient_makes_an_infinite_gate_gradient_without_a_bias(vd, ctx, post, gate):
+    """dg = beta sum D wp hat(f): infinite in one channel where hat(f) is not zero.  A bias that was not given adds nothing to it."""
+    t = make(3, 2, 5, 72, "fp32", "fp32", "none", post, gate, bias=False)
+    t["dr"][1, 2, 7] = np.inf
+    dev = on_device(t, "fp32", "fp32")
+    kinds = {"none": vd.NORM_NONE, "rms": vd.NORM_RMS}
+    _, _, stats = vd.vardrop_block_norm_fwd(ctx, dev["x"], dev["f"], pre=vd.NORM_NONE, post=kinds[post], wp=dev["wp"], gate=dev["gate"])
+    *_, dgate = vd.vardrop_block_norm_bwd(ctx, dev["dr"], None, dev["x"], dev["f"], stats, pre=vd.NORM_NONE, post=kinds[post], wp=dev["wp"],
+                                          gate=dev["gate"], beta=0.5)
+    got = dgate.cpu().numpy().reshape(-1, 72)
+    sign = np.sign(t["f"][1, 2, 7] * (1.0 if t["wp"] is None else t["wp"][7]))
+    assert got[-1, 7] == sign * np.inf
+    got[-1, 7] = 0.0
+    assert np.isfinite(got).all()
