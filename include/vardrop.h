@@ -486,7 +486,8 @@ int vardrop_clip_grads(vardrop_ctx* ctx, const vardrop_tensor_list* list, const 
  * (norm NULL or max_norm 0: s = 1), so that clipped gradients are never written:
  *   m = beta1 m + (1 - beta1) s g,   v = beta2 v + (1 - beta2) (s g)^2
  *   param = param (1 - lr decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps),   weight = bf16(param)
- * step >= 1 counts this step; 0 <= beta1, beta2 < 1, eps > 0.  When `norm` is given and not finite the step is skipped: nothing
+ * step >= 1 counts this step; 0 <= beta1, beta2 < 1, eps > 0; eps and lr / (1 - beta1^step) are used in fp32 and have to be in its
+ * range (eps > 0 there too, EINVAL otherwise).  When `norm` is given and not finite the step is skipped: nothing
  * is written (nor is the step counted, below) and *status is set to 1.
  * vardrop_adamw_dev reads the rate from lr_dev (fp32 [1]) and the number of steps already done from step_dev (int64 [1],
  * 8-byte aligned), and with advance != 0 stores that number + 1 once the step is done, so that a recorded launch makes the next

@@ -381,18 +381,20 @@ int adamw(vardrop_ctx* ctx, const vardrop_tensor_list* l, Adam a, double beta1, 
   const int rc = check_list(ctx, l);
   if (rc) return rc;
   if (l->tensors > 0 && !(l->has & kHasParams)) return VARDROP_EINVAL;
-  if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps > 0.0) || !(eps - eps == 0.0)) return VARDROP_EINVAL;
+  if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return VARDROP_EINVAL;
   if (!(a.max_norm >= 0.f) || (a.max_norm > 0.f && !a.norm)) return VARDROP_EINVAL;
   a.b1 = (float)beta1;
   a.c1 = (float)(1.0 - beta1);
   a.b2 = (float)beta2;
   a.c2 = (float)(1.0 - beta2);
   a.eps = (float)eps;
+  if (!(a.eps > 0.f) || !(a.eps - a.eps == 0.f)) return VARDROP_EINVAL;      // (it is used in fp32: no 0 / 0 for a weight without moments)
   a.log_b1 = log(beta1);
   a.log_b2 = log(beta2);
   if (!a.step_dev) {
     a.rate = (float)((double)a.lr / -expm1((double)step * a.log_b1));
     a.root = (float)(1.0 / sqrt(-expm1((double)step * a.log_b2)));
+    if (!(a.rate - a.rate == 0.f)) return VARDROP_EINVAL;       // (a.lr is at most that)
   }
   hipStream_t s = (hipStream_t)stream;
   VdTimer timer(ctx, VARDROP_K_ADAMW, s);
