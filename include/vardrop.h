@@ -491,7 +491,8 @@ int vardrop_clip_grads(vardrop_ctx* ctx, const vardrop_tensor_list* list, const 
  * is written (nor is the step counted, below) and *status is set to 1.
  * vardrop_adamw_dev reads the rate from lr_dev (fp32 [1]) and the number of steps already done from step_dev (int64 [1],
  * 8-byte aligned), and with advance != 0 stores that number + 1 once the step is done, so that a recorded launch makes the next
- * step at every replay.  Calls that share a step_dev must be ordered by their streams. */
+ * step at every replay.  A rate or a counter that vardrop_adamw refuses (negative, not finite, out of range) skips the step like a
+ * norm that is not finite.  Calls that share a step_dev must be ordered by their streams. */
 int vardrop_adamw(vardrop_ctx* ctx, const vardrop_tensor_list* list, double lr, double beta1, double beta2, double eps,
                   int64_t step, const float* norm, float max_norm, int32_t* status, void* stream);
 int vardrop_adamw_dev(vardrop_ctx* ctx, const vardrop_tensor_list* list, const float* lr_dev, double beta1, double beta2,

@@ -286,13 +286,14 @@ __global__ __launch_bounds__(kAdamThreads) void adamw_kernel(Head* head, const C
   auto prepare = [&]() {
     ready = true;
     sound = clip_factor(a.norm, a.max_norm, s);
-    if (!sound && a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = 1;
-    if (a.step_dev) {                  // (the host has filled `rate` and `root` in otherwise)
+    if (a.step_dev) {                  // (the host has filled `rate` and `root` in otherwise, and refused what is not sound)
       t = *a.step_dev + 1;
       a.lr = *a.lr_dev;
       a.rate = (float)((double)a.lr / -expm1((double)t * a.log_b1));
       a.root = (float)(1.0 / sqrt(-expm1((double)t * a.log_b2)));
+      sound = sound && t >= 1 && a.lr >= 0.f && a.rate - a.rate == 0.f;
     }
+    if (!sound && a.status && blockIdx.x == 0 && threadIdx.x == 0) *a.status = 1;
   };
   for (int i = blockIdx.x; i < n && sound; i += gridDim.x) {
     const Chunk c = chunks[i];

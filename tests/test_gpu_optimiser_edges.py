@@ -48,3 +48,25 @@ def test_the_smallest_eps_is_taken(vd, ctx):
     kept = [t.clone() for t in state[1]]
     vd.vardrop_adamw(ctx, tensors, 0.1, 1, eps=1.5e-45)
     assert all(torch.equal(a, b) for a, b in zip(state[1], kept))
+
+
+@pytest.mark.parametrize("rate,step", [(float("nan"), 3), (float("inf"), 3), (-0.1, 3), (0.1, -1), (0.1, -5), (1e38, 0)])
+def test_a_device_rate_or_counter_out_of_range_skips_the_step(vd, ctx, rate, step):
+    """What the call with host scalars refuses, the one that reads them on the device cannot: it writes nothing and says so."""
+    tensors, state, kept = whole_list(vd, ctx, (5000, 7, 4096 * 40))
+    rate_dev, status = torch.full((1,), rate, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    step_dev = torch.full((1,), step, dtype=torch.int64, device="cuda")
+    vd.vardrop_adamw_dev(ctx, tensors, rate_dev, step_dev, status=status)
+    assert int(status) == 1 and int(step_dev) == step and unchanged(state, kept)
+    # the list and its counters work again
+    rate_dev.fill_(0.1)
+    step_dev.fill_(2)
+    status.zero_()
+    vd.vardrop_adamw_dev(ctx, tensors, rate_dev, step_dev, status=status)
+    assert int(status) == 0 and int(step_dev) == 3
+    again, state2, _ = whole_list(vd, ctx, (5000, 7, 4096 * 40))
+    for a, b in zip(state2, kept):
+        for x, y in zip(a, b):
+            x.copy_(y)
+    vd.vardrop_adamw(ctx, again, float(rate_dev), 3)
+    assert unchanged(state, state2)
