@@ -478,8 +478,9 @@ int vardrop_tensor_list_build(vardrop_ctx* ctx, int tensors, const int64_t* nume
  * exceeds fp32. */
 int vardrop_grad_norm(vardrop_ctx* ctx, const vardrop_tensor_list* list, float* norm, void* stream);
 /* Clipping to a global norm: out = g * min(1, max_norm / (norm + 1e-6)), rounded once to the type of `out` (the gradients
- * themselves for a list without clip tensors).  `norm` is read on the device, max_norm > 0.  When it is not finite nothing is written
- * and *status (device int32, optional, never cleared by the library) is set to 1. */
+ * themselves for a list without clip tensors).  `norm` is read on the device, max_norm > 0.  When it is not finite *status (device
+ * int32, optional, never cleared by the library) is set to 1; clip tensors get what the formula gives (0 or NaN for an infinite norm, NaN
+ * otherwise), so that they never hold an earlier step's gradients, and gradients that would be clipped in place stay as they are. */
 int vardrop_clip_grads(vardrop_ctx* ctx, const vardrop_tensor_list* list, const float* norm, float max_norm,
                        int32_t* status, void* stream);
 /* One AdamW step (decoupled weight decay) of every tensor of a list, in place, all in fp32; with s the clipping factor above

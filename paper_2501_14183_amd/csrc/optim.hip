@@ -228,14 +228,15 @@ __device__ inline bool clip_factor(const float* norm, float max_norm, float& s) 
 // 10.5 million fp32 gradients into others 11.4 us (7.4 TB/s, they are still in the memory-side cache); 1.1 million into bf16 3.3 us.
 __global__ __launch_bounds__(kThreads) void clip_kernel(const Chunk* __restrict__ chunks, int n, const float* norm, float max_norm, int32_t* status) {
   float s;
-  if (!clip_factor(norm, max_norm, s)) {
+  const bool sound = clip_factor(norm, max_norm, s);
+  if (!sound) {                                       // the formula without its minimum, which would take 1 for NaN
     if (status && blockIdx.x == 0 && threadIdx.x == 0) *status = 1;
-    return;
+    s = max_norm / *norm;
   }
   for (int i = blockIdx.x; i < n; i += gridDim.x) {
     const Chunk c = chunks[i];
     void* out = c.clip ? c.clip : c.grad;
-    if (out == c.grad && s == 1.f) continue;          // in place and short enough: nothing changes
+    if (out == c.grad && (s == 1.f || !sound)) continue;          // in place: nothing changes, or nothing may
     const Places<kThreads> at(c.count);
     constexpr int U = kChunk / (4 * kThreads);
     auto scale = [&](auto from, auto to) {

@@ -2,6 +2,8 @@
 import pytest
 import torch
 
+from test_gpu_optimiser import grads_of
+
 pytestmark = pytest.mark.gpu
 
 
@@ -70,3 +72,22 @@ def test_a_device_rate_or_counter_out_of_range_skips_the_step(vd, ctx, rate, ste
             x.copy_(y)
     vd.vardrop_adamw(ctx, again, float(rate_dev), 3)
     assert unchanged(state, state2)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("to", [torch.float32, torch.bfloat16])
+def test_clipped_gradients_are_never_those_of_an_earlier_step(vd, ctx, value, to):
+    """With a norm that is not finite the clip tensors get what the formula gives (g times max_norm / norm: zero or not a number)."""
+    host, grads = grads_of([4097, 30], 7)
+    out = [torch.empty(g.numel(), dtype=to, device="cuda") for g in grads]
+    tensors = vd.TensorList(ctx, grads, clipped=out)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    vd.vardrop_clip_grads(ctx, tensors, vd.vardrop_grad_norm(ctx, tensors), 0.5, status=status)
+    assert int(status) == 0 and all(bool(c.any()) for c in out)
+    grads[0][4096] = value
+    norm = vd.vardrop_grad_norm(ctx, tensors)
+    vd.vardrop_clip_grads(ctx, tensors, norm, 0.5, status=status)
+    assert int(status) == 1
+    for g, c in zip(grads, out):
+        want = (g * (0.5 / (norm + 1e-6))).to(to)
+        assert torch.equal(c.nan_to_num(7.0), want.nan_to_num(7.0))
