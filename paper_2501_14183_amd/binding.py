@@ -734,6 +734,13 @@ class TensorList:
         ctx.check(rc, "vardrop_tensor_list_build")
 
 
+def _clip_norm(max_norm, where):
+    """max_norm, 0 for no clipping, as the library gets it: one that only rounds to 0 is none."""
+    if 0.0 < max_norm <= 2.0 ** -150:
+        raise VarDropError(-1, where)
+    return max_norm
+
+
 def vardrop_grad_norm(ctx, tensors, out=None, stream=None):
     """Global norm of a TensorList's gradients -> float32 [1] on the device (`out` when given)."""
     if out is None:
@@ -754,7 +761,8 @@ def vardrop_clip_grads(ctx, tensors, norm, max_norm, status=None, stream=None):
 
 def vardrop_adamw(ctx, tensors, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, norm=None, max_norm=0.0, status=None, stream=None):
     """AdamW step number `step` (from 1) of a TensorList with params; with `norm` and max_norm the gradients are clipped in it."""
-    rc = ctx._lib.vardrop_adamw(ctx.handle, tensors.pointer, lr, beta1, beta2, eps, step, _p(norm), max_norm, _p(status),
+    rc = ctx._lib.vardrop_adamw(ctx.handle, tensors.pointer, lr, beta1, beta2, eps, step, _p(norm),
+                                _clip_norm(max_norm, "vardrop_adamw"), _p(status),
                                 _stream(tensors.table, stream))
     if rc:
         ctx.check(rc, "vardrop_adamw")
@@ -764,6 +772,6 @@ def vardrop_adamw_dev(ctx, tensors, lr_dev, step_dev, beta1=0.9, beta2=0.999, ep
                       status=None, stream=None):
     """vardrop_adamw with the rate (float32 [1]) and the number of steps done (int64 [1], advanced) in device memory."""
     rc = ctx._lib.vardrop_adamw_dev(ctx.handle, tensors.pointer, _p(lr_dev), beta1, beta2, eps, _p(step_dev), 1 if advance else 0,
-                                    _p(norm), max_norm, _p(status), _stream(tensors.table, stream))
+                                    _p(norm), _clip_norm(max_norm, "vardrop_adamw_dev"), _p(status), _stream(tensors.table, stream))
     if rc:
         ctx.check(rc, "vardrop_adamw_dev")
