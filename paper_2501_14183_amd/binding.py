@@ -133,6 +133,15 @@ def _p(t):
     return None if t is None else t.data_ptr()
 
 
+def _scalar(name, t, dtype, device):
+    """Address of a number that the library reads or writes in the memory of `device` (None: not given)."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.get_device() == device and t.numel() > 0:
+        return t.data_ptr()
+    raise TypeError("%s must hold a %s on device %d: got %s %s on %s" % (name, dtype, device, t.dtype, list(t.shape), t.device))
+
+
 # torch's own short cut to the current stream's handle: 0.1 us where the stream object takes 2 us, a third of a short call.
 _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -723,6 +732,7 @@ class TensorList:
         rates = None if decay is None else (ctypes.c_float * room)(*decay)
         sizes = (ctypes.c_int64 * room)(*numel)
         self.tensors = (grads, clipped, params, exp_avg, exp_avg_sq, weights)
+        self.device = device
         nbytes = ctx._lib.vardrop_tensor_list_bytes(count, sizes)
         if nbytes == 0:
             raise VarDropError(-1, "vardrop_tensor_list_bytes")
@@ -746,7 +756,8 @@ def vardrop_grad_norm(ctx, tensors, out=None, stream=None):
     if out is None:
         _own_buffers(stream, "vardrop_grad_norm", out=out)
         out = torch.empty(1, dtype=torch.float32, device=ctx.device)
-    rc = ctx._lib.vardrop_grad_norm(ctx.handle, tensors.pointer, out.data_ptr(), _stream(tensors.table, stream))
+    rc = ctx._lib.vardrop_grad_norm(ctx.handle, tensors.pointer, _scalar("out", out, torch.float32, tensors.device),
+                                    _stream(tensors.table, stream))
     if rc:
         ctx.check(rc, "vardrop_grad_norm")
     return out
@@ -754,15 +765,16 @@ def vardrop_grad_norm(ctx, tensors, out=None, stream=None):
 
 def vardrop_clip_grads(ctx, tensors, norm, max_norm, status=None, stream=None):
     """Gradients times min(1, max_norm / (norm + 1e-6)) into the list's `clipped` tensors (in place without them)."""
-    rc = ctx._lib.vardrop_clip_grads(ctx.handle, tensors.pointer, _p(norm), max_norm, _p(status), _stream(tensors.table, stream))
+    rc = ctx._lib.vardrop_clip_grads(ctx.handle, tensors.pointer, _scalar("norm", norm, torch.float32, tensors.device), max_norm,
+                                     _scalar("status", status, torch.int32, tensors.device), _stream(tensors.table, stream))
     if rc:
         ctx.check(rc, "vardrop_clip_grads")
 
 
 def vardrop_adamw(ctx, tensors, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, norm=None, max_norm=0.0, status=None, stream=None):
     """AdamW step number `step` (from 1) of a TensorList with params; with `norm` and max_norm the gradients are clipped in it."""
-    rc = ctx._lib.vardrop_adamw(ctx.handle, tensors.pointer, lr, beta1, beta2, eps, step, _p(norm),
-                                _clip_norm(max_norm, "vardrop_adamw"), _p(status),
+    rc = ctx._lib.vardrop_adamw(ctx.handle, tensors.pointer, lr, beta1, beta2, eps, step, _scalar("norm", norm, torch.float32, tensors.device),
+                                _clip_norm(max_norm, "vardrop_adamw"), _scalar("status", status, torch.int32, tensors.device),
                                 _stream(tensors.table, stream))
     if rc:
         ctx.check(rc, "vardrop_adamw")
@@ -771,7 +783,9 @@ def vardrop_adamw(ctx, tensors, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, norm
 def vardrop_adamw_dev(ctx, tensors, lr_dev, step_dev, beta1=0.9, beta2=0.999, eps=1e-8, norm=None, max_norm=0.0, advance=True,
                       status=None, stream=None):
     """vardrop_adamw with the rate (float32 [1]) and the number of steps done (int64 [1], advanced) in device memory."""
-    rc = ctx._lib.vardrop_adamw_dev(ctx.handle, tensors.pointer, _p(lr_dev), beta1, beta2, eps, _p(step_dev), 1 if advance else 0,
-                                    _p(norm), _clip_norm(max_norm, "vardrop_adamw_dev"), _p(status), _stream(tensors.table, stream))
+    rc = ctx._lib.vardrop_adamw_dev(ctx.handle, tensors.pointer, _scalar("lr_dev", lr_dev, torch.float32, tensors.device), beta1, beta2, eps,
+                                    _scalar("step_dev", step_dev, torch.int64, tensors.device), 1 if advance else 0,
+                                    _scalar("norm", norm, torch.float32, tensors.device), _clip_norm(max_norm, "vardrop_adamw_dev"),
+                                    _scalar("status", status, torch.int32, tensors.device), _stream(tensors.table, stream))
     if rc:
         ctx.check(rc, "vardrop_adamw_dev")

@@ -45,7 +45,7 @@ class Ctx:
 def a_list():
     """A TensorList that was not built."""
     tensors = object.__new__(vd.TensorList)
-    tensors.table, tensors.struct = gpu(256, dtype=torch.uint8), binding._TensorListStruct()
+    tensors.device, tensors.table, tensors.struct = 0, gpu(256, dtype=torch.uint8), binding._TensorListStruct()
     tensors.pointer = ctypes.addressof(tensors.struct)
     return tensors
 
@@ -64,3 +64,35 @@ def test_a_clipping_norm_that_single_precision_takes_for_none_is_refused():
         vd.vardrop_adamw(ctx, tensors, 0.1, 1, norm=gpu(1), max_norm=max_norm, stream=0)
         vd.vardrop_adamw_dev(ctx, tensors, gpu(1), gpu(1, dtype=I64), norm=gpu(1), max_norm=max_norm, stream=0)
     assert ctx._lib.calls == ["vardrop_adamw", "vardrop_adamw_dev"] * 3
+
+
+# what may stand in the place of a device scalar of the given type
+def bad_scalars(dtype):
+    other = {F32: torch.float64, I32: I64, I64: I32}[dtype]
+    return [torch.zeros(1, dtype=dtype), gpu(1, dtype=other), gpu(1, dtype=BF16), gpu(0, dtype=dtype)]
+
+
+def optimiser_calls():
+    """The library that counts, and (call, its device scalars with their types)."""
+    ctx, tensors = Ctx(), a_list()
+    return ctx._lib, [
+        (lambda **k: vd.vardrop_grad_norm(ctx, tensors, stream=0, **k), dict(out=F32)),
+        (lambda **k: vd.vardrop_clip_grads(ctx, tensors, max_norm=1.0, stream=0, **k), dict(norm=F32, status=I32)),
+        (lambda **k: vd.vardrop_adamw(ctx, tensors, 0.1, 1, max_norm=1.0, stream=0, **k), dict(norm=F32, status=I32)),
+        (lambda **k: vd.vardrop_adamw_dev(ctx, tensors, max_norm=1.0, stream=0, **k),
+         dict(lr_dev=F32, step_dev=I64, norm=F32, status=I32)),
+    ]
+
+
+def test_device_scalars_of_the_optimiser():
+    library, calls = optimiser_calls()
+    for call, scalars in calls:
+        good = {name: gpu(1, dtype=dtype) for name, dtype in scalars.items()}
+        for name, dtype in scalars.items():
+            for bad in bad_scalars(dtype):
+                with pytest.raises(TypeError):
+                    call(**{**good, name: bad})
+    assert library.calls == []
+    for call, scalars in calls:
+        call(**{name: gpu(3, dtype=dtype)[1:] for name, dtype in scalars.items()})
+    assert library.calls == ["vardrop_grad_norm", "vardrop_clip_grads", "vardrop_adamw", "vardrop_adamw_dev"]
