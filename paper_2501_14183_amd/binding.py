@@ -146,16 +146,20 @@ def _scalar(name, t, dtype, device):
 _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream(t, stream=None):
-    """Raw hipStream_t: `stream` (an integer handle, e.g. torch.cuda.Stream.cuda_stream) or torch's current one."""
+def _device_stream(device, stream=None):
+    """Raw hipStream_t: `stream` (an integer handle, e.g. torch.cuda.Stream.cuda_stream) or torch's current one on `device`."""
     if stream is not None:
         return stream
-    device = t.get_device()
     if device < 0:
         raise TypeError("the tensors must be on the GPU")
     if _current_raw_stream is not None:
         return _current_raw_stream(device)
     return torch.cuda.current_stream(device).cuda_stream
+
+
+def _stream(t, stream=None):
+    """_device_stream of a tensor's device."""
+    return _device_stream(t.get_device(), stream)
 
 
 def _own_buffers(stream, what, **bufs):
@@ -757,7 +761,7 @@ def vardrop_grad_norm(ctx, tensors, out=None, stream=None):
         _own_buffers(stream, "vardrop_grad_norm", out=out)
         out = torch.empty(1, dtype=torch.float32, device=ctx.device)
     rc = ctx._lib.vardrop_grad_norm(ctx.handle, tensors.pointer, _scalar("out", out, torch.float32, tensors.device),
-                                    _stream(tensors.table, stream))
+                                    _device_stream(tensors.device, stream))
     if rc:
         ctx.check(rc, "vardrop_grad_norm")
     return out
@@ -766,7 +770,7 @@ def vardrop_grad_norm(ctx, tensors, out=None, stream=None):
 def vardrop_clip_grads(ctx, tensors, norm, max_norm, status=None, stream=None):
     """Gradients times min(1, max_norm / (norm + 1e-6)) into the list's `clipped` tensors (in place without them)."""
     rc = ctx._lib.vardrop_clip_grads(ctx.handle, tensors.pointer, _scalar("norm", norm, torch.float32, tensors.device), max_norm,
-                                     _scalar("status", status, torch.int32, tensors.device), _stream(tensors.table, stream))
+                                     _scalar("status", status, torch.int32, tensors.device), _device_stream(tensors.device, stream))
     if rc:
         ctx.check(rc, "vardrop_clip_grads")
 
@@ -775,7 +779,7 @@ def vardrop_adamw(ctx, tensors, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, norm
     """AdamW step number `step` (from 1) of a TensorList with params; with `norm` and max_norm the gradients are clipped in it."""
     rc = ctx._lib.vardrop_adamw(ctx.handle, tensors.pointer, lr, beta1, beta2, eps, step, _scalar("norm", norm, torch.float32, tensors.device),
                                 _clip_norm(max_norm, "vardrop_adamw"), _scalar("status", status, torch.int32, tensors.device),
-                                _stream(tensors.table, stream))
+                                _device_stream(tensors.device, stream))
     if rc:
         ctx.check(rc, "vardrop_adamw")
 
@@ -786,6 +790,6 @@ def vardrop_adamw_dev(ctx, tensors, lr_dev, step_dev, beta1=0.9, beta2=0.999, ep
     rc = ctx._lib.vardrop_adamw_dev(ctx.handle, tensors.pointer, _scalar("lr_dev", lr_dev, torch.float32, tensors.device), beta1, beta2, eps,
                                     _scalar("step_dev", step_dev, torch.int64, tensors.device), 1 if advance else 0,
                                     _scalar("norm", norm, torch.float32, tensors.device), _clip_norm(max_norm, "vardrop_adamw_dev"),
-                                    _scalar("status", status, torch.int32, tensors.device), _stream(tensors.table, stream))
+                                    _scalar("status", status, torch.int32, tensors.device), _device_stream(tensors.device, stream))
     if rc:
         ctx.check(rc, "vardrop_adamw_dev")
