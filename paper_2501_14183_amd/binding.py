@@ -148,10 +148,10 @@ _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 def _device_stream(device, stream=None):
     """Raw hipStream_t: `stream` (an integer handle, e.g. torch.cuda.Stream.cuda_stream) or torch's current one on `device`."""
-    if stream is not None:
-        return stream
     if device < 0:
         raise TypeError("the tensors must be on the GPU")
+    if stream is not None:
+        return stream
     if _current_raw_stream is not None:
         return _current_raw_stream(device)
     return torch.cuda.current_stream(device).cuda_stream
@@ -159,7 +159,7 @@ def _device_stream(device, stream=None):
 
 def _stream(t, stream=None):
     """_device_stream of a tensor's device."""
-    return _device_stream(t.get_device(), stream)
+    return stream if stream is not None else _device_stream(t.get_device())
 
 
 def _own_buffers(stream, what, **bufs):
@@ -538,7 +538,8 @@ _CODES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
 def _refuse(name, t, numel, dtype):
-    raise TypeError("%s must be contiguous, %s, of %d elements: got %s %s" % (name, dtype, numel, t.dtype, list(t.shape)))
+    raise TypeError("%s must be contiguous, %s, of %d elements, on the device of the call's first tensor: got %s %s on %s"
+                    % (name, dtype, numel, t.dtype, list(t.shape), t.device))
 
 
 def _block_type(res, *others):
@@ -550,8 +551,6 @@ def _block_type(res, *others):
 
 
 def _gate_rows(gate, B, d):
-    if gate is None:
-        return 0
     k = gate.numel()
     if gate.shape[-1] != d or (k != d and k != B * d):
         raise TypeError("gate must be [d], [1, d] or [B, d]")
@@ -572,7 +571,7 @@ def vardrop_block_norm_fwd(ctx, x, f=None, pre=NORM_LAYER, w=None, b=None, post=
     triple of preallocated tensors; entries that are None are not written (h is None exactly when pre is NORM_NONE).
     n_dev (int32 [1] on the device): the tensors are buffers for x.shape[1] tokens that hold [B, N', d] packed."""
     B, n, d = x.shape
-    res, dt, fp32 = x.dtype, _block_type(x, f, w, b, wp, bp, gate), torch.float32
+    res, dt, fp32 = x.dtype, f.dtype if f is not None else _block_type(x, w, b, wp, bp, gate), torch.float32
     if out is not None:
         r, h, stats = out
     else:
@@ -580,29 +579,35 @@ def vardrop_block_norm_fwd(ctx, x, f=None, pre=NORM_LAYER, w=None, b=None, post=
         r = torch.empty_like(x) if want_r or pre == NORM_NONE else None
         h = torch.empty((B, n, d), dtype=dt, device=x.device) if pre != NORM_NONE else None
         stats = torch.empty((B * n, 4), dtype=torch.float32, device=x.device) if want_stats else None
+    dev = x.get_device()                       # and all others on the same
     rows = B * n
     k = rows * d
-    gates = _gate_rows(gate, B, d)
+    gates = 0 if gate is None else _gate_rows(gate, B, d)
     p_x = x.data_ptr() if x.dtype is res and x.numel() == k and x.is_contiguous() else _refuse("x", x, k, res)
-    p_f = None if f is None else f.data_ptr() if f.dtype is dt and f.numel() == k and f.is_contiguous() else _refuse("f", f, k, dt)
-    p_r = None if r is None else (r.data_ptr() if r.dtype is res and r.numel() == k and r.is_contiguous()
+    p_f = None if f is None else (f.data_ptr() if f.dtype is dt and f.numel() == k and f.is_contiguous() and f.get_device() == dev
+                                  else _refuse("f", f, k, dt))
+    p_r = None if r is None else (r.data_ptr() if r.dtype is res and r.numel() == k and r.is_contiguous() and r.get_device() == dev
                                   else _refuse("r", r, k, res))
-    p_h = None if h is None else h.data_ptr() if h.dtype is dt and h.numel() == k and h.is_contiguous() else _refuse("h", h, k, dt)
-    p_w = None if w is None else w.data_ptr() if w.dtype is dt and w.numel() == d and w.is_contiguous() else _refuse("w", w, d, dt)
-    p_b = None if b is None else b.data_ptr() if b.dtype is dt and b.numel() == d and b.is_contiguous() else _refuse("b", b, d, dt)
+    p_h = None if h is None else (h.data_ptr() if h.dtype is dt and h.numel() == k and h.is_contiguous() and h.get_device() == dev
+                                  else _refuse("h", h, k, dt))
+    p_w = None if w is None else (w.data_ptr() if w.dtype is dt and w.numel() == d and w.is_contiguous() and w.get_device() == dev
+                                  else _refuse("w", w, d, dt))
+    p_b = None if b is None else (b.data_ptr() if b.dtype is dt and b.numel() == d and b.is_contiguous() and b.get_device() == dev
+                                  else _refuse("b", b, d, dt))
     p_wp = None if wp is None else (wp.data_ptr() if wp.dtype is dt and wp.numel() == d and wp.is_contiguous()
-                                    else _refuse("wp", wp, d, dt))
+                                    and wp.get_device() == dev else _refuse("wp", wp, d, dt))
     p_bp = None if bp is None else (bp.data_ptr() if bp.dtype is dt and bp.numel() == d and bp.is_contiguous()
-                                    else _refuse("bp", bp, d, dt))
+                                    and bp.get_device() == dev else _refuse("bp", bp, d, dt))
     p_gate = None if gate is None else (gate.data_ptr() if gate.dtype is dt and gate.numel() == gates * d and gate.is_contiguous()
-                                        else _refuse("gate", gate, gates * d, dt))
+                                        and gate.get_device() == dev else _refuse("gate", gate, gates * d, dt))
     p_stats = None if stats is None else (stats.data_ptr() if stats.dtype is fp32 and stats.numel() == 4 * rows and stats.is_contiguous()
-                                          else _refuse("stats", stats, 4 * rows, fp32))
-    args = (post, p_wp, p_bp, p_gate, gates, alpha, beta, pre, p_w, p_b, eps, p_r, p_h, p_stats, _stream(x, stream))
+                                          and stats.get_device() == dev else _refuse("stats", stats, 4 * rows, fp32))
+    args = (post, p_wp, p_bp, p_gate, gates, alpha, beta, pre, p_w, p_b, eps, p_r, p_h, p_stats, _device_stream(dev, stream))
     if n_dev is None:
         rc = ctx._lib.vardrop_block_norm_fwd(ctx.handle, p_x, p_f, B, n, d, _CODES.get(res, -1), _CODES.get(dt, -1), *args)
     else:
-        rc = ctx._lib.vardrop_block_norm_fwd_dev(ctx.handle, p_x, p_f, B, _p(n_dev), n, _p(status), d, _CODES.get(res, -1),
+        rc = ctx._lib.vardrop_block_norm_fwd_dev(ctx.handle, p_x, p_f, B, _scalar("n_dev", n_dev, torch.int32, dev), n,
+                                                 _scalar("status", status, torch.int32, dev), d, _CODES.get(res, -1),
                                                  _CODES.get(dt, -1), *args)
     if rc:
         ctx.check(rc, "vardrop_block_norm_fwd")
@@ -619,7 +624,7 @@ def vardrop_block_norm_bwd(ctx, dr, dh, r, f, stats, pre=NORM_LAYER, w=None, pos
     tuple of preallocated tensors; entries that are None are skipped."""
     like = dr if dr is not None else r
     B, n, d = like.shape
-    res, dt, fp32 = like.dtype, _block_type(like, dh, f, w, wp, bp, gate), torch.float32
+    res, dt, fp32 = like.dtype, dh.dtype if dh is not None else _block_type(like, f, w, wp, bp, gate), torch.float32
     if out is not None:
         dx, df, dw, db, dwp, dbp, dgate = out
     else:
@@ -633,49 +638,55 @@ def vardrop_block_norm_bwd(ctx, dr, dh, r, f, stats, pre=NORM_LAYER, w=None, pos
         dw, db = vector(w is not None, d), vector(bias_grads and pre != NORM_NONE, d)
         dwp, dbp = vector(wp is not None, d), vector(bias_grads and post != NORM_NONE, d)
         dgate = None if gate is None else vector(True, *gate.shape)
+    dev = like.get_device()                    # and all others on the same
     rows = B * n
     k = rows * d
-    gates = _gate_rows(gate, B, d)
+    gates = 0 if gate is None else _gate_rows(gate, B, d)
     p_dr = None if dr is None else (dr.data_ptr() if dr.dtype is res and dr.numel() == k and dr.is_contiguous()
                                     else _refuse("dr", dr, k, res))
     p_dh = None if dh is None else (dh.data_ptr() if dh.dtype is dt and dh.numel() == k and dh.is_contiguous()
-                                    else _refuse("dh", dh, k, dt))
-    p_r = None if r is None else (r.data_ptr() if r.dtype is res and r.numel() == k and r.is_contiguous()
+                                    and dh.get_device() == dev else _refuse("dh", dh, k, dt))
+    p_r = None if r is None else (r.data_ptr() if r.dtype is res and r.numel() == k and r.is_contiguous() and r.get_device() == dev
                                   else _refuse("r", r, k, res))
-    p_f = None if f is None else f.data_ptr() if f.dtype is dt and f.numel() == k and f.is_contiguous() else _refuse("f", f, k, dt)
+    p_f = None if f is None else (f.data_ptr() if f.dtype is dt and f.numel() == k and f.is_contiguous() and f.get_device() == dev
+                                  else _refuse("f", f, k, dt))
     p_dx = None if dx is None else (dx.data_ptr() if dx.dtype is res and dx.numel() == k and dx.is_contiguous()
-                                    else _refuse("dx", dx, k, res))
+                                    and dx.get_device() == dev else _refuse("dx", dx, k, res))
     p_df = None if df is None else (df.data_ptr() if df.dtype is dt and df.numel() == k and df.is_contiguous()
-                                    else _refuse("df", df, k, dt))
-    p_w = None if w is None else w.data_ptr() if w.dtype is dt and w.numel() == d and w.is_contiguous() else _refuse("w", w, d, dt)
+                                    and df.get_device() == dev else _refuse("df", df, k, dt))
+    p_w = None if w is None else (w.data_ptr() if w.dtype is dt and w.numel() == d and w.is_contiguous() and w.get_device() == dev
+                                  else _refuse("w", w, d, dt))
     p_wp = None if wp is None else (wp.data_ptr() if wp.dtype is dt and wp.numel() == d and wp.is_contiguous()
-                                    else _refuse("wp", wp, d, dt))
+                                    and wp.get_device() == dev else _refuse("wp", wp, d, dt))
     p_bp = None if bp is None else (bp.data_ptr() if bp.dtype is dt and bp.numel() == d and bp.is_contiguous()
-                                    else _refuse("bp", bp, d, dt))
+                                    and bp.get_device() == dev else _refuse("bp", bp, d, dt))
     p_gate = None if gate is None else (gate.data_ptr() if gate.dtype is dt and gate.numel() == gates * d and gate.is_contiguous()
-                                        else _refuse("gate", gate, gates * d, dt))
+                                        and gate.get_device() == dev else _refuse("gate", gate, gates * d, dt))
     p_stats = None if stats is None else (stats.data_ptr() if stats.dtype is fp32 and stats.numel() == 4 * rows and stats.is_contiguous()
-                                          else _refuse("stats", stats, 4 * rows, fp32))
+                                          and stats.get_device() == dev else _refuse("stats", stats, 4 * rows, fp32))
     p_dw = None if dw is None else (dw.data_ptr() if dw.dtype is fp32 and dw.numel() == d and dw.is_contiguous()
-                                    else _refuse("dw", dw, d, fp32))
+                                    and dw.get_device() == dev else _refuse("dw", dw, d, fp32))
     p_db = None if db is None else (db.data_ptr() if db.dtype is fp32 and db.numel() == d and db.is_contiguous()
-                                    else _refuse("db", db, d, fp32))
+                                    and db.get_device() == dev else _refuse("db", db, d, fp32))
     p_dwp = None if dwp is None else (dwp.data_ptr() if dwp.dtype is fp32 and dwp.numel() == d and dwp.is_contiguous()
-                                      else _refuse("dwp", dwp, d, fp32))
+                                      and dwp.get_device() == dev else _refuse("dwp", dwp, d, fp32))
     p_dbp = None if dbp is None else (dbp.data_ptr() if dbp.dtype is fp32 and dbp.numel() == d and dbp.is_contiguous()
-                                      else _refuse("dbp", dbp, d, fp32))
+                                      and dbp.get_device() == dev else _refuse("dbp", dbp, d, fp32))
     p_dgate = None if dgate is None else (dgate.data_ptr() if dgate.dtype is fp32 and dgate.numel() == gates * d and dgate.is_contiguous()
-                                          else _refuse("dgate", dgate, gates * d, fp32))
+                                          and dgate.get_device() == dev else _refuse("dgate", dgate, gates * d, fp32))
     if ws is None and (dw is not None or db is not None or dwp is not None or dbp is not None or dgate is not None):
         _own_buffers(stream, "vardrop_block_norm_bwd", ws=ws)
         ws = torch.empty(vardrop_block_norm_workspace_bytes(B, n, d, gates), dtype=torch.uint8, device=like.device)
+    if ws is not None and not (ws.is_contiguous() and ws.get_device() == dev):
+        raise TypeError("ws must be contiguous, on device %d" % dev)
     tokens = (p_dr, p_dh, p_r, p_f, p_stats)
     args = (post, p_wp, p_bp, p_gate, gates, alpha, beta, pre, p_w, p_dx, p_df, p_dw, p_db, p_dwp, p_dbp, p_dgate, _p(ws),
-            0 if ws is None else ws.numel(), _stream(like, stream))
+            0 if ws is None else ws.numel(), _device_stream(dev, stream))
     if n_dev is None:
         rc = ctx._lib.vardrop_block_norm_bwd(ctx.handle, *tokens, B, n, d, _CODES.get(res, -1), _CODES.get(dt, -1), *args)
     else:
-        rc = ctx._lib.vardrop_block_norm_bwd_dev(ctx.handle, *tokens, B, _p(n_dev), n, _p(status), d, _CODES.get(res, -1),
+        rc = ctx._lib.vardrop_block_norm_bwd_dev(ctx.handle, *tokens, B, _scalar("n_dev", n_dev, torch.int32, dev), n,
+                                                 _scalar("status", status, torch.int32, dev), d, _CODES.get(res, -1),
                                                  _CODES.get(dt, -1), *args)
     if rc:
         ctx.check(rc, "vardrop_block_norm_bwd")

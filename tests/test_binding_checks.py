@@ -96,3 +96,53 @@ def test_device_scalars_of_the_optimiser():
     for call, scalars in calls:
         call(**{name: gpu(3, dtype=dtype)[1:] for name, dtype in scalars.items()})
     assert library.calls == ["vardrop_grad_norm", "vardrop_clip_grads", "vardrop_adamw", "vardrop_adamw_dev"]
+
+
+def norm_arguments(B=2, n=3, d=8):
+    """Everything the two calls take, on the GPU: (forward, backward), results and gradients under their own names."""
+    tokens = lambda: gpu(B, n, d)
+    forward = dict(x=tokens(), f=tokens(), w=gpu(d), b=gpu(d), wp=gpu(d), bp=gpu(d), gate=gpu(B, d), r=tokens(), h=tokens(),
+                   stats=gpu(B * n, 4), n_dev=gpu(1, dtype=I32), status=gpu(1, dtype=I32))
+    backward = dict(dr=tokens(), dh=tokens(), r=tokens(), f=tokens(), stats=gpu(B * n, 4), w=gpu(d), wp=gpu(d), bp=gpu(d), gate=gpu(B, d),
+                    ws=gpu(vd.vardrop_block_norm_workspace_bytes(B, n, d, B), dtype=torch.uint8), n_dev=gpu(1, dtype=I32),
+                    status=gpu(1, dtype=I32), dx=tokens(), df=tokens(), dw=gpu(d), db=gpu(d), dwp=gpu(d), dbp=gpu(d), dgate=gpu(B, d))
+    return forward, backward
+
+
+def call_norm(ctx, arguments):
+    a = dict(arguments)
+    kinds = dict(pre=vd.NORM_LAYER, post=vd.NORM_RMS, stream=0)
+    if "x" in a:
+        out = tuple(a.pop(k) for k in ("r", "h", "stats"))
+        return vd.vardrop_block_norm_fwd(ctx, out=out, **a, **kinds)
+    out = tuple(a.pop(k) for k in ("dx", "df", "dw", "db", "dwp", "dbp", "dgate"))
+    return vd.vardrop_block_norm_bwd(ctx, out=out, **a, **kinds)
+
+
+@pytest.mark.parametrize("which,name", [(i, k) for i, a in enumerate(norm_arguments()) for k in a])
+def test_every_tensor_of_the_block_norms_has_to_be_on_the_device(which, name):
+    ctx, arguments = Ctx(), norm_arguments()[which]
+    call_norm(ctx, arguments)
+    assert len(ctx._lib.calls) == 1
+    with pytest.raises(TypeError):
+        call_norm(ctx, {**arguments, name: torch.zeros_like(arguments[name].as_subclass(torch.Tensor))})
+    assert len(ctx._lib.calls) == 1
+
+
+@pytest.mark.parametrize("which,name", [(i, k) for i in (0, 1) for k in ("n_dev", "status")])
+def test_device_scalars_of_the_block_norms(which, name):
+    ctx, arguments = Ctx(), norm_arguments()[which]
+    for bad in bad_scalars(I32):
+        with pytest.raises(TypeError):
+            call_norm(ctx, {**arguments, name: bad})
+    assert ctx._lib.calls == []
+
+
+def test_a_workspace_that_is_smaller_than_it_says_is_refused():
+    """An expanded view counts its elements, not the memory behind them."""
+    ctx, arguments = Ctx(), norm_arguments()[1]
+    size = arguments["ws"].numel()
+    for bad in (gpu(1, dtype=torch.uint8).expand(size), gpu(2 * size, dtype=torch.uint8)[::2]):
+        with pytest.raises(TypeError):
+            call_norm(ctx, {**arguments, "ws": bad})
+    assert ctx._lib.calls == []
