@@ -543,7 +543,7 @@ def _refuse(name, t, numel, dtype):
 
 
 def _block_type(res, *others):
-    """Element type of a block's tensors (the first one given), that of the residual stream where there is none."""
+    """Element type of a block's tensors (the first one given, results included), that of the residual stream where there is none."""
     for t in others:
         if t is not None:
             return t.dtype
@@ -571,10 +571,10 @@ def vardrop_block_norm_fwd(ctx, x, f=None, pre=NORM_LAYER, w=None, b=None, post=
     triple of preallocated tensors; entries that are None are not written (h is None exactly when pre is NORM_NONE).
     n_dev (int32 [1] on the device): the tensors are buffers for x.shape[1] tokens that hold [B, N', d] packed."""
     B, n, d = x.shape
-    res, dt, fp32 = x.dtype, f.dtype if f is not None else _block_type(x, w, b, wp, bp, gate), torch.float32
-    if out is not None:
-        r, h, stats = out
-    else:
+    res, fp32 = x.dtype, torch.float32
+    r, h, stats = (None, None, None) if out is None else out
+    dt = f.dtype if f is not None else _block_type(x, h, w, b, wp, bp, gate)
+    if out is None:
         _own_buffers(stream, "vardrop_block_norm_fwd", out=out)
         r = torch.empty_like(x) if want_r or pre == NORM_NONE else None
         h = torch.empty((B, n, d), dtype=dt, device=x.device) if pre != NORM_NONE else None
@@ -624,10 +624,10 @@ def vardrop_block_norm_bwd(ctx, dr, dh, r, f, stats, pre=NORM_LAYER, w=None, pos
     tuple of preallocated tensors; entries that are None are skipped."""
     like = dr if dr is not None else r
     B, n, d = like.shape
-    res, dt, fp32 = like.dtype, dh.dtype if dh is not None else _block_type(like, f, w, wp, bp, gate), torch.float32
-    if out is not None:
-        dx, df, dw, db, dwp, dbp, dgate = out
-    else:
+    res, fp32 = like.dtype, torch.float32
+    dx, df, dw, db, dwp, dbp, dgate = (None,) * 7 if out is None else out
+    dt = dh.dtype if dh is not None else _block_type(like, f, df, w, wp, bp, gate)
+    if out is None:
         _own_buffers(stream, "vardrop_block_norm_bwd", out=out)
 
         def vector(wanted, *shape):

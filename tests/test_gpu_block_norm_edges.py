@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from oracle import block_norm as o
-from test_gpu_block_norm import TYPES, U, make
+from test_gpu_block_norm import K_ROW, TYPES, U, backward_magnitudes, close, forward_magnitudes, make
 from util_gpu import to_dev, torch_dtype
 
 pytestmark = pytest.mark.gpu
@@ -81,3 +81,41 @@ def test_an_infinite_gradient_makes_an_infinite_gate_gradient_without_a_bias(vd,
     assert got[-1, 7] == sign * np.inf
     got[-1, 7] = 0.0
     assert np.isfinite(got).all()
+
+
+@pytest.mark.parametrize("pre", ["layer", "rms"])
+def test_a_first_block_without_weights_in_another_type_than_the_residual(vd, ctx, pre):
+    """Only the results say that the block is bf16 beside a fp32 residual."""
+    t = make(4, 2, 9, 136, "fp32", "bf16", pre, "none", "none")
+    t = {**t, **dict.fromkeys(("f", "w", "b", "gate"))}
+    dev = on_device(t, "fp32", "bf16")
+    kind = {"layer": vd.NORM_LAYER, "rms": vd.NORM_RMS}[pre]
+    h, stats = torch.empty(2, 9, 136, dtype=torch.bfloat16, device="cuda"), torch.empty(18, 4, device="cuda")
+    got = vd.vardrop_block_norm_fwd(ctx, dev["x"], pre=kind, out=(None, h, stats))
+    wr, wh, wstats = o.block_norm_forward(t["x"], pre=pre)
+    close(got[1], wh, forward_magnitudes(t, pre, "none", 1.0, 1.0, wstats, wr)[1], K_ROW, "h")
+    st = stats.double().cpu().numpy().reshape(2, 9, 4)
+    dx = torch.empty_like(dev["x"])
+    vd.vardrop_block_norm_bwd(ctx, dev["dr"], dev["dh"], dev["x"], None, stats, pre=kind, out=(dx,) + (None,) * 6)
+    want = o.block_norm_backward(t["dr"], t["dh"], t["x"], None, st, pre=pre)
+    close(dx, want["dx"], backward_magnitudes(t, pre, "none", 1.0, 1.0, st, t["x"])["dx"], K_ROW, "dx")
+
+
+@pytest.mark.parametrize("res,dtype", TYPES)
+@pytest.mark.parametrize("pre", ["none", "layer"])
+@pytest.mark.parametrize("d", [3, 40, 321, 1100])
+def test_the_branch_gradient_needs_no_branch_without_a_post_norm_and_a_gate(vd, ctx, res, dtype, pre, d):
+    """df = beta D with f not given; with no norm at all df alone says what type the block has."""
+    t = make(5, 2, 5, d, res, dtype, pre, "none", "none")
+    dev = on_device(t, res, dtype)
+    kind = {"none": vd.NORM_NONE, "layer": vd.NORM_LAYER}[pre]
+    r, _, stats = vd.vardrop_block_norm_fwd(ctx, dev["x"], dev["f"], pre=kind, w=dev["w"], b=dev["b"], beta=0.5)
+    dx, df = torch.empty_like(dev["x"]), torch.empty_like(dev["f"])
+    vd.vardrop_block_norm_bwd(ctx, dev["dr"], dev["dh"], r if pre == "layer" else None, None, stats, pre=kind, w=dev["w"], beta=0.5,
+                              out=(dx, df) + (None,) * 5)
+    r64, st64 = r.double().cpu().numpy(), stats.double().cpu().numpy().reshape(2, 5, 4)
+    t["f"] = None
+    want = o.block_norm_backward(t["dr"], t["dh"], r64, None, st64, pre=pre, w=t["w"], beta=0.5)
+    mag = backward_magnitudes(t, pre, "none", 1.0, 0.5, st64, r64)
+    close(dx, want["dx"], mag["dx"], K_ROW, "dx")
+    close(df, want["df"], mag["df"], K_ROW, "df")
