@@ -623,6 +623,8 @@ def vardrop_block_norm_bwd(ctx, dr, dh, r, f, stats, pre=NORM_LAYER, w=None, pos
     made when f is given, the vectors' gradients for the vectors given (db, dbp with bias_grads).  `out`, when given, is that
     tuple of preallocated tensors; entries that are None are skipped."""
     like = dr if dr is not None else r
+    if like is None:
+        raise TypeError("one of dr and r has to be given")
     B, n, d = like.shape
     res, fp32 = like.dtype, torch.float32
     dx, df, dw, db, dwp, dbp, dgate = (None,) * 7 if out is None else out

@@ -146,3 +146,10 @@ def test_a_workspace_that_is_smaller_than_it_says_is_refused():
         with pytest.raises(TypeError):
             call_norm(ctx, {**arguments, "ws": bad})
     assert ctx._lib.calls == []
+
+
+def test_a_backward_without_dr_and_r_is_refused():
+    ctx, arguments = Ctx(), norm_arguments()[1]
+    with pytest.raises(TypeError):
+        call_norm(ctx, {**arguments, "dr": None, "r": None})
+    assert ctx._lib.calls == []
