@@ -435,12 +435,20 @@ def vardrop_sample_nearest(ctx, hsh, abar, gs, ratio_num, ratio_den, stream=None
 
 
 # ---------------------------------------------------------------- device-side token count
+def _count(t, n_dev, status):
+    """Device of the tensor t, and the addresses of the count and of the status word there."""
+    device = t.get_device()
+    return device, _scalar("n_dev", n_dev, torch.int32, device), _scalar("status", status, torch.int32, device)
+
+
 def vardrop_sample_dev(ctx, hsh, gs, ratio_num, ratio_den, seed, step_dev, advance, out, stream=None):
     """vardrop_sample with the step counter in device memory (step_dev: int64 [1]); out = (group_id, sel, counts)."""
     N = hsh.shape[0]
     gid, sel, counts = out
-    rc = ctx._lib.vardrop_sample_dev(ctx.handle, _p(hsh), N, gs, ratio_num, ratio_den, seed, _p(step_dev), 1 if advance else 0,
-                                     _p(gid), _p(sel), _p(counts), None, 0, _stream(hsh, stream))
+    device = hsh.get_device()
+    rc = ctx._lib.vardrop_sample_dev(ctx.handle, _p(hsh), N, gs, ratio_num, ratio_den, seed,
+                                     _scalar("step_dev", step_dev, torch.int64, device), 1 if advance else 0,
+                                     _p(gid), _p(sel), _p(counts), None, 0, _device_stream(device, stream))
     ctx.check(rc, "vardrop_sample_dev")
     return gid, sel, counts
 
@@ -448,8 +456,9 @@ def vardrop_sample_dev(ctx, hsh, gs, ratio_num, ratio_den, seed, step_dev, advan
 def vardrop_gather_dev(ctx, tokens, sel, n_dev, n_max, out, status=None, stream=None):
     """tokens [B, N, d], sel int32, n_dev int32 [1] on the device -> out (>= B * n_max * d elements), packed [B, N', d]."""
     B, N, d = tokens.shape
-    rc = ctx._lib.vardrop_gather_dev(ctx.handle, _p(tokens), B, N, d, _dtype_code(tokens), _p(sel), _p(n_dev), n_max,
-                                     _p(status), _p(out), _stream(tokens, stream))
+    device, p_n, p_status = _count(tokens, n_dev, status)
+    rc = ctx._lib.vardrop_gather_dev(ctx.handle, _p(tokens), B, N, d, _dtype_code(tokens), _p(sel), p_n, n_max,
+                                     p_status, _p(out), _device_stream(device, stream))
     ctx.check(rc, "vardrop_gather_dev")
     return out
 
@@ -457,8 +466,9 @@ def vardrop_gather_dev(ctx, tokens, sel, n_dev, n_max, out, status=None, stream=
 def vardrop_scatter_dev(ctx, dxs, sel, n_dev, n_max, out, status=None, stream=None):
     """dxs packed [B, N', d] -> out [B, N, d] with zeros at dropped variates; N' read from n_dev on the device."""
     B, N, d = out.shape
-    rc = ctx._lib.vardrop_scatter_dev(ctx.handle, _p(dxs), B, N, d, _dtype_code(out), _p(sel), _p(n_dev), n_max,
-                                      _p(status), _p(out), _stream(out, stream))
+    device, p_n, p_status = _count(out, n_dev, status)
+    rc = ctx._lib.vardrop_scatter_dev(ctx.handle, _p(dxs), B, N, d, _dtype_code(out), _p(sel), p_n, n_max,
+                                      p_status, _p(out), _device_stream(device, stream))
     ctx.check(rc, "vardrop_scatter_dev")
     return out
 
@@ -468,10 +478,11 @@ def vardrop_gather_attn_fwd_dev(ctx, tokens, sel, n_dev, n_max, Wq, Wk, Wv, Wo, 
     """Gather + attention forward with N' read on the device from n_dev (int32 [1]); xs, y hold >= B * n_max * d
     elements and receive [B, N', d] packed; saved holds vardrop_attn_saved_bytes(B, n_max, d, H) bytes."""
     B, N, d = tokens.shape
-    rc = ctx._lib.vardrop_gather_attn_fwd_dev(ctx.handle, _p(tokens), B, N, _p(sel), _p(n_dev), n_max, _p(status), d, H,
+    device, p_n, p_status = _count(tokens, n_dev, status)
+    rc = ctx._lib.vardrop_gather_attn_fwd_dev(ctx.handle, _p(tokens), B, N, _p(sel), p_n, n_max, p_status, d, H,
                                               _dtype_code(tokens), _p(Wq), _p(Wk), _p(Wv), _p(Wo),
                                               _p(bq), _p(bk), _p(bv), _p(bo), _p(xs), _p(y), _p(saved), None, 0,
-                                              _stream(tokens, stream))
+                                              _device_stream(device, stream))
     ctx.check(rc, "vardrop_gather_attn_fwd_dev")
     return xs, y, saved
 
@@ -483,9 +494,10 @@ def vardrop_attn_bwd_dev(ctx, dy, xs, n_dev, n_max, Wq, Wk, Wv, Wo, H, saved, ws
     d = Wq.shape[0]
     dxs, dW = out[0], list(out[1:5])
     db = list(out[5:9]) if len(out) >= 9 else [None] * 4
-    rc = ctx._lib.vardrop_attn_bwd_dev(ctx.handle, _p(dy), _p(xs), B, _p(n_dev), n_max, _p(status), d, H, _dtype_code(Wq),
+    device, p_n, p_status = _count(Wq, n_dev, status)
+    rc = ctx._lib.vardrop_attn_bwd_dev(ctx.handle, _p(dy), _p(xs), B, p_n, n_max, p_status, d, H, _dtype_code(Wq),
                                        _p(Wq), _p(Wk), _p(Wv), _p(Wo), _p(saved), _p(dxs), *[_p(t) for t in dW],
-                                       *[_p(t) for t in db], _p(ws), ws.numel(), _stream(Wq, stream))
+                                       *[_p(t) for t in db], _p(ws), ws.numel(), _device_stream(device, stream))
     ctx.check(rc, "vardrop_attn_bwd_dev")
     return out
 
@@ -504,9 +516,10 @@ def vardrop_attn_fwd_dev(ctx, xs, n_dev, n_max, Wq, Wk, Wv, Wo, H, y, saved, bq=
                          status=None, stream=None):
     """Attention forward on packed tokens xs ([B, n_max, d] buffer holding [B, N', d]) with N' read on the device."""
     B, d = xs.shape[0], Wq.shape[0]
-    rc = ctx._lib.vardrop_attn_fwd_dev(ctx.handle, _p(xs), B, _p(n_dev), n_max, _p(status), d, H, _dtype_code(Wq),
+    device, p_n, p_status = _count(xs, n_dev, status)
+    rc = ctx._lib.vardrop_attn_fwd_dev(ctx.handle, _p(xs), B, p_n, n_max, p_status, d, H, _dtype_code(Wq),
                                        _p(Wq), _p(Wk), _p(Wv), _p(Wo), _p(bq), _p(bk), _p(bv), _p(bo),
-                                       _p(y), _p(saved), None, 0, _stream(xs, stream))
+                                       _p(y), _p(saved), None, 0, _device_stream(device, stream))
     ctx.check(rc, "vardrop_attn_fwd_dev")
     return y, saved
 
@@ -514,9 +527,10 @@ def vardrop_attn_fwd_dev(ctx, xs, n_dev, n_max, Wq, Wk, Wv, Wo, H, y, saved, bq=
 def vardrop_embed_fwd_dev(ctx, x, sel, n_dev, n_max, We, be, xs, saved, standardise=True, status=None, stream=None):
     """Embedding of the kept windows with their count read on the device; xs: [B, n_max, d] buffer, packed [B, N', d]."""
     B, N, L = x.shape
-    rc = ctx._lib.vardrop_embed_fwd_dev(ctx.handle, _p(x), B, N, L, x.stride(0), x.stride(1), _p(sel), _p(n_dev), n_max,
-                                        _p(status), 1 if standardise else 0, _p(We), _p(be), We.shape[1], _dtype_code(We),
-                                        _p(xs), _p(saved), _stream(x, stream))
+    device, p_n, p_status = _count(x, n_dev, status)
+    rc = ctx._lib.vardrop_embed_fwd_dev(ctx.handle, _p(x), B, N, L, x.stride(0), x.stride(1), _p(sel), p_n, n_max,
+                                        p_status, 1 if standardise else 0, _p(We), _p(be), We.shape[1], _dtype_code(We),
+                                        _p(xs), _p(saved), _device_stream(device, stream))
     ctx.check(rc, "vardrop_embed_fwd_dev")
     return xs, saved
 
@@ -525,8 +539,9 @@ def vardrop_embed_bwd_dev(ctx, dxs, n_dev, n_max, L, saved, ws, out, stream=None
     """Weight gradients of the embedding with the count read on the device; out = (dWe, dbe or None)."""
     B, d = dxs.shape[0], dxs.shape[-1]
     dWe, dbe = out
-    rc = ctx._lib.vardrop_embed_bwd_dev(ctx.handle, _p(dxs), B, _p(n_dev), n_max, L, d, _dtype_code(dxs), _p(saved),
-                                        _p(dWe), _p(dbe), _p(ws), ws.numel(), _stream(dxs, stream))
+    device, p_n, _ = _count(dxs, n_dev, None)
+    rc = ctx._lib.vardrop_embed_bwd_dev(ctx.handle, _p(dxs), B, p_n, n_max, L, d, _dtype_code(dxs), _p(saved),
+                                        _p(dWe), _p(dbe), _p(ws), ws.numel(), _device_stream(device, stream))
     ctx.check(rc, "vardrop_embed_bwd_dev")
     return dWe, dbe
 

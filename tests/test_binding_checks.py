@@ -153,3 +153,39 @@ def test_a_backward_without_dr_and_r_is_refused():
     with pytest.raises(TypeError):
         call_norm(ctx, {**arguments, "dr": None, "r": None})
     assert ctx._lib.calls == []
+
+
+def counted_calls():
+    """The library that counts, and every older call that reads a count or a counter on the device with its scalars' types."""
+    ctx = Ctx()
+    B, N, n, d, L, H = 2, 6, 4, 8, 12, 2
+    tok, few, x, index = gpu(B, N, d), gpu(B, n, d), gpu(B, N, L), gpu(N, dtype=I32)
+    We, room, W, dW = gpu(L, d), gpu(4096, dtype=torch.uint8), [gpu(d, d)] * 4, [gpu(d, d) for _ in range(4)]
+    counts = dict(n_dev=I32, status=I32)
+    return ctx._lib, [
+        (lambda step_dev: vd.vardrop_sample_dev(ctx, gpu(N, dtype=I64), 4, 1, 10, 1, step_dev, True, (index, index, gpu(2, dtype=I32)), stream=0),
+         dict(step_dev=I64)),
+        (lambda n_dev, status: vd.vardrop_gather_dev(ctx, tok, index, n_dev, n, few, status=status, stream=0), counts),
+        (lambda n_dev, status: vd.vardrop_scatter_dev(ctx, few, index, n_dev, n, tok, status=status, stream=0), counts),
+        (lambda n_dev, status: vd.vardrop_gather_attn_fwd_dev(ctx, tok, index, n_dev, n, *W, H, few, few, room, status=status, stream=0), counts),
+        (lambda n_dev, status: vd.vardrop_attn_fwd_dev(ctx, few, n_dev, n, *W, H, few, room, status=status, stream=0), counts),
+        (lambda n_dev, status: vd.vardrop_attn_bwd_dev(ctx, few, few, n_dev, n, *W, H, room, room, (few, *dW), status=status, stream=0), counts),
+        (lambda n_dev, status: vd.vardrop_embed_fwd_dev(ctx, x, index, n_dev, n, We, gpu(d), few, room, status=status, stream=0), counts),
+        (lambda n_dev: vd.vardrop_embed_bwd_dev(ctx, few, n_dev, n, L, room, room, (We, gpu(d)), stream=0), dict(n_dev=I32)),
+    ]
+
+
+def test_device_scalars_of_the_older_calls():
+    library, calls = counted_calls()
+    for call, scalars in calls:
+        good = {name: gpu(1, dtype=dtype) for name, dtype in scalars.items()}
+        for name, dtype in scalars.items():
+            for bad in bad_scalars(dtype):
+                with pytest.raises(TypeError):
+                    call(**{**good, name: bad})
+    assert library.calls == []
+    for call, scalars in calls:
+        call(**{name: gpu(3, dtype=dtype)[1:] for name, dtype in scalars.items()})
+        if "status" in scalars:
+            call(n_dev=gpu(1, dtype=I32), status=None)
+    assert len(library.calls) == 2 * len(calls) - 2
