@@ -125,11 +125,16 @@ def loss_and_gradient(h, target, n_dev, B):
     return diff.square().sum() / count, (2.0 * diff / count).to(h.dtype).reshape(h.shape)
 
 
-def windows(B, N, L, seed):
-    """Noisy daily and weekly profiles, [B, N, L]."""
+def periods():
+    """The profiles' periods, on the device once: a table made there in every step would be a copy that the host waits for."""
+    return torch.tensor([24.0, 12.0, 8.0, 48.0], device="cuda")
+
+
+def windows(B, N, L, seed, table=None):
+    """Noisy daily and weekly profiles, [B, N, L]; table: periods(), made here when it is not given."""
     g = torch.Generator(device="cuda").manual_seed(seed)
     t = torch.arange(L, device="cuda").float() + 24.0 * torch.rand(B, N, 1, generator=g, device="cuda")
-    period = torch.tensor([24.0, 12.0, 8.0, 48.0], device="cuda")[torch.randint(4, (1, N, 1), generator=g, device="cuda")]
+    period = (periods() if table is None else table)[torch.randint(4, (1, N, 1), generator=g, device="cuda")]
     return torch.sin(6.2831853 * t / period) + 0.5 * torch.sin(6.2831853 * t / 24.0) + 0.2 * torch.randn(B, N, L, generator=g, device="cuda")
 
 
@@ -141,9 +146,9 @@ def train(steps=200, B=8, N=96, L=96, d=128, H=2, layers=2, gs=4, rate=2e-3, max
     draw = torch.zeros(1, dtype=torch.int64, device="cuda")
     selection = tuple(torch.zeros(k, dtype=torch.int32, device="cuda") for k in (N, N, 2))
     rate_dev, status = torch.full((1,), rate, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
-    losses = []
+    table, losses = periods(), []
     for step in range(steps):
-        x = windows(B, N, L, seed=step)
+        x = windows(B, N, L, seed=step, table=table)
         _, hashes, _ = vd.vardrop_hash(ctx, x, 2)
         _, sel, counts = vd.vardrop_sample_dev(ctx, hashes, gs, 1, 1, 42, draw, True, selection)
         n_dev = counts[:1]
