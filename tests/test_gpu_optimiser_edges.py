@@ -1,8 +1,10 @@
-"""Tensor lists where a scalar or a gradient is out of the ordinary."""
+"""Tensor lists where a scalar, a gradient or the size is out of the ordinary.  (Bounds of a step: test_gpu_optimiser.py.)"""
 import pytest
 import torch
 
-from test_gpu_optimiser import grads_of
+from oracle import optimiser as o
+from test_gpu_optimiser import check_step, grads_of, norm_close, state_of
+from util_gpu import to_dev
 
 pytestmark = pytest.mark.gpu
 
@@ -91,3 +93,29 @@ def test_clipped_gradients_are_never_those_of_an_earlier_step(vd, ctx, value, to
     for g, c in zip(grads, out):
         want = (g * (0.5 / (norm + 1e-6))).to(to)
         assert torch.equal(c.nan_to_num(7.0), want.nan_to_num(7.0))
+
+
+@pytest.mark.parametrize("low", [False, True])
+def test_a_large_model_steps_on_the_device(vd, ctx, low):
+    """9.6 million weights in 2347 chunks: weights past the caches, counters shared by more than 32 workgroups, norms of workgroups with
+    several chunks; three steps in a row, each against the oracle."""
+    sizes = [4500001, 3, 3000017, 900003, 777777, 409600]
+    host, grads = grads_of(sizes, 11, ("bf16", "fp32"))
+    dev = [[to_dev(a) for a in k] for k in state_of(sizes, 12, True)]
+    weights = [torch.empty(n, dtype=torch.bfloat16, device="cuda") if low or i % 2 else None for i, n in enumerate(sizes)]
+    decay = [0.1 * (i % 2) for i in range(len(sizes))]
+    tensors = vd.TensorList(ctx, grads, params=dev[0], exp_avg=dev[1], exp_avg_sq=dev[2], weights=weights, decay=decay)
+    assert tensors.struct.chunks > 2048 and tensors.struct.numel > 6000000
+    step, rate = torch.full((1,), 40, dtype=torch.int64, device="cuda"), torch.full((1,), 0.01, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    lr = float(rate)
+    for k in range(41, 44):
+        before = [[t.cpu().numpy() for t in a] for a in dev]
+        norm = vd.vardrop_grad_norm(ctx, tensors)
+        norm_close(norm, o.grad_norm(host))
+        vd.vardrop_adamw_dev(ctx, tensors, rate, step, beta1=0.9, beta2=0.99, eps=1e-7, norm=norm, max_norm=0.3, status=status)
+        assert int(step) == k and int(status) == 0
+        check_step(host, before, dev, lr, k, decay, o.clip_factor(o.grad_norm(host), 0.3), 0.9, 0.99, 1e-7, weights)
+        for i, g in enumerate(grads):
+            g.mul_(-0.5)
+            host[i] = -0.5 * host[i]
