@@ -119,3 +119,23 @@ def test_the_branch_gradient_needs_no_branch_without_a_post_norm_and_a_gate(vd, 
     mag = backward_magnitudes(t, pre, "none", 1.0, 0.5, st64, r64)
     close(dx, want["dx"], mag["dx"], K_ROW, "dx")
     close(df, want["df"], mag["df"], K_ROW, "df")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("B,n,d", [(2, 5, 3), (3, 700, 40), (2, 333, 128), (4, 90, 321), (2, 41, 1100), (1, 9, 8192)])
+def test_results_may_overwrite_the_other_input(vd, ctx, B, n, d, dtype):
+    """r over f and h over x, dx over dh and df over dr, as in buffers of their own."""
+    t = make(6, B, n, d, dtype, dtype, "layer", "rms", "window")
+    dev = on_device(t, dtype, dtype)
+    kw = dict(pre=vd.NORM_LAYER, post=vd.NORM_RMS, w=dev["w"], wp=dev["wp"], bp=dev["bp"], gate=dev["gate"], alpha=0.9, beta=-0.5)
+    r, h, stats = vd.vardrop_block_norm_fwd(ctx, dev["x"], dev["f"], b=dev["b"], **kw)
+    grads = vd.vardrop_block_norm_bwd(ctx, dev["dr"], dev["dh"], r, dev["f"], stats, bias_grads=True, **kw)
+    x, f, st = dev["x"].clone(), dev["f"].clone(), torch.empty_like(stats)
+    vd.vardrop_block_norm_fwd(ctx, x, f, b=dev["b"], out=(f, x, st), **kw)
+    assert torch.equal(f, r) and torch.equal(x, h) and torch.equal(st, stats)
+    dr, dh = dev["dr"].clone(), dev["dh"].clone()
+    vectors = tuple(torch.empty_like(g) for g in grads[2:])
+    ws = torch.empty(vd.vardrop_block_norm_workspace_bytes(B, n, d, B), dtype=torch.uint8, device="cuda")
+    vd.vardrop_block_norm_bwd(ctx, dr, dh, r, dev["f"], stats, ws=ws, out=(dh, dr) + vectors, **kw)
+    for a, b in zip((dh, dr) + vectors, grads):
+        assert torch.equal(a, b)
