@@ -617,13 +617,14 @@ def vardrop_block_norm_fwd(ctx, x, f=None, pre=NORM_LAYER, w=None, b=None, post=
                                         and gate.get_device() == dev else _refuse("gate", gate, gates * d, dt))
     p_stats = None if stats is None else (stats.data_ptr() if stats.dtype is fp32 and stats.numel() == 4 * rows and stats.is_contiguous()
                                           and stats.get_device() == dev else _refuse("stats", stats, 4 * rows, fp32))
-    args = (post, p_wp, p_bp, p_gate, gates, alpha, beta, pre, p_w, p_b, eps, p_r, p_h, p_stats, _device_stream(dev, stream))
+    on = _device_stream(dev, stream)
     if n_dev is None:
-        rc = ctx._lib.vardrop_block_norm_fwd(ctx.handle, p_x, p_f, B, n, d, _CODES.get(res, -1), _CODES.get(dt, -1), *args)
+        rc = ctx._lib.vardrop_block_norm_fwd(ctx.handle, p_x, p_f, B, n, d, _CODES.get(res, -1), _CODES.get(dt, -1), post, p_wp, p_bp, p_gate,
+                                             gates, alpha, beta, pre, p_w, p_b, eps, p_r, p_h, p_stats, on)
     else:
         rc = ctx._lib.vardrop_block_norm_fwd_dev(ctx.handle, p_x, p_f, B, _scalar("n_dev", n_dev, torch.int32, dev), n,
-                                                 _scalar("status", status, torch.int32, dev), d, _CODES.get(res, -1),
-                                                 _CODES.get(dt, -1), *args)
+                                                 _scalar("status", status, torch.int32, dev), d, _CODES.get(res, -1), _CODES.get(dt, -1), post,
+                                                 p_wp, p_bp, p_gate, gates, alpha, beta, pre, p_w, p_b, eps, p_r, p_h, p_stats, on)
     if rc:
         ctx.check(rc, "vardrop_block_norm_fwd")
     return r, h, stats
@@ -696,15 +697,16 @@ def vardrop_block_norm_bwd(ctx, dr, dh, r, f, stats, pre=NORM_LAYER, w=None, pos
         ws = torch.empty(vardrop_block_norm_workspace_bytes(B, n, d, gates), dtype=torch.uint8, device=like.device)
     if ws is not None and not (ws.is_contiguous() and ws.get_device() == dev):
         raise TypeError("ws must be contiguous, on device %d" % dev)
-    tokens = (p_dr, p_dh, p_r, p_f, p_stats)
-    args = (post, p_wp, p_bp, p_gate, gates, alpha, beta, pre, p_w, p_dx, p_df, p_dw, p_db, p_dwp, p_dbp, p_dgate, _p(ws),
-            0 if ws is None else ws.numel(), _device_stream(dev, stream))
+    p_ws, room, on = _p(ws), 0 if ws is None else ws.numel(), _device_stream(dev, stream)
     if n_dev is None:
-        rc = ctx._lib.vardrop_block_norm_bwd(ctx.handle, *tokens, B, n, d, _CODES.get(res, -1), _CODES.get(dt, -1), *args)
+        rc = ctx._lib.vardrop_block_norm_bwd(ctx.handle, p_dr, p_dh, p_r, p_f, p_stats, B, n, d, _CODES.get(res, -1), _CODES.get(dt, -1), post,
+                                             p_wp, p_bp, p_gate, gates, alpha, beta, pre, p_w, p_dx, p_df, p_dw, p_db, p_dwp, p_dbp, p_dgate,
+                                             p_ws, room, on)
     else:
-        rc = ctx._lib.vardrop_block_norm_bwd_dev(ctx.handle, *tokens, B, _scalar("n_dev", n_dev, torch.int32, dev), n,
-                                                 _scalar("status", status, torch.int32, dev), d, _CODES.get(res, -1),
-                                                 _CODES.get(dt, -1), *args)
+        rc = ctx._lib.vardrop_block_norm_bwd_dev(ctx.handle, p_dr, p_dh, p_r, p_f, p_stats, B, _scalar("n_dev", n_dev, torch.int32, dev), n,
+                                                 _scalar("status", status, torch.int32, dev), d, _CODES.get(res, -1), _CODES.get(dt, -1), post,
+                                                 p_wp, p_bp, p_gate, gates, alpha, beta, pre, p_w, p_dx, p_df, p_dw, p_db, p_dwp, p_dbp, p_dgate,
+                                                 p_ws, room, on)
     if rc:
         ctx.check(rc, "vardrop_block_norm_bwd")
     return dx, df, dw, db, dwp, dbp, dgate
