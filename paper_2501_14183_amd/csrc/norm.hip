@@ -183,7 +183,7 @@ template <int LPR> __device__ inline int first_group() {
 }
 template <int LPR> __device__ inline int sub_group() { return LPR < 64 ? (int)(threadIdx.x % 64) / LPR : 0; }
 
-// A row has LPR lanes, the least that keeps 16 elements or fewer a lane; a group of lanes takes one row or several, the next one on its way
+// A row has LPR lanes of 4 to 16 elements each (shape_of); a group of lanes takes one row or several, the next one on its way
 // while this one is worked on.  Everything a row needs is asked for at once.  27 584 rows of 512 with a fp32 residual, norms on both sides and a
 // gate for each window 27-28 us (6.1 TB/s; 46 with each vector asked for when it was needed), 2080 rows of 512 bf16 4.6 us (launch and one round
 // of loads).  The statistics are taken from fp32 values before r is rounded, deviations about the mean.
@@ -298,8 +298,10 @@ __global__ __launch_bounds__(threads_of<LPR>()) void block_norm_fwd_kernel(NormA
 }
 
 // Rows of one segment (the tokens of a gate row) in `pieces` ranges, one workgroup each; its groups walk the range in
-// turn and keep their column sums in registers, the next row on its way while this one is worked on.  65 536 rows of 768 bf16, everything on, 120 us
-// (5.0 TB/s; a large copy reaches 5.1 on this card), 2784 of 512 7.6 us, 2002 of 2048 fp32 18 us.
+// turn and keep their column sums in registers, the next row on its way while this one is worked on.  65 536 rows of 768 bf16, everything on, 121 us:
+// 5.0 TB/s, as a large copy, but less than the 7.1 that the update of the weights reaches, so that memory is not all that bounds it; two
+// wavefronts a SIMD are what its 172 registers leave.  2784 of 512 7.8 us, 2002 of 2048 fp32 18.4 us.  The instances of fp32 blocks beyond 6144
+// channels, and of bf16 blocks with a fp32 residual whose rows do not fill 512 lanes of 16, keep 4 to 21 registers of a lane in scratch memory.
 template <typename TR, typename TB, int LPR, int CH, End kEnd>
 __global__ __launch_bounds__(threads_of<LPR>()) void block_norm_bwd_kernel(NormArgs a) {
   constexpr int T = threads_of<LPR>(), G = T / LPR;
@@ -449,8 +451,8 @@ __global__ __launch_bounds__(threads_of<LPR>()) void block_norm_bwd_kernel(NormA
 }
 
 // The vector gradients from the pieces' column sums.  A workgroup takes 16 columns (64 bytes of a sum) and 64 pieces at a time, so
-// that it has all it reads under way in one round (6.2 us for 512 pieces of 768 columns and eight gate rows, 18.6 with 64 columns a workgroup
-// and three rounds and more; 4.2 us is the least); blockIdx.y 0: db, dw; 1: dbp, dwp (every piece weighted with its
+// that it has all it reads under way in one round (6.2-7.3 us for 512 pieces of 768 columns and eight gate rows, 18.6 with 64 columns a workgroup
+// and three rounds and more; 4.2 us is the least; the sums are read from memory twice, by different dies); blockIdx.y 0: db, dw; 1: dbp, dwp (every piece weighted with its
 // gate row) and the gradient of a single gate row; 2 + g: gate row g of several.
 constexpr int kVectorCols = 16;
 __device__ inline float to_float(float v) { return v; }
@@ -543,10 +545,14 @@ Shape shape_of(int d) {
 #define VD_NORM_SHAPES(X) \
   X(16, 1) X(32, 1) X(64, 1) X(64, 2) X(64, 3) X(64, 4) X(256, 2) X(256, 3) X(256, 4) X(512, 3) X(512, 4)
 
-// Ranges of rows per segment: two workgroups a compute unit, one for wide rows, whose column sums (32 d bytes a range, written and read
-// again) weigh more; at least eight rows, two for every group of lanes.  Backward with 256 / 512 / 1024 ranges in all, us: 390 625 x 64 bf16 84 / 64 / 68,
-// 97 656 x 256 82 / 64 / 69, 48 828 x 512 64.4 / 65.5 / 67.4, 32 552 x 768 66.8 / 66.4 / 67.0, 24 414 x 1024 67.4 / 67.9 / 68.6, fp32 129 / 127 / 128;
-// 12 207 x 2048 67.5 / 72.1 / 81.9, 6103 x 4096 71.8 / 81.7 / 89.9; 2784 x 512 with 174, 348, 696 ranges 15.8 / 14.8 / 17.0 (an earlier kernel).
+// Ranges of rows per segment: 512 over all segments, 256 for rows wider than 1024, whose column sums (32 d bytes a range, written and read
+// again) weigh more; rounded up in every segment (five gate rows have 515), and no more than one for eight rows or two for every group of
+// lanes (9 rows have two).  512 are two workgroups a compute unit where registers allow them: fp32 of 769 to 1024 and of 3073 to 4096
+// channels, and ragged widths of these with a fp32 residual alone, have one.  Both launches with 256 / 512 / 1024 ranges, us: 390 625 x 64 bf16 84 /
+// 65 / 68, 97 656 x 256 82 / 64 / 69, 77 881 x 321 86 / 78 / 79, 48 828 x 512 64.1 / 65.9 / 67.7, 39 062 x 640 69.7 / 67.2 / 67.2 (with eight gate rows
+// 67.9 / 73.4 / 69.6), 24 414 x 1024 67.6 / 68.0 / 69.2, fp32 126 / 125 / 127; 12 207 x 2048 67.6 / 70.2 / 77.7, 6103 x 4096 70.5 / 78.2 / 84.4, fp32
+// 131 / 136 / 141.  Few rows: 6016 x 512 15.0 / 15.8 / 17.6; 2784 x 512 with 128 / 256 / 348 ranges 13.7 / 11.7 / 12.2, x 1024 17.6 / 15.6 / 16.7, fp32
+// 19.3 / 19.0 / 22.0; 2002 x 2048 fp32 with 64 / 128 / 252 39.9 / 27.9 / 24.7.
 int pieces_of(int B, int n, int d, int gates) {
   const int segments = gates > 1 ? gates : 1;
   const Shape s = shape_of(d);
@@ -660,6 +666,7 @@ int backward(vardrop_ctx* ctx, const void* dr, const void* dh, const void* r, co
   if (!vd_aligned(stats, 16) || !aligned_to(res_dtype, dr, r, dx) || !aligned_to(dtype, dh, f, df, w, wp, bp, gate) ||
       !aligned_to(VARDROP_F32, dw, db, dwp, dbp, dgate))
     return VARDROP_EINVAL;
+  // (f is read wherever it is given, also where neither a post norm nor a gate's gradient needs it: a sixth of the bytes there)
   const bool vectors = dw || db || dwp || dbp || dgate;
   if ((long long)B * n == 0 && !vectors) return VARDROP_OK;
   const size_t need = vardrop_block_norm_workspace_bytes(B, n, d, gates);
