@@ -9,7 +9,9 @@
  *      backward                                               (vardrop_attn_fwd / _bwd).
  * What turns that block into a layer that trains comes with it: the norms before and after a block with its gate and
  * residual scale (vardrop_block_norm_fwd / _bwd), the global norm and clipping of all gradients (vardrop_grad_norm,
- * vardrop_clip_grads) and the update of the weights (vardrop_adamw).
+ * vardrop_clip_grads) and the update of the weights (vardrop_adamw).  The layer's other half is the feed-forward block
+ * (vardrop_ffn_fwd / _bwd), whose activations wait for the backward pass in 8 bits (vardrop_pack8); a model that answers multiplies
+ * in 8-bit integers (vardrop_linear_i8).
  *
  * General rules
  *   - Every pointer is a DEVICE pointer owned by the caller unless its name ends in
@@ -56,7 +58,8 @@ enum {
   VARDROP_EUNSUPPORTED = -4  /* valid request outside what the kernels implement         */
 };
 
-enum { VARDROP_F32 = 0, VARDROP_BF16 = 1 };   /* element type of tokens / weights */
+enum { VARDROP_F32 = 0, VARDROP_BF16 = 1, VARDROP_I8 = 2 };   /* element type of tokens / weights (I8: vardrop_linear_i8 only) */
+enum { VARDROP_ACT_NONE = 0, VARDROP_ACT_RELU = 1, VARDROP_ACT_GELU = 2 };   /* activation; GELU is x Phi(x) */
 
 /* Creates a context on HIP device `device_id` (allocates a 2 MiB cosine / sine table there).
  * Synchronous. */
@@ -107,6 +110,17 @@ enum {
   VARDROP_K_GRAD_NORM,       /* global norm of a tensor list's gradients                    */
   VARDROP_K_CLIP,            /* gradients scaled to a norm                                  */
   VARDROP_K_ADAMW,           /* AdamW step of a tensor list                                 */
+  VARDROP_K_PACK8,           /* an activation into 8 bits                                   */
+  VARDROP_K_UNPACK8,         /* and back                                                    */
+  VARDROP_K_FFN_UP,          /* act(x W1 + b1), and x W1 + b1 in 8 bits                     */
+  VARDROP_K_FFN_DOWN,        /* y = a W2 + b2                                               */
+  VARDROP_K_FFN_DH,          /* (dy W2^T) act'(h)                                           */
+  VARDROP_K_FFN_DX,          /* dx = dh W1^T                                                */
+  VARDROP_K_FFN_WEIGHTS,     /* dW1, dW2 (K slices)                                         */
+  VARDROP_K_FFN_ACT,         /* fp32: activation, its checkpoint and its gradient           */
+  VARDROP_K_FFN_BIAS,        /* column sums of dh and dy                                    */
+  VARDROP_K_QUANTIZE,        /* rows or weights as 8-bit integers                           */
+  VARDROP_K_LINEAR_I8,       /* product of 8-bit integers                                   */
   VARDROP_K_COUNT
 };
 int vardrop_profile_select(vardrop_ctx* ctx, int kernel_id);
@@ -499,6 +513,91 @@ int vardrop_adamw(vardrop_ctx* ctx, const vardrop_tensor_list* list, double lr, 
 int vardrop_adamw_dev(vardrop_ctx* ctx, const vardrop_tensor_list* list, const float* lr_dev, double beta1, double beta2,
                       double eps, int64_t* step_dev, int advance, const float* norm, float max_norm,
                       int32_t* status, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * Activations in 8 bits: what the backward pass needs of a forward pass, put away in 33/32 bytes an element.
+ *
+ *   x      [B][n][d], element type `dtype`
+ *   saved  vardrop_pack8_bytes(B, n, d), a multiple of 256, 256-byte aligned: a signed byte for every element, and an exponent byte for
+ *          every block of 32 channels of a row (the last may be shorter).  An element stands for its byte times a power of two, the
+ *          smallest (of at least 2^-126) with which the block's largest magnitude is, rounded, at most 127 steps; ties to even.  So it
+ *          is off by at most half a step, 2^-7 of the block's largest, and what it stands for is a bf16 number.  A block with an
+ *          infinity or NaN comes back as NaN; magnitudes from 127.5 * 2^121 on as 127 * 2^121.
+ * vardrop_unpack8 writes what `saved` stands for; its `dtype` need not be that of the tensor packed.  Rows need element alignment
+ * only; d <= 2^20, B*n < 2^31 (EUNSUPPORTED above).  B*n == 0 is a no-op.  The _dev forms read n on the device (see the general rules);
+ * the same n_max has to be given to the size query and both calls.
+ */
+size_t vardrop_pack8_bytes(int B, int n, int d);
+int vardrop_pack8(vardrop_ctx* ctx, const void* x, int B, int n, int d, int dtype, void* saved, void* stream);
+int vardrop_unpack8(vardrop_ctx* ctx, const void* saved, int B, int n, int d, int dtype, void* x, void* stream);
+int vardrop_pack8_dev(vardrop_ctx* ctx, const void* x, int B, const int32_t* n_dev, int n_max, int32_t* status, int d, int dtype,
+                      void* saved, void* stream);
+int vardrop_unpack8_dev(vardrop_ctx* ctx, const void* saved, int B, const int32_t* n_dev, int n_max, int32_t* status, int d, int dtype,
+                        void* x, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * The feed-forward block -- the other half of an encoder layer of the backbone (Sec. 4.1), beside the attention above:
+ *
+ *   h = x W1 + b1,  y = act(h) W2 + b2                        act: VARDROP_ACT_RELU or VARDROP_ACT_GELU
+ *   backward, with x' and h' what the checkpoints of x and h stand for:
+ *   dh = (dy W2^T) act'(h'),  dx = dh W1^T,  dW1 = x'^T dh,  db1 = sum dh,  dW2 = act(h')^T dy,  db2 = sum dy
+ *
+ *   x, y, dy, dx     [B][n][d], element type `dtype`
+ *   W1 [d][f], W2 [f][d] row-major, `dtype`; biases b1 [f], b2 [d], `dtype`, NULL = none
+ *   saved            vardrop_ffn_saved_bytes: the checkpoint of x, as vardrop_pack8 writes it, and behind it (at
+ *                    vardrop_pack8_bytes(B, n, d)) that of h [B][n][f]; written by fwd, read by bwd.  NULL in the forward: no backward
+ *                    pass follows, nothing is kept.  (act'(0) = 0 for RELU.)
+ *   dx               NULL = not wanted
+ *   dW1, dW2, db1, db2   element type grad_dtype: VARDROP_F32, or VARDROP_BF16 with VARDROP_BF16 tokens; overwritten; db NULL = skip
+ *   ws               vardrop_ffn_workspace_bytes, 256-byte aligned; forward and backward, and all layers, may share one
+ * VARDROP_BF16 multiplies on the matrix cores with fp32 accumulation (act(h) and dh are rounded to bf16 in between) and requires d and
+ * f multiples of 64 and 16-byte aligned tensors (but db1, db2); VARDROP_F32 multiplies and sums in fp32, at any d and f.  B*n*d, B*n*f and
+ * d*f < 2^31 (EUNSUPPORTED otherwise).  Outputs must not overlap inputs.  B*n == 0 is a no-op (weight gradients zero-filled).  The _dev
+ * forms read n on the device (see the general rules); the same n_max has to be given to the size queries, the forward and the
+ * backward.  Sums run in an order that does not depend on scheduling. */
+size_t vardrop_ffn_saved_bytes(int B, int n, int d, int f);
+size_t vardrop_ffn_workspace_bytes(int B, int n, int d, int f, int dtype);
+int vardrop_ffn_fwd(vardrop_ctx* ctx, const void* x, int B, int n, int d, int f, int dtype, int act,
+                    const void* W1, const void* b1, const void* W2, const void* b2,
+                    void* y, void* saved, void* ws, size_t ws_bytes, void* stream);
+int vardrop_ffn_bwd(vardrop_ctx* ctx, const void* dy, int B, int n, int d, int f, int dtype, int act,
+                    const void* W1, const void* W2, const void* saved,
+                    void* dx, void* dW1, void* dW2, void* db1, void* db2, int grad_dtype,
+                    void* ws, size_t ws_bytes, void* stream);
+int vardrop_ffn_fwd_dev(vardrop_ctx* ctx, const void* x, int B, const int32_t* n_dev, int n_max, int32_t* status,
+                        int d, int f, int dtype, int act,
+                        const void* W1, const void* b1, const void* W2, const void* b2,
+                        void* y, void* saved, void* ws, size_t ws_bytes, void* stream);
+int vardrop_ffn_bwd_dev(vardrop_ctx* ctx, const void* dy, int B, const int32_t* n_dev, int n_max, int32_t* status,
+                        int d, int f, int dtype, int act,
+                        const void* W1, const void* W2, const void* saved,
+                        void* dx, void* dW1, void* dW2, void* db1, void* db2, int grad_dtype,
+                        void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------
+ * Products in 8-bit integers, for a model that answers: a scale for each token and for each output channel.
+ *
+ *   scale_t = max|x_t| / 127,  code = x * (127 / max|x_t|) to the nearest whole number, ties to even     (fp32, a row of x at a time)
+ *   y[t][c] = act(scale_t scale_c sum_k code_t[k] code_c[k] + bias[c])
+ *
+ *   x       [rows][K] of x_dtype VARDROP_F32 or VARDROP_BF16, quantised by the call (codes and scales in `ws`), or VARDROP_I8: codes
+ *           [rows][vardrop_i8_pitch(K)] that vardrop_quantize_rows wrote, 16-byte aligned, with their scales sx fp32 [rows] (several
+ *           products of the same rows then share them).  sx NULL exactly when the call quantises.
+ *   codes   int8 [N][vardrop_i8_pitch(K)], 16-byte aligned, and scale fp32 [N]: a weight W [K][N] (y = x W) as vardrop_quantize_weight
+ *           lays it out, once
+ *   bias    [N], `dtype`, NULL = none;  act any of the three;  y [rows][N], `dtype`
+ *   ws      vardrop_linear_i8_workspace_bytes, 256-byte aligned; not needed with VARDROP_I8
+ * Sums are exact 32-bit integers, scaled in fp32.  A row (or column of W) without a magnitude of 2^-100 or more counts as zeros, one
+ * that holds an infinity or NaN makes its results NaN.  Any K up to 65536 (EUNSUPPORTED above) and any N; x and y need element
+ * alignment only, and must not overlap.  rows == 0 is a no-op.
+ */
+int vardrop_i8_pitch(int K);      /* bytes of a row of codes: K up to a multiple of 128, zeros behind K; 0 when out of range */
+int vardrop_quantize_rows(vardrop_ctx* ctx, const void* x, int rows, int K, int dtype, void* codes, float* scale, void* stream);
+int vardrop_quantize_weight(vardrop_ctx* ctx, const void* W, int K, int N, int dtype, void* codes, float* scale, void* stream);
+size_t vardrop_linear_i8_workspace_bytes(int rows, int K, int N);
+int vardrop_linear_i8(vardrop_ctx* ctx, const void* x, const float* sx, int rows, int K, int N, int x_dtype,
+                      const void* codes, const float* scale, const void* bias, int act, void* y, int dtype,
+                      void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -10,4 +10,7 @@ from .binding import (  # noqa: F401
     vardrop_sample_nearest_noalloc, vardrop_attn_fwd_dev, vardrop_embed_fwd_dev, vardrop_embed_bwd_dev, vardrop_profile_read_all, K_ALL, vardrop_signal_after,
     NORM_LAYER, NORM_NONE, NORM_RMS, TensorList, vardrop_adamw, vardrop_adamw_dev, vardrop_block_norm_bwd, vardrop_block_norm_fwd,
     vardrop_block_norm_workspace_bytes, vardrop_clip_grads, vardrop_grad_norm,
+    ACT_GELU, ACT_NONE, ACT_RELU, I8, vardrop_ffn_bwd, vardrop_ffn_fwd, vardrop_ffn_saved_bytes, vardrop_ffn_workspace_bytes,
+    vardrop_linear_i8, vardrop_linear_i8_workspace_bytes, vardrop_pack8, vardrop_pack8_bytes, vardrop_quantize_rows,
+    vardrop_quantize_weight, vardrop_unpack8,
 )

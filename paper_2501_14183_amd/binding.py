@@ -11,6 +11,10 @@ import torch
 
 F32 = 0
 BF16 = 1
+I8 = 2
+ACT_NONE = 0
+ACT_RELU = 1
+ACT_GELU = 2
 NORM_NONE = 0
 NORM_LAYER = 1
 NORM_RMS = 2
@@ -29,6 +33,9 @@ _ptr = ctypes.c_void_p
 # post, wp, bp, gate, gates, alpha, beta, pre, w, then b, eps, r, h, stats or the gradients and the workspace; stream
 _BLOCK_NORM_FWD = [_c_int, _ptr, _ptr, _ptr, _c_int, _c_float, _c_float, _c_int, _ptr] + [_ptr, _c_float] + [_ptr] * 4
 _BLOCK_NORM_BWD = [_c_int, _ptr, _ptr, _ptr, _c_int, _c_float, _c_float, _c_int, _ptr] + [_ptr] * 8 + [_c_size, _ptr]
+# d, f, dtype, act, W1, then b1, W2, b2, y, saved or W2, saved, five gradients and their type; workspace, stream
+_FFN_FWD = [_c_int] * 4 + [_ptr] * 6 + [_ptr, _c_size, _ptr]
+_FFN_BWD = [_c_int] * 4 + [_ptr] * 8 + [_c_int] + [_ptr, _c_size, _ptr]
 
 _SIGNATURES = {
     "vardrop_create": (_c_int, [ctypes.POINTER(_ptr), _c_int]),
@@ -94,6 +101,23 @@ _SIGNATURES = {
     "vardrop_grad_norm": (_c_int, [_ptr, _ptr, _ptr, _ptr]),
     "vardrop_clip_grads": (_c_int, [_ptr, _ptr, _ptr, _c_float, _ptr, _ptr]),
     "vardrop_adamw": (_c_int, [_ptr, _ptr, _c_double, _c_double, _c_double, _c_double, _c_i64, _ptr, _c_float, _ptr, _ptr]),
+    "vardrop_pack8_bytes": (_c_size, [_c_int] * 3),
+    "vardrop_pack8": (_c_int, [_ptr, _ptr, _c_int, _c_int, _c_int, _c_int, _ptr, _ptr]),
+    "vardrop_unpack8": (_c_int, [_ptr, _ptr, _c_int, _c_int, _c_int, _c_int, _ptr, _ptr]),
+    "vardrop_pack8_dev": (_c_int, [_ptr, _ptr, _c_int, _ptr, _c_int, _ptr, _c_int, _c_int, _ptr, _ptr]),
+    "vardrop_unpack8_dev": (_c_int, [_ptr, _ptr, _c_int, _ptr, _c_int, _ptr, _c_int, _c_int, _ptr, _ptr]),
+    "vardrop_ffn_saved_bytes": (_c_size, [_c_int] * 4),
+    "vardrop_ffn_workspace_bytes": (_c_size, [_c_int] * 5),
+    "vardrop_ffn_fwd": (_c_int, [_ptr, _ptr, _c_int, _c_int] + _FFN_FWD),
+    "vardrop_ffn_fwd_dev": (_c_int, [_ptr, _ptr, _c_int, _ptr, _c_int, _ptr] + _FFN_FWD),
+    "vardrop_ffn_bwd": (_c_int, [_ptr, _ptr, _c_int, _c_int] + _FFN_BWD),
+    "vardrop_ffn_bwd_dev": (_c_int, [_ptr, _ptr, _c_int, _ptr, _c_int, _ptr] + _FFN_BWD),
+    "vardrop_i8_pitch": (_c_int, [_c_int]),
+    "vardrop_quantize_rows": (_c_int, [_ptr, _ptr, _c_int, _c_int, _c_int, _ptr, _ptr, _ptr]),
+    "vardrop_quantize_weight": (_c_int, [_ptr, _ptr, _c_int, _c_int, _c_int, _ptr, _ptr, _ptr]),
+    "vardrop_linear_i8_workspace_bytes": (_c_size, [_c_int] * 3),
+    "vardrop_linear_i8": (_c_int, [_ptr, _ptr, _ptr, _c_int, _c_int, _c_int, _c_int, _ptr, _ptr, _ptr, _c_int, _ptr, _c_int,
+                                   _ptr, _c_size, _ptr]),
     "vardrop_adamw_dev": (_c_int, [_ptr, _ptr, _ptr, _c_double, _c_double, _c_double, _ptr, _c_int, _ptr, _c_float, _ptr, _ptr]),
 }
 
@@ -825,3 +849,235 @@ def vardrop_adamw_dev(ctx, tensors, lr_dev, step_dev, beta1=0.9, beta2=0.999, ep
                                     _scalar("status", status, torch.int32, tensors.device), _device_stream(tensors.device, stream))
     if rc:
         ctx.check(rc, "vardrop_adamw_dev")
+
+
+# ---------------------------------------------------------------- activations in 8 bits, feed-forward block, 8-bit products
+def _tensor(name, t, numel, dtype, dev):
+    """Address of a contiguous tensor on device `dev` (None: not given)."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.numel() == numel and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
+    _refuse(name, t, numel, dtype)
+
+
+def _bytes(name, t, least, dev):
+    """Address of a byte buffer of at least `least` bytes on device `dev`."""
+    if t.dtype is torch.uint8 and t.numel() >= least and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
+    raise TypeError("%s must be contiguous uint8, of %d bytes at least, on device %d: got %s %s on %s"
+                    % (name, least, dev, t.dtype, list(t.shape), t.device))
+
+
+def _room(nbytes, device):
+    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+
+
+def vardrop_pack8_bytes(B, n, d):
+    """Bytes of an 8-bit checkpoint of a [B, n, d] tensor (a multiple of 256)."""
+    return load_library().vardrop_pack8_bytes(B, n, d)
+
+
+def vardrop_pack8(ctx, x, out=None, stream=None, n_dev=None, status=None):
+    """x [B, n, d] in 8 bits: 33/32 bytes an element -> uint8 buffer (`out` when given; 256-byte aligned).
+
+    n_dev (int32 [1] on the device): x is a buffer for x.shape[1] tokens that holds [B, N', d] packed."""
+    B, n, d = x.shape
+    dev, need = x.get_device(), ctx._lib.vardrop_pack8_bytes(B, n, d)
+    on = _device_stream(dev, stream)
+    if out is None:
+        _own_buffers(stream, "vardrop_pack8", out=out)
+        out = _room(need, x.device)
+    p_x, p_out = _tensor("x", x, B * n * d, x.dtype, dev), _bytes("out", out, need, dev)
+    if n_dev is None:
+        rc = ctx._lib.vardrop_pack8(ctx.handle, p_x, B, n, d, _CODES.get(x.dtype, -1), p_out, on)
+    else:
+        rc = ctx._lib.vardrop_pack8_dev(ctx.handle, p_x, B, _scalar("n_dev", n_dev, torch.int32, dev), n,
+                                        _scalar("status", status, torch.int32, dev), d, _CODES.get(x.dtype, -1), p_out, on)
+    if rc:
+        ctx.check(rc, "vardrop_pack8")
+    return out
+
+
+def vardrop_unpack8(ctx, saved, out, stream=None, n_dev=None, status=None):
+    """What the checkpoint `saved` of vardrop_pack8 stands for, into out [B, n, d] (float32 or bfloat16)."""
+    B, n, d = out.shape
+    dev = out.get_device()
+    on = _device_stream(dev, stream)
+    p_out, p_saved = _tensor("out", out, B * n * d, out.dtype, dev), _bytes("saved", saved, ctx._lib.vardrop_pack8_bytes(B, n, d), dev)
+    if n_dev is None:
+        rc = ctx._lib.vardrop_unpack8(ctx.handle, p_saved, B, n, d, _CODES.get(out.dtype, -1), p_out, on)
+    else:
+        rc = ctx._lib.vardrop_unpack8_dev(ctx.handle, p_saved, B, _scalar("n_dev", n_dev, torch.int32, dev), n,
+                                          _scalar("status", status, torch.int32, dev), d, _CODES.get(out.dtype, -1), p_out, on)
+    if rc:
+        ctx.check(rc, "vardrop_unpack8")
+    return out
+
+
+def vardrop_ffn_saved_bytes(B, n, d, f):
+    """Bytes of what vardrop_ffn_fwd keeps for the backward: the checkpoints of x [B, n, d] and of x W1 + b1 [B, n, f]."""
+    return load_library().vardrop_ffn_saved_bytes(B, n, d, f)
+
+
+def vardrop_ffn_workspace_bytes(B, n, d, f, dtype):
+    """Bytes of the workspace of vardrop_ffn_fwd and vardrop_ffn_bwd for tokens of a torch dtype."""
+    return load_library().vardrop_ffn_workspace_bytes(B, n, d, f, _CODES.get(dtype, -1))
+
+
+def _ffn_weights(W1, W2, d, dt, dev):
+    if W1.dim() != 2 or W1.shape[0] != d:
+        raise TypeError("W1 must be [d, f] for tokens of d = %d channels: got %s" % (d, list(W1.shape)))
+    f = W1.shape[1]
+    if W2.dim() != 2 or W2.shape[0] != f or W2.shape[1] != d:
+        raise TypeError("W2 must be [%d, %d]: got %s" % (f, d, list(W2.shape)))
+    return f, _tensor("W1", W1, d * f, dt, dev), _tensor("W2", W2, d * f, dt, dev)
+
+
+def vardrop_ffn_fwd(ctx, x, W1, W2, b1=None, b2=None, act=ACT_GELU, train=True, saved=None, ws=None, out=None, stream=None, n_dev=None,
+                    status=None):
+    """y = act(x W1 + b1) W2 + b2 for x [B, n, d], W1 [d, f], W2 [f, d] -> (y, saved).
+
+    saved: uint8 buffer for the backward, x and x W1 + b1 in 8 bits (made when missing; with train=False nothing is kept and it is
+    None).  ws: uint8 workspace, free again once the call's work is done.  n_dev: as in vardrop_pack8."""
+    B, n, d = x.shape
+    dt, dev = x.dtype, x.get_device()
+    on = _device_stream(dev, stream)
+    f, p_W1, p_W2 = _ffn_weights(W1, W2, d, dt, dev)
+    code = _CODES.get(dt, -1)
+    need, room = ctx._lib.vardrop_ffn_saved_bytes(B, n, d, f), ctx._lib.vardrop_ffn_workspace_bytes(B, n, d, f, code)
+    if not train and saved is not None:
+        raise TypeError("saved is for train=True")
+    if out is None or ws is None or (train and saved is None):
+        _own_buffers(stream, "vardrop_ffn_fwd", out=out, ws=ws, **({"saved": saved} if train else {}))
+        out = torch.empty_like(x) if out is None else out
+        ws = _room(room, x.device) if ws is None else ws
+        saved = _room(need, x.device) if train and saved is None else saved
+    p_x, p_y = _tensor("x", x, B * n * d, dt, dev), _tensor("out", out, B * n * d, dt, dev)
+    p_b1, p_b2 = _tensor("b1", b1, f, dt, dev), _tensor("b2", b2, d, dt, dev)
+    p_saved = None if saved is None else _bytes("saved", saved, need, dev)
+    p_ws = _bytes("ws", ws, 0, dev)
+    if n_dev is None:
+        rc = ctx._lib.vardrop_ffn_fwd(ctx.handle, p_x, B, n, d, f, code, act, p_W1, p_b1, p_W2, p_b2, p_y, p_saved, p_ws, ws.numel(), on)
+    else:
+        rc = ctx._lib.vardrop_ffn_fwd_dev(ctx.handle, p_x, B, _scalar("n_dev", n_dev, torch.int32, dev), n,
+                                          _scalar("status", status, torch.int32, dev), d, f, code, act, p_W1, p_b1, p_W2, p_b2, p_y, p_saved,
+                                          p_ws, ws.numel(), on)
+    if rc:
+        ctx.check(rc, "vardrop_ffn_fwd")
+    return out, saved
+
+
+def vardrop_ffn_bwd(ctx, dy, W1, W2, saved, act=ACT_GELU, bias_grads=False, grad_dtype=torch.float32, ws=None, out=None, stream=None,
+                    n_dev=None, status=None):
+    """Gradients of vardrop_ffn_fwd from dy [B, n, d] and what it saved -> (dx, dW1, dW2, db1, db2).
+
+    dx in dy's type, the others in grad_dtype (float32, or bfloat16 beside bfloat16 tokens); db1 and db2 with bias_grads.  `out`, when
+    given, is that tuple of preallocated tensors, whose dW1 says the type; dx, db1 and db2 may be None: not wanted."""
+    B, n, d = dy.shape
+    dt, dev = dy.dtype, dy.get_device()
+    on = _device_stream(dev, stream)
+    f, p_W1, p_W2 = _ffn_weights(W1, W2, d, dt, dev)
+    code = _CODES.get(dt, -1)
+    if out is None:
+        _own_buffers(stream, "vardrop_ffn_bwd", out=out)
+
+        def grad(wanted, *shape):
+            return torch.empty(shape, dtype=grad_dtype, device=dy.device) if wanted else None
+
+        out = (torch.empty_like(dy), grad(True, d, f), grad(True, f, d), grad(bias_grads, f), grad(bias_grads, d))
+    dx, dW1, dW2, db1, db2 = out
+    gt = dW1.dtype
+    if ws is None:
+        _own_buffers(stream, "vardrop_ffn_bwd", ws=ws)
+        ws = _room(ctx._lib.vardrop_ffn_workspace_bytes(B, n, d, f, code), dy.device)
+    p_dy, p_dx = _tensor("dy", dy, B * n * d, dt, dev), _tensor("dx", dx, B * n * d, dt, dev)
+    p_dW1, p_dW2 = _tensor("dW1", dW1, d * f, gt, dev), _tensor("dW2", dW2, d * f, gt, dev)
+    p_db1, p_db2 = _tensor("db1", db1, f, gt, dev), _tensor("db2", db2, d, gt, dev)
+    p_saved = _bytes("saved", saved, ctx._lib.vardrop_ffn_saved_bytes(B, n, d, f), dev)
+    p_ws = _bytes("ws", ws, 0, dev)
+    if n_dev is None:
+        rc = ctx._lib.vardrop_ffn_bwd(ctx.handle, p_dy, B, n, d, f, code, act, p_W1, p_W2, p_saved, p_dx, p_dW1, p_dW2, p_db1, p_db2,
+                                      _CODES.get(gt, -1), p_ws, ws.numel(), on)
+    else:
+        rc = ctx._lib.vardrop_ffn_bwd_dev(ctx.handle, p_dy, B, _scalar("n_dev", n_dev, torch.int32, dev), n,
+                                          _scalar("status", status, torch.int32, dev), d, f, code, act, p_W1, p_W2, p_saved, p_dx, p_dW1, p_dW2,
+                                          p_db1, p_db2, _CODES.get(gt, -1), p_ws, ws.numel(), on)
+    if rc:
+        ctx.check(rc, "vardrop_ffn_bwd")
+    return out
+
+
+def vardrop_quantize_rows(ctx, x, out=None, stream=None):
+    """Rows of x [..., K] as 8-bit integers and a scale each -> (codes int8 [rows, pitch], scale float32 [rows]).
+
+    pitch is K up to a multiple of 128, with zeros behind K.  The pair can be given to vardrop_linear_i8 in x's place."""
+    K = x.shape[-1]
+    rows = x.numel() // K if K else 0
+    dev, pitch = x.get_device(), ctx._lib.vardrop_i8_pitch(K)
+    on = _device_stream(dev, stream)
+    if out is None:
+        _own_buffers(stream, "vardrop_quantize_rows", out=out)
+        out = (torch.empty(rows, pitch, dtype=torch.int8, device=x.device), torch.empty(rows, dtype=torch.float32, device=x.device))
+    codes, scale = out
+    rc = ctx._lib.vardrop_quantize_rows(ctx.handle, _tensor("x", x, x.numel(), x.dtype, dev), rows, K, _CODES.get(x.dtype, -1),
+                                        _tensor("codes", codes, rows * pitch, torch.int8, dev), _tensor("scale", scale, rows, torch.float32, dev), on)
+    if rc:
+        ctx.check(rc, "vardrop_quantize_rows")
+    return codes, scale
+
+
+def vardrop_quantize_weight(ctx, W, out=None, stream=None):
+    """A weight W [K, N] (y = x W) laid out for vardrop_linear_i8, once -> (codes int8 [N, pitch], scale float32 [N])."""
+    K, N = W.shape
+    dev, pitch = W.get_device(), ctx._lib.vardrop_i8_pitch(K)
+    on = _device_stream(dev, stream)
+    if out is None:
+        _own_buffers(stream, "vardrop_quantize_weight", out=out)
+        out = (torch.empty(N, pitch, dtype=torch.int8, device=W.device), torch.empty(N, dtype=torch.float32, device=W.device))
+    codes, scale = out
+    rc = ctx._lib.vardrop_quantize_weight(ctx.handle, _tensor("W", W, K * N, W.dtype, dev), K, N, _CODES.get(W.dtype, -1),
+                                          _tensor("codes", codes, N * pitch, torch.int8, dev), _tensor("scale", scale, N, torch.float32, dev), on)
+    if rc:
+        ctx.check(rc, "vardrop_quantize_weight")
+    return codes, scale
+
+
+def vardrop_linear_i8_workspace_bytes(rows, K, N):
+    """Bytes of the workspace of vardrop_linear_i8 for rows that it quantises itself."""
+    return load_library().vardrop_linear_i8_workspace_bytes(rows, K, N)
+
+
+def vardrop_linear_i8(ctx, x, codes, scale, bias=None, act=ACT_NONE, dtype=None, ws=None, out=None, stream=None):
+    """y = act(x W + bias) from 8-bit integers, with (codes, scale) of W from vardrop_quantize_weight -> y [..., N].
+
+    x [..., K] float32 or bfloat16, or the pair of vardrop_quantize_rows (then y is [rows, N]).  y is of type `dtype`: that of `out`, of
+    the bias or of x where it is not given.  ws: uint8 workspace for rows that the call quantises."""
+    given = isinstance(x, tuple)
+    first = x[0] if given else x
+    dev, N = first.get_device(), scale.numel()
+    on = _device_stream(dev, stream)
+    K = first.shape[-1]
+    pitch = ctx._lib.vardrop_i8_pitch(K)
+    rows = first.numel() // K if K else 0
+    if codes.dim() != 2 or codes.shape[1] != pitch:
+        raise TypeError("codes must be [N, %d] for rows of %d: got %s" % (pitch, K, list(codes.shape)))
+    if dtype is None:
+        dtype = out.dtype if out is not None else bias.dtype if bias is not None else torch.bfloat16 if given else x.dtype
+    if out is None:
+        _own_buffers(stream, "vardrop_linear_i8", out=out)
+        out = torch.empty((rows, N) if given else (*x.shape[:-1], N), dtype=dtype, device=first.device)
+    if ws is None and not given:
+        _own_buffers(stream, "vardrop_linear_i8", ws=ws)
+        ws = _room(ctx._lib.vardrop_linear_i8_workspace_bytes(rows, K, N), first.device)
+    if given:
+        p_x, p_sx, code = _tensor("x", first, rows * pitch, torch.int8, dev), _tensor("sx", x[1], rows, torch.float32, dev), I8
+    else:
+        p_x, p_sx, code = _tensor("x", x, rows * K, x.dtype, dev), None, _CODES.get(x.dtype, -1)
+    rc = ctx._lib.vardrop_linear_i8(ctx.handle, p_x, p_sx, rows, K, N, code, _tensor("codes", codes, N * pitch, torch.int8, dev),
+                                    _tensor("scale", scale, N, torch.float32, dev), _tensor("bias", bias, N, dtype, dev), act,
+                                    _tensor("out", out, rows * N, dtype, dev), _CODES.get(dtype, -1),
+                                    None if ws is None else _bytes("ws", ws, 0, dev), 0 if ws is None else ws.numel(), on)
+    if rc:
+        ctx.check(rc, "vardrop_linear_i8")
+    return out

@@ -1,0 +1,148 @@
+// The format of an activation in 8 bits, and the activations of the feed-forward block: device helpers of pack8.hip, ffn.hip and
+// int8.hip.
+//
+// A row is cut into blocks of 32 channels.  A block has one exponent byte E and a signed byte for each channel, which stands for
+// code * 2^(E - 127): the step is the smallest power of two (of at least 2^-126) of which the block's largest magnitude is, rounded,
+// at most 127 steps, and a code is the nearest whole number, ties to even.  A power of two, and not the largest value over 127,
+// because code * step then is a bf16 number: what the backward pass multiplies is the checkpoint itself, with no rounding of its
+// own.  It costs half a bit on average: a value is off by at most half a step, 2^-7 of the block's largest.  A block that holds an
+// infinity or NaN has E = 255 and stands for NaN.  Magnitudes from 127.5 * 2^121 on count as 127 * 2^121.
+#ifndef VARDROP_PACK8_H
+#define VARDROP_PACK8_H
+#include "bf16_mfma.h"
+
+namespace {
+
+constexpr int kPackBlock = 32;
+__host__ __device__ inline int pack_blocks(int d) { return (d + kPackBlock - 1) / kPackBlock; }
+// Codes [rows][d], then exponents [rows][blocks].
+__host__ __device__ inline size_t pack_exponents_at(long long rows, int d) { return vd_align_up((size_t)rows * d, 256); }
+inline size_t pack_bytes(long long rows, int d) { return pack_exponents_at(rows, d) + vd_align_up((size_t)rows * pack_blocks(d), 256); }
+
+__device__ inline uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// E of a block whose largest magnitude has these bits (127.5 / 64 is the mantissa that 0x10000 carries into the exponent)
+__device__ inline uint32_t pack_exponent(uint32_t most) {
+  if (most >= 0x7f800000u) return 255u;
+  const uint32_t e = (most + 0x10000u) >> 23;
+  return min(max(e, 7u) - 6u, 248u);
+}
+__device__ inline float pack_up(uint32_t e) { return __uint_as_float((254u - min(e, 253u)) << 23); }
+__device__ inline float pack_step(uint32_t e) { return __uint_as_float(e == 255u ? 0x7fc00000u : e << 23); }
+// Code of v in the low byte: 1.5 * 2^23 has steps of one, and the product with a power of two is exact.
+__device__ inline uint32_t pack_code(float v, float up) {
+  return __float_as_uint(__builtin_amdgcn_fmed3f(v * up, -127.f, 127.f) + 12582912.f);
+}
+__device__ inline uint32_t pack_four(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x0c0c0400u), hi = __builtin_amdgcn_perm(d, c, 0x0c0c0400u);
+  return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+}
+// Codes of eight neighbouring values; the four lanes of a block come together, `e` is the block's.
+__device__ inline u32x2 pack_eight(const float (&v)[8], uint32_t& e) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[i]));
+  most = max(most, (uint32_t)__builtin_amdgcn_mov_dpp((int)most, 0xb1, 0xf, 0xf, true));      // lanes ^ 1
+  most = max(most, (uint32_t)__builtin_amdgcn_mov_dpp((int)most, 0x4e, 0xf, 0xf, true));      // lanes ^ 2
+  e = pack_exponent(most);
+  const float up = pack_up(e);
+  uint32_t c[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c[i] = pack_code(v[i], up);
+  return u32x2{pack_four(c[0], c[1], c[2], c[3]), pack_four(c[4], c[5], c[6], c[7])};
+}
+// Values of four codes (one conversion with sign extension and one product each)
+__device__ inline void unpack_four(uint32_t w, float step, float* v) {
+  v[0] = (float)(int8_t)w * step;
+  v[1] = (float)(int8_t)(w >> 8) * step;
+  v[2] = (float)(int8_t)(w >> 16) * step;
+  v[3] = (float)((int)w >> 24) * step;
+}
+__device__ inline void unpack_eight(u32x2 codes, uint32_t e, float (&v)[8]) {
+  const float step = pack_step(e);
+  unpack_four(codes.x, step, v);
+  unpack_four(codes.y, step, v + 4);
+}
+
+// ---- GELU(x) = x Phi(x), and its derivative Phi(x) + x phi(x)
+// Upper tail Q(|x|) of the normal distribution and phi(x) sqrt(2 pi): Abramowitz and Stegun, Handbook of Mathematical Functions,
+// 7.1.26 (erf to 1.5e-7), whose exponential the derivative needs as well.  For results in bf16.
+__device__ inline float normal_tail(float x, float& bell) {
+  const float z = fabsf(x) * 0.70710678118f;
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, z, 1.f));
+  bell = fast_exp2(z * z * -1.44269504089f);
+  const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  return 0.5f * p * bell;
+}
+enum { kActNone = VARDROP_ACT_NONE, kActRelu = VARDROP_ACT_RELU, kActGelu = VARDROP_ACT_GELU };
+// `exact`: with the library's erf, for fp32 results
+template <int ACT, bool EXACT>
+__device__ inline float act_value(float x) {
+  if constexpr (ACT == kActNone) return x;
+  if constexpr (ACT == kActRelu) return x < 0.f ? 0.f : x;              // (NaN stays)
+  if constexpr (EXACT) return x * 0.5f * erfcf(x * -0.70710678118654752f);
+  float bell;
+  const float q = normal_tail(x, bell);
+  return x * (x < 0.f ? q : 1.f - q);
+}
+// value and derivative
+template <int ACT, bool EXACT>
+__device__ inline float act_both(float x, float& slope) {
+  if constexpr (ACT == kActRelu) {
+    slope = x > 0.f ? 1.f : (x <= 0.f ? 0.f : x);
+    return x < 0.f ? 0.f : x;
+  }
+  float below, bell;
+  if constexpr (EXACT) {
+    below = 0.5f * erfcf(x * -0.70710678118654752f);
+    bell = expf(-0.5f * x * x);
+  } else {
+    const float q = normal_tail(x, bell);
+    below = x < 0.f ? q : 1.f - q;
+  }
+  slope = fmaf(x * 0.39894228040f, bell, below);
+  return x * below;
+}
+
+// eight neighbouring elements
+template <typename T> __device__ inline void load_eight(const T* p, float (&v)[8]);
+template <> __device__ inline void load_eight<bf16_t>(const bf16_t* p, float (&v)[8]) {
+  const u32x4 q = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    v[2 * w] = __uint_as_float(q[w] << 16);
+    v[2 * w + 1] = __uint_as_float(q[w] & 0xffff0000u);
+  }
+}
+template <> __device__ inline void load_eight<float>(const float* p, float (&v)[8]) {
+  const u32x4 a = reinterpret_cast<const u32x4*>(p)[0], b = reinterpret_cast<const u32x4*>(p)[1];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    v[w] = __uint_as_float(a[w]);
+    v[4 + w] = __uint_as_float(b[w]);
+  }
+}
+__device__ inline u32x4 eight_bf16(const float (&v)[8]) {
+  return u32x4{pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
+}
+__device__ inline void store_eight(bf16_t* p, const float (&v)[8]) { *reinterpret_cast<u32x4*>(p) = eight_bf16(v); }
+__device__ inline void store_eight(float* p, const float (&v)[8]) {
+  reinterpret_cast<u32x4*>(p)[0] = u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+  reinterpret_cast<u32x4*>(p)[1] = u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])};
+}
+__device__ inline float to_float(bf16_t v) { return bf2f(v); }
+__device__ inline float to_float(float v) { return v; }
+__device__ inline void from_float(bf16_t* p, float v) { *p = f2bf(v); }
+__device__ inline void from_float(float* p, float v) { *p = v; }
+
+}  // namespace
+
+// ---- element-wise passes (pack8.hip); rows = B * n, or with dn.dev B times what it holds (at most n).  Null pointers: not wanted
+// codes and exponents of x, and act(x) into `a` (which may be x), both of `dtype`; act VARDROP_ACT_NONE with a = nullptr: codes only
+int vd_pack8(vardrop_ctx*, int kid, const void* x, int B, int n, int d, int dtype, int act, void* codes, void* exps, void* a, hipStream_t s,
+             VdDevCount dn);
+// values of a checkpoint into x
+int vd_unpack8(vardrop_ctx*, int kid, const void* codes, const void* exps, int B, int n, int d, int dtype, void* x, hipStream_t s, VdDevCount dn);
+// dh = da * act'(h), a = act(h) with h from its checkpoint (fp32); dh may be da
+int vd_act_bwd_f32(vardrop_ctx*, int kid, const float* da, const void* codes, const void* exps, int B, int n, int d, int act, float* dh, float* a,
+                   hipStream_t s, VdDevCount dn);
+#endif  // VARDROP_PACK8_H

@@ -1,0 +1,271 @@
+"""The feed-forward block (vardrop_ffn_fwd / vardrop_ffn_bwd) against the fp64 oracle; bounds in util_ffn.py.
+
+The backward is compared from what its checkpoints stand for, which the oracle takes as exact."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import feedforward as o
+from util_ffn import assert_within, backward_bounds, forward_bounds, make
+from util_gpu import to_dev, torch_dtype
+
+pytestmark = pytest.mark.gpu
+NAMES = ("dx", "dW1", "dW2", "db1", "db2")
+
+
+@pytest.fixture(scope="module")
+def vd():
+    import paper_2501_14183_amd as m
+    return m
+
+
+@pytest.fixture(scope="module")
+def ctx(vd):
+    return vd.Context(0)
+
+
+def kind(vd, act):
+    return {"relu": vd.ACT_RELU, "gelu": vd.ACT_GELU}[act]
+
+
+def behind(t, extra=4096):
+    """A copy of t with NaN in the memory behind it."""
+    room = torch.full((t.numel() + extra,), float("nan"), dtype=t.dtype, device="cuda")
+    room[:t.numel()].copy_(t.reshape(-1))
+    return room[:t.numel()].view(t.shape)
+
+
+def on_device(t, B, n, dtype):
+    dt = torch_dtype(dtype)
+    up = {k: None if v is None else behind(to_dev(v, dt)) for k, v in t.items()}
+    for k in ("x", "dy"):
+        up[k] = up[k].view(B, n, -1)
+    return up
+
+
+def kept(vd, ctx, saved, B, n, d, f):
+    """x and h that a checkpoint stands for, fp64."""
+    first = vd.vardrop_pack8_bytes(B, n, d)
+    x = vd.vardrop_unpack8(ctx, saved[:first], torch.empty(B, n, d, device="cuda"))
+    h = vd.vardrop_unpack8(ctx, saved[first:], torch.empty(B, n, f, device="cuda"))
+    return x.double().cpu().numpy().reshape(B * n, d), h.double().cpu().numpy().reshape(B * n, f)
+
+
+def check(vd, ctx, B, n, d, f, dtype, act, bias=True, grad="fp32", seed=0):
+    t = make(seed, B, n, d, f, dtype, bias)
+    g = on_device(t, B, n, dtype)
+    y, saved = vd.vardrop_ffn_fwd(ctx, g["x"], g["W1"], g["W2"], g["b1"], g["b2"], act=kind(vd, act))
+    want, bound, h, eh = forward_bounds(t, dtype, act)
+    assert_within("y", y, want, bound)
+    again, none = vd.vardrop_ffn_fwd(ctx, g["x"], g["W1"], g["W2"], g["b1"], g["b2"], act=kind(vd, act), train=False)
+    assert none is None and torch.equal(again, y)
+    kx, kh = kept(vd, ctx, saved, B, n, d, f)
+    assert np.array_equal(kx, o.through_8_bits(t["x"]))
+    # half a step of the block's largest, whose own error may move the step by a factor of two
+    most = np.maximum.reduceat(np.abs(h) + eh, np.arange(0, f, 32), axis=1)
+    assert (np.abs(kh - h) <= eh + np.repeat(most, 32, axis=1)[:, :f] * 2.0 ** -7 * 1.005).all()
+    out = vd.vardrop_ffn_bwd(ctx, g["dy"], g["W1"], g["W2"], saved, act=kind(vd, act), bias_grads=True, grad_dtype=torch_dtype(grad))
+    want = backward_bounds(t, kx, kh, dtype, act, grad)
+    for name, got in zip(NAMES, out):
+        assert_within(name, got, *want[name])
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu"])
+@pytest.mark.parametrize("B,n,d,f", [(1, 1, 64, 64), (1, 2, 64, 192), (2, 31, 128, 64), (1, 63, 192, 320), (1, 64, 64, 128), (1, 65, 128, 128), (3, 43, 64, 448),
+                                     (1, 127, 320, 64), (4, 32, 256, 512), (1, 129, 576, 192), (7, 100, 320, 832), (2, 701, 64, 128)])
+def test_bf16(vd, ctx, B, n, d, f, act):
+    check(vd, ctx, B, n, d, f, "bf16", act)
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu"])
+@pytest.mark.parametrize("B,n,d,f", [(1, 1, 1, 1), (1, 1, 64, 128), (4, 10, 64, 128), (2, 33, 50, 97), (1, 65, 96, 31), (3, 111, 321, 65), (1, 600, 128, 256)])
+def test_fp32(vd, ctx, B, n, d, f, act):
+    check(vd, ctx, B, n, d, f, "fp32", act)
+
+
+@pytest.mark.parametrize("B,n,d,f", [(1, 17, 64, 128), (2, 600, 128, 192)])
+def test_without_biases_and_with_gradients_in_bf16(vd, ctx, B, n, d, f):
+    check(vd, ctx, B, n, d, f, "bf16", "gelu", bias=False, grad="bf16")
+
+
+@pytest.mark.parametrize("B,n,d,f", [(8, 1100, 256, 512), (16, 1024, 512, 128), (9, 1000, 64, 1088)])
+def test_many_tokens(vd, ctx, B, n, d, f):
+    """Large tiles, several slices of the weight gradients."""
+    check(vd, ctx, B, n, d, f, "bf16", "gelu", grad="bf16")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_results_repeat(vd, ctx, dtype):
+    g = on_device(make(3, 2, 1500, 128, 256, dtype), 2, 1500, dtype)
+    runs = []
+    for _ in range(3):
+        saved = torch.zeros(vd.vardrop_ffn_saved_bytes(2, 1500, 128, 256), dtype=torch.uint8, device="cuda")
+        y, _ = vd.vardrop_ffn_fwd(ctx, g["x"], g["W1"], g["W2"], g["b1"], g["b2"], saved=saved)
+        runs.append((y, saved, *vd.vardrop_ffn_bwd(ctx, g["dy"], g["W1"], g["W2"], saved, bias_grads=True)))
+    for other in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(runs[0], other))
+
+
+def test_gradients_are_differences(vd, ctx):
+    """fp32, at an x and h that 8 bits hold exactly (whole sixteenths below 4, W1 of whole numbers), so that the checkpoints are the forward's."""
+    rng = np.random.default_rng(5)
+    T, d, f = 6, 32, 32
+    x, W1 = rng.integers(-15, 16, (T, d)) / 16, np.eye(d)[rng.permutation(d)] * 2.0
+    p = dict(x=x, W1=W1, W2=rng.standard_normal((f, d)) / 4, b1=np.zeros(f), b2=rng.standard_normal(d) / 4)
+    dy = rng.standard_normal((T, d))
+    dev = lambda a: to_dev(a.astype(np.float32))
+
+    def forward(q):
+        return vd.vardrop_ffn_fwd(ctx, dev(q["x"]).view(1, T, d), dev(q["W1"]), dev(q["W2"]), dev(q["b1"]), dev(q["b2"]))
+
+    saved = forward(p)[1]
+    got = dict(zip(NAMES, vd.vardrop_ffn_bwd(ctx, dev(dy).view(1, T, d), dev(p["W1"]), dev(p["W2"]), saved, bias_grads=True)))
+    step = 2.0 ** -7
+    for name in p:
+        for _ in range(4):
+            way = rng.standard_normal(p[name].shape)
+            way = np.round(way * 2 ** 10) / 2 ** 10                  # (every point of the difference is an fp32 number)
+            hi, lo = (dict(p, **{name: p[name] + s * step * way}) for s in (1, -1))
+            diff = ((forward(hi)[0].double() - forward(lo)[0].double()).cpu().numpy().reshape(T, d) * dy).sum() / (2 * step)
+            mine = (got["d" + name].double().cpu().numpy().reshape(way.shape) * way).sum()
+            # third derivatives are below 2 for GELU: step^2 / 6 of it along `way`, cubed, and fp32's own error over the step
+            size = np.abs(dy).sum() * (np.abs(way).max() ** 3 * 8 * step ** 2 / 3 * np.abs(p["W2"]).sum(0).max() + 2e-6 / step)
+            assert abs(diff - mine) <= size, (name, diff, mine, size)
+            assert abs(diff - mine) <= 2e-2 * np.abs(way).max() ** 3 * np.sqrt((got["d" + name].double() ** 2).sum().item()) + 1e-2, (name, diff, mine)
+
+
+@pytest.mark.parametrize("dtype,d,f", [("bf16", 64, 128), ("fp32", 50, 70)])
+def test_a_count_on_the_device(vd, ctx, dtype, d, f):
+    B, n_max = 3, 200
+    dt = torch_dtype(dtype)
+    ws = torch.zeros(vd.vardrop_ffn_workspace_bytes(B, n_max, d, f, dt), dtype=torch.uint8, device="cuda")
+    for n in (200, 0, 1, 77, 128, 201):
+        good = 0 <= n <= n_max
+        rows = B * n if good else 0
+        t = make(n, B, n_max, d, f, dtype)
+        g = on_device(t, B, n_max, dtype)
+        for k in ("x", "dy"):                                      # rows behind the last: not to be read
+            g[k].view(-1, d)[rows:] = float("nan")
+        n_dev, status = torch.tensor([n], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        saved = torch.full((vd.vardrop_ffn_saved_bytes(B, n_max, d, f),), 0xFF, dtype=torch.uint8, device="cuda")
+        ws.fill_(0xFF)                                             # NaN in every type
+        y = torch.full((B, n_max, d), 5.0, dtype=dt, device="cuda")
+        vd.vardrop_ffn_fwd(ctx, g["x"], g["W1"], g["W2"], g["b1"], g["b2"], saved=saved, ws=ws, out=y, n_dev=n_dev, status=status)
+        assert int(status) == (0 if good else 1)
+        assert bool((y.view(-1, d)[rows:] == 5.0).all())
+        grads = (torch.full((B, n_max, d), 5.0, dtype=dt, device="cuda"), *[torch.full(s, 5.0, device="cuda") for s in ((d, f), (f, d), (f,), (d,))])
+        status.zero_()
+        ws.fill_(0xFF)
+        vd.vardrop_ffn_bwd(ctx, g["dy"], g["W1"], g["W2"], saved, ws=ws, out=grads, n_dev=n_dev, status=status)
+        assert int(status) == (0 if good else 1)
+        assert bool((grads[0].view(-1, d)[rows:] == 5.0).all())
+        if not good:
+            assert all(bool((t == 5.0).all()) for t in grads)
+            continue
+        live = {k: v[:rows] if k in ("x", "dy") else v for k, v in t.items()}
+        want, bound, h, _ = forward_bounds(live, dtype, "gelu")
+        assert_within("y", y.view(-1, d)[:rows], want, bound)
+        saved_h = saved[vd.vardrop_pack8_bytes(B, n_max, d):]
+        out = torch.zeros(B, n_max, f, device="cuda")
+        kh = vd.vardrop_unpack8(ctx, saved_h, out, n_dev=n_dev).double().cpu().numpy().reshape(-1, f)[:rows]
+        want = backward_bounds(live, o.through_8_bits(live["x"]), kh, dtype, "gelu")
+        for name, got in zip(NAMES, grads):
+            assert_within(name, got.view(-1, d)[:rows] if name == "dx" else got, *want[name])
+
+
+def test_no_tokens(vd, ctx):
+    for dt in (torch.bfloat16, torch.float32):
+        W1, W2 = torch.ones(64, 128, dtype=dt, device="cuda"), torch.ones(128, 64, dtype=dt, device="cuda")
+        x = torch.zeros(2, 0, 64, dtype=dt, device="cuda")
+        y, saved = vd.vardrop_ffn_fwd(ctx, x, W1, W2)
+        out = (None, *[torch.full(s, 5.0, device="cuda") for s in ((64, 128), (128, 64), (128,), (64,))])
+        vd.vardrop_ffn_bwd(ctx, x, W1, W2, saved, out=out)
+        assert y.numel() == 0 and all(not t.any() for t in out[1:])
+
+
+def test_what_is_not_finite_stays_in_its_tokens(vd, ctx):
+    t = make(1, 1, 200, 64, 128, "bf16")
+    g = on_device(t, 1, 200, "bf16")
+    g["x"][0, 7, 3], g["x"][0, 130, 5] = float("nan"), float("inf")
+    y, saved = vd.vardrop_ffn_fwd(ctx, g["x"], g["W1"], g["W2"], g["b1"], g["b2"])
+    bad = ~torch.isfinite(y).all(-1)[0]
+    assert bad.nonzero().flatten().tolist() == [7, 130]
+    dx, dW1, _, _, db2 = vd.vardrop_ffn_bwd(ctx, g["dy"], g["W1"], g["W2"], saved, bias_grads=True)
+    assert (~torch.isfinite(dx).all(-1)[0]).nonzero().flatten().tolist() == [7, 130]
+    assert not torch.isfinite(dW1).any() or torch.isnan(dW1).any()
+    assert bool(torch.isfinite(db2).all())
+
+
+def test_a_graph_of_both_ways(vd, ctx):
+    """Recorded, with a count on the device that changes between the replays, beside eager work on the same tensors."""
+    B, n_max, d, f = 2, 300, 64, 192
+    g = on_device(make(2, B, n_max, d, f, "bf16"), B, n_max, "bf16")
+    n_dev = torch.tensor([300], dtype=torch.int32, device="cuda")
+
+    def buffers():
+        return dict(saved=torch.zeros(vd.vardrop_ffn_saved_bytes(B, n_max, d, f), dtype=torch.uint8, device="cuda"),
+                    ws=torch.zeros(vd.vardrop_ffn_workspace_bytes(B, n_max, d, f, torch.bfloat16), dtype=torch.uint8, device="cuda"),
+                    y=torch.zeros(B, n_max, d, dtype=torch.bfloat16, device="cuda"),
+                    grads=(torch.zeros(B, n_max, d, dtype=torch.bfloat16, device="cuda"),
+                           *[torch.zeros(s, device="cuda") for s in ((d, f), (f, d), (f,), (d,))]))
+
+    def step(b):
+        vd.vardrop_ffn_fwd(ctx, g["x"], g["W1"], g["W2"], g["b1"], g["b2"], saved=b["saved"], ws=b["ws"], out=b["y"], n_dev=n_dev)
+        vd.vardrop_ffn_bwd(ctx, g["dy"], g["W1"], g["W2"], b["saved"], ws=b["ws"], out=b["grads"], n_dev=n_dev)
+
+    recorded, eager = buffers(), buffers()
+    step(recorded)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(recorded)
+    for n in (300, 17, 0, 299):
+        n_dev.fill_(n)
+        graph.replay()
+        step(eager)
+        torch.cuda.synchronize()
+        assert torch.equal(recorded["y"].view(-1, d)[:B * n], eager["y"].view(-1, d)[:B * n])
+        assert all(torch.equal(a, b) for a, b in zip(recorded["grads"][1:], eager["grads"][1:]))
+
+
+def test_another_stream(vd, ctx):
+    g = on_device(make(4, 2, 333, 128, 128, "bf16"), 2, 333, "bf16")
+    saved, saved2 = torch.zeros(2, vd.vardrop_ffn_saved_bytes(2, 333, 128, 128), dtype=torch.uint8, device="cuda")
+    y, _ = vd.vardrop_ffn_fwd(ctx, g["x"], g["W1"], g["W2"], g["b1"], g["b2"], saved=saved)
+    grads = vd.vardrop_ffn_bwd(ctx, g["dy"], g["W1"], g["W2"], saved)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        y2, _ = vd.vardrop_ffn_fwd(ctx, g["x"], g["W1"], g["W2"], g["b1"], g["b2"], saved=saved2)
+        grads2 = vd.vardrop_ffn_bwd(ctx, g["dy"], g["W1"], g["W2"], saved2)
+    side.synchronize()
+    assert torch.equal(y, y2) and torch.equal(saved, saved2)
+    assert all(torch.equal(a, b) for a, b in zip(grads[:3], grads2[:3]))
+
+
+def test_refusals(vd, ctx):
+    bf, f32 = torch.bfloat16, torch.float32
+    x, W1, W2 = (torch.zeros(*s, dtype=bf, device="cuda") for s in ((1, 4, 64), (64, 128), (128, 64)))
+    y, saved = vd.vardrop_ffn_fwd(ctx, x, W1, W2)
+    z = lambda *s, dt=bf: torch.zeros(*s, dtype=dt, device="cuda")
+    ws = z(vd.vardrop_ffn_workspace_bytes(1, 4, 64, 128, bf) + 256, dt=torch.uint8)
+    grads = lambda dt=f32, d=64, f=128: (z(1, 4, d), z(d, f, dt=dt), z(f, d, dt=dt), None, None)
+    wide = z(5 * 64 + 1)
+    calls = [
+        lambda: vd.vardrop_ffn_fwd(ctx, x, W1, W2, act=vd.ACT_NONE), lambda: vd.vardrop_ffn_fwd(ctx, x, W1, W2, act=7),
+        lambda: vd.vardrop_ffn_fwd(ctx, x, W1.float(), W2), lambda: vd.vardrop_ffn_fwd(ctx, x, W2, W1), lambda: vd.vardrop_ffn_fwd(ctx, x, W1, W2.t()),
+        lambda: vd.vardrop_ffn_fwd(ctx, x.half(), W1.half(), W2.half()), lambda: vd.vardrop_ffn_fwd(ctx, x, W1, W2, b1=z(64)),
+        lambda: vd.vardrop_ffn_fwd(ctx, x, W1, W2, out=x), lambda: vd.vardrop_ffn_fwd(ctx, x, W1, W2, ws=ws[:-512]),
+        lambda: vd.vardrop_ffn_fwd(ctx, x, W1, W2, ws=ws[1:]), lambda: vd.vardrop_ffn_fwd(ctx, x, W1, W2, saved=saved[:-1]),
+        lambda: vd.vardrop_ffn_fwd(ctx, z(1, 4, 72), z(72, 128), z(128, 72)), lambda: vd.vardrop_ffn_fwd(ctx, x, z(64, 100), z(100, 64)),
+        lambda: vd.vardrop_ffn_fwd(ctx, wide[1:257].view(1, 4, 64), W1, W2), lambda: vd.vardrop_ffn_fwd(ctx, x, W1, W2, stream=0),
+        lambda: vd.vardrop_ffn_fwd(ctx, x, W1, W2, train=False, saved=saved), lambda: vd.vardrop_ffn_fwd(ctx, x.cpu(), W1.cpu(), W2.cpu()),
+        lambda: vd.vardrop_ffn_bwd(ctx, x, W1, W2, saved[:-1]), lambda: vd.vardrop_ffn_bwd(ctx, x, W1, W2, saved, act=vd.ACT_NONE),
+        lambda: vd.vardrop_ffn_bwd(ctx, x, W1, W2, saved, out=(x, *grads()[1:])), lambda: vd.vardrop_ffn_bwd(ctx, x, W1, W2, saved, out=(None, None, *grads()[2:])),
+        lambda: vd.vardrop_ffn_bwd(ctx, x, W1, W2, saved, grad_dtype=torch.float16), lambda: vd.vardrop_ffn_bwd(ctx, x, W1, W2, saved, ws=ws[:-512]),
+        lambda: vd.vardrop_ffn_bwd(ctx, x.float(), W1.float(), W2.float(), saved, grad_dtype=bf),
+    ]
+    for k, call in enumerate(calls):
+        with pytest.raises((TypeError, AttributeError, vd.VarDropError)):
+            call()
+            pytest.fail("call %d was taken" % k)
