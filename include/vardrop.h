@@ -115,10 +115,9 @@ enum {
   VARDROP_K_FFN_UP,          /* act(x W1 + b1), and x W1 + b1 in 8 bits                     */
   VARDROP_K_FFN_DOWN,        /* y = a W2 + b2                                               */
   VARDROP_K_FFN_DH,          /* (dy W2^T) act'(h)                                           */
-  VARDROP_K_FFN_DX,          /* dx = dh W1^T                                                */
-  VARDROP_K_FFN_WEIGHTS,     /* dW1, dW2 (K slices)                                         */
+  VARDROP_K_FFN_GRADS,       /* dx, dW1, dW2 (K slices)                                     */
   VARDROP_K_FFN_ACT,         /* fp32: activation, its checkpoint and its gradient           */
-  VARDROP_K_FFN_BIAS,        /* column sums of dh and dy                                    */
+  VARDROP_K_FFN_BIAS,        /* fp32: column sums of dh and dy                              */
   VARDROP_K_QUANTIZE,        /* rows or weights as 8-bit integers                           */
   VARDROP_K_LINEAR_I8,       /* product of 8-bit integers                                   */
   VARDROP_K_COUNT

@@ -28,6 +28,7 @@ struct EpiOut {              // C = sums + bias, bf16
   } a;
   float b[8];
   __device__ void columns(int n, int N) { bias_eight(a.bias, n, N, b); }
+  __device__ void done(int, int, bool) {}
   __device__ void row(int, int m, int n, bool live, float (&v)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += b[e];
@@ -45,6 +46,7 @@ struct EpiAct {              // h = sums + bias, packed with KEEP; a = act(h)
   } a;
   float b[8];
   __device__ void columns(int n, int N) { bias_eight(a.bias, n, N, b); }
+  __device__ void done(int, int, bool) {}
   __device__ void row(int, int m, int n, bool live, float (&v)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += b[e];
@@ -63,14 +65,19 @@ struct EpiAct {              // h = sums + bias, packed with KEEP; a = act(h)
   }
 };
 
-template <int ACT>
-struct EpiActBwd {           // sums = da; dh = da act'(h'), a = act(h')
+template <int ACT, int NJ>
+struct EpiActBwd {           // sums = da; dh = da act'(h'), a = act(h'); column sums of dh over a wavefront's rows
   struct Args {
     bf16_t *dh, *act;
     const uint8_t *codes, *exps;
+    float* sums;             // [bands][N], null: not wanted
     int N;
   } a;
-  __device__ void columns(int, int) {}
+  float c[8];
+  __device__ void columns(int, int) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c[e] = 0.f;
+  }
   __device__ void row(int, int m, int n, bool live, float (&v)[8]) {
     if (!live) return;
     const long long at = (long long)m * a.N + n;
@@ -81,9 +88,18 @@ struct EpiActBwd {           // sums = da; dh = da act'(h'), a = act(h')
       float slope;
       h[e] = act_both<ACT, false>(h[e], slope);
       v[e] *= slope;
+      c[e] += v[e];
     }
     store_eight(a.dh + at, v);
     store_eight(a.act + at, h);
+  }
+  __device__ void done(int band, int n, bool live) {
+    if (!a.sums) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int m = 4 * NJ; m < 64; m <<= 1) c[e] += __shfl_xor(c[e], m, 64);
+    if (live && (threadIdx.x & 63) < 4 * NJ) store_eight(a.sums + (long long)band * a.N + n, c);
   }
 };
 
@@ -94,6 +110,7 @@ struct EpiGrad {             // weight gradients: the result in the type of the 
     int M, N, bf16;
   } a;
   __device__ void columns(int, int) {}
+  __device__ void done(int, int, bool) {}
   __device__ void row(int slice, int m, int n, bool live, float (&v)[8]) {
     if (!live) return;
     const long long at = (long long)m * a.N + n;
@@ -103,83 +120,247 @@ struct EpiGrad {             // weight gradients: the result in the type of the 
   }
 };
 
-// ---- column sums of dh and dy: partial sums of a range of rows each (grid: columns / 64, ranges, matrices), rows in order
-constexpr int kColRanges = 64;
-struct ColArgs {
-  const void* src[2];
-  int cols[2];
-  float* part;               // [kColRanges][cols[0] + cols[1]]
-  int B, n, ranges;
+// ---- what else a launch carries: element-wise work in workgroups behind those of the product, which has no need of it
+// x into 8 bits, or x' out of them: groups of eight elements, `pieces` workgroups (d is a multiple of 32)
+struct PieceArgs {
+  const bf16_t* x;
+  bf16_t* values;
+  uint8_t *codes, *exps;
+  int B, n, d, pieces;
   const int32_t* n_dev;
 };
+template <int THREADS, bool PACK>
+__device__ __forceinline__ void piece_8(const PieceArgs& p, int piece) {
+  int n;
+  if (!vd_count(p.n_dev, p.n, n)) return;
+  const long long groups = (long long)p.B * n * (p.d >> 3), step = (long long)p.pieces * THREADS;
+  for (long long i0 = (long long)piece * THREADS + threadIdx.x; i0 < groups; i0 += 4 * step) {
+    float v[4][8];
+    u32x2 c[4];
+    uint32_t e[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const long long i = i0 + u * step;
+      if (i < groups) {
+        if constexpr (PACK) {
+          load_eight(p.x + i * 8, v[u]);
+        } else {
+          c[u] = *reinterpret_cast<const u32x2*>(p.codes + i * 8);
+          e[u] = p.exps[i >> 2];
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const long long i = i0 + u * step;
+      if (i < groups) {                        // (a block's four lanes agree)
+        if constexpr (PACK) {
+          const u32x2 code = pack_eight(v[u], e[u]);
+          *reinterpret_cast<u32x2*>(p.codes + i * 8) = code;
+          if ((i & 3) == 0) p.exps[i >> 2] = (uint8_t)e[u];
+        } else {
+          unpack_eight(c[u], e[u], v[u]);
+          store_eight(p.values + i * 8, v[u]);
+        }
+      }
+    }
+  }
+}
+// Column sums of src [B n][d] over a range of rows for each of `pieces` workgroups: a wavefront takes every WAVES-th row, the sums of the
+// wavefronts are added in order
 template <typename T>
-__global__ __launch_bounds__(256) void ffn_colsum_kernel(ColArgs c) {
+struct ColArgs {
+  const T* src;
+  float* part;                 // [pieces][d]
+  int B, n, d, pieces;
+  const int32_t* n_dev;
+};
+template <int THREADS>
+__device__ __forceinline__ void piece_columns(const ColArgs<bf16_t>& c, int piece) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  float(*red)[64][9] = reinterpret_cast<float(*)[64][9]>(smem);
+  constexpr int W = THREADS / 64;
   int n;
   if (!vd_count(c.n_dev, c.n, n)) return;
-  const bool second = blockIdx.z != 0;
-  const int cols = second ? c.cols[1] : c.cols[0], col = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
-  const T* src = (const T*)(second ? c.src[1] : c.src[0]);
-  if (!src || (int)blockIdx.x * 64 >= cols) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, units = c.d >> 3;
+  const long long rows = (long long)c.B * n, per = (rows + c.pieces - 1) / c.pieces, r0 = piece * per, r1 = min(rows, r0 + per);
+  for (int u0 = 0; u0 < units; u0 += 64) {
+    float s[8] = {};
+    if (u0 + lane < units) {
+      const bf16_t* p = c.src + (u0 + lane) * 8;
+      long long r = r0 + wave;
+      for (; r + 7 * W < r1; r += 8 * W) {
+        u32x4 q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = *reinterpret_cast<const u32x4*>(p + (r + i * W) * c.d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            s[2 * w] += __uint_as_float(q[i][w] << 16);
+            s[2 * w + 1] += __uint_as_float(q[i][w] & 0xffff0000u);
+          }
+      }
+      for (; r < r1; r += W) {
+        float v[8];
+        load_eight(p + r * c.d, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] += v[e];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) red[wave][lane][e] = s[e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 512; i += THREADS) {
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) sum += red[w][i >> 3][i & 7];
+      if (u0 * 8 + i < c.d) c.part[(long long)piece * c.d + u0 * 8 + i] = sum;
+    }
+  }
+}
+
+template <typename S, int ACT, bool KEEP>
+__global__ __launch_bounds__(S::THREADS, S::simd) void ffn_up_kernel(TileArgs g, typename EpiAct<ACT, KEEP>::Args args, PieceArgs p) {
+  const int tiles = gridDim.x - p.pieces;
+  if ((int)blockIdx.x >= tiles) {
+    if constexpr (KEEP) piece_8<S::THREADS, true>(p, blockIdx.x - tiles);
+    return;
+  }
+  int M, K;
+  if (!tile_dims(g, M, K)) return;
+  const int total = (int)tile_count<S>(g, M);
+  if ((int)blockIdx.x < total) tile_gemm<false, true, false, S, EpiAct<ACT, KEEP>>(g, args, M, K, xcd_contiguous(blockIdx.x, total));
+}
+
+template <typename S, int ACT>
+__global__ __launch_bounds__(S::THREADS, S::simd) void ffn_dh_kernel(TileArgs g, typename EpiActBwd<ACT, S::NJ>::Args args, PieceArgs p, ColArgs<bf16_t> c) {
+  const int tiles = gridDim.x - p.pieces - c.pieces;
+  if ((int)blockIdx.x >= tiles) {
+    const int piece = blockIdx.x - tiles;
+    if (piece < p.pieces) piece_8<S::THREADS, false>(p, piece);
+    else piece_columns<S::THREADS>(c, piece - p.pieces);
+    return;
+  }
+  int M, K;
+  if (!tile_dims(g, M, K)) return;
+  const int total = (int)tile_count<S>(g, M);
+  if ((int)blockIdx.x < total) tile_gemm<false, true, true, S, EpiActBwd<ACT, S::NJ>>(g, args, M, K, xcd_contiguous(blockIdx.x, total));
+}
+
+// dx, dW1 and dW2 need the results of the launch before and nothing of each other.  The kind whose tiles are longer comes first; a die takes
+// a contiguous range of either kind.
+template <typename S>
+__global__ __launch_bounds__(S::THREADS, S::simd) void ffn_grads_kernel(TileArgs gx, EpiOut::Args ax, TileArgs g1, EpiGrad::Args a1, TileArgs g2,
+                                                                        EpiGrad::Args a2) {
+  int Mx, Kx, M1, K1, M2, K2;
+  if (!tile_dims(gx, Mx, Kx) || !tile_dims(g1, M1, K1) || !tile_dims(g2, M2, K2)) return;
+  const int nx = gx.A ? (int)tile_count<S>(gx, Mx) : 0, n1 = (int)tile_count<S>(g1, M1), nw = n1 + (int)tile_count<S>(g2, M2);
+  if ((int)blockIdx.x >= nx + nw) return;
+  const bool w_first = K1 / g1.slices > Kx;
+  const int first = w_first ? nw : nx, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
+  const int of_first = (first >> 3) + (xcd < (first & 7) ? 1 : 0), from = xcd_range_start(xcd, first);
+  const bool in_first = slot < of_first;
+  const int t = in_first ? from + slot : xcd_range_start(xcd, nx + nw) - from + (slot - of_first);
+  if (in_first != w_first) tile_gemm<false, true, true, S, EpiOut>(gx, ax, Mx, Kx, t);
+  else if (t < n1) tile_gemm<false, false, false, S, EpiGrad>(g1, a1, M1, K1, t);
+  else tile_gemm<false, false, false, S, EpiGrad>(g2, a2, M2, K2, t - n1);
+}
+
+// ---- fp32: column sums of dh and dy (grid: columns / 64, pieces, matrices), rows in order
+__global__ __launch_bounds__(256) void ffn_columns_f32_kernel(ColArgs<float> c0, ColArgs<float> c1) {
+  const ColArgs<float> c = blockIdx.z ? c1 : c0;
+  int n;
+  if (!c.src || !vd_count(c.n_dev, c.n, n)) return;
+  const int col = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
+  if ((int)blockIdx.x * 64 >= c.d) return;
   __shared__ float red[4][64];
-  const long long rows = (long long)c.B * n, per = (rows + c.ranges - 1) / c.ranges;
+  const long long rows = (long long)c.B * n, per = (rows + c.pieces - 1) / c.pieces;
   const long long r0 = blockIdx.y * per, r1 = min(rows, r0 + per);
   float s = 0.f;
-  if (col < cols) {
+  if (col < c.d) {
     long long r = r0 + wave;
     for (; r + 28 < r1; r += 32) {
       float v[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = to_float(src[(r + 4 * i) * cols + col]);
+      for (int i = 0; i < 8; ++i) v[i] = c.src[(r + 4 * i) * c.d + col];
 #pragma unroll
       for (int i = 0; i < 8; ++i) s += v[i];
     }
-    for (; r < r1; r += 4) s += to_float(src[r * cols + col]);
+    for (; r < r1; r += 4) s += c.src[r * c.d + col];
   }
   red[wave][threadIdx.x & 63] = s;
   __syncthreads();
-  if (wave == 0 && col < cols)
-    c.part[(long long)blockIdx.y * (c.cols[0] + c.cols[1]) + (second ? c.cols[0] : 0) + col] =
-        ((red[0][threadIdx.x] + red[1][threadIdx.x]) + red[2][threadIdx.x]) + red[3][threadIdx.x];
+  if (wave == 0 && col < c.d)
+    c.part[(long long)blockIdx.y * c.d + col] = ((red[0][threadIdx.x] + red[1][threadIdx.x]) + red[2][threadIdx.x]) + red[3][threadIdx.x];
 }
 
-// ---- sums over slices and ranges, in order: dW1, dW2, db1, db2
+// ---- sums over slices and pieces, in an order of their own: dW1, dW2 (four elements a thread), then db1, db2 (16 columns a workgroup, 16
+// threads for each)
 struct FinishArgs {
-  const float* part[2];      // [slices][d f]; null: already there
-  const float* colpart;
+  const float* part[2];        // [slices][count]; null: already there
+  const float* col[2];         // [pieces][cols]; null: not wanted
   void* dW[2];
   void* db[2];
-  int cols[2];
+  int cols[2], pieces[2];
+  int band;                    // rows of a piece of db1 (0: pieces[0] of them whatever the count)
   long long count;
-  int slices, ranges, bf16;
+  int slices, blocks, bf16;    // blocks: workgroups of a weight
   const int32_t* n_dev;
-  int n;
+  int B, n;
 };
-__device__ inline void put(void* p, long long i, float v, int bf16) {
-  if (bf16) ((bf16_t*)p)[i] = f2bf(v);
-  else ((float*)p)[i] = v;
-}
 __global__ __launch_bounds__(256) void ffn_finish_kernel(FinishArgs f) {
   int n;
   if (!vd_count(f.n_dev, f.n, n)) return;
-  const int z = blockIdx.y;
-  const long long step = (long long)gridDim.x * 256;
-  if (z < 2) {
-    const float* p = z ? f.part[1] : f.part[0];
-    if (!p) return;
-    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < f.count; i += step) {
-      float s = 0.f;
-      for (int k = 0; k < f.slices; ++k) s += p[k * f.count + i];
-      put(z ? f.dW[1] : f.dW[0], i, s, f.bf16);
+  const int weights = (f.part[0] ? 2 : 0) * f.blocks;
+  if ((int)blockIdx.x < weights) {
+    const int z = (int)blockIdx.x >= f.blocks;
+    const long long n4 = f.count >> 2;
+    const float4* p = reinterpret_cast<const float4*>(z ? f.part[1] : f.part[0]);
+    void* out = z ? f.dW[1] : f.dW[0];
+    for (long long i = (long long)(blockIdx.x - z * f.blocks) * 256 + threadIdx.x; i < n4; i += (long long)f.blocks * 256) {
+      float4 s = p[i];
+      int k = 1;
+      for (; k + 4 <= f.slices; k += 4) {
+        float4 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = p[(long long)(k + u) * n4 + i];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) { s.x += v[u].x; s.y += v[u].y; s.z += v[u].z; s.w += v[u].w; }
+      }
+      for (; k < f.slices; ++k) {
+        const float4 v = p[(long long)k * n4 + i];
+        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+      }
+      if (f.bf16) reinterpret_cast<u32x2*>(out)[i] = u32x2{pack2(s.x, s.y), pack2(s.z, s.w)};
+      else reinterpret_cast<float4*>(out)[i] = s;
     }
     return;
   }
-  void* db = z == 2 ? f.db[0] : f.db[1];
-  if (!db) return;
-  const int cols = z == 2 ? f.cols[0] : f.cols[1], all = f.cols[0] + f.cols[1];
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < cols; i += step) {
-    float s = 0.f;
-    for (int k = 0; k < f.ranges; ++k) s += f.colpart[(long long)k * all + (z == 2 ? 0 : f.cols[0]) + i];
-    put(db, i, s, f.bf16);
+  __shared__ float red[16][17];
+  const int at = blockIdx.x - weights, b0 = f.col[0] ? (f.cols[0] + 15) / 16 : 0, z = at >= b0;
+  const int c = threadIdx.x & 15, group = threadIdx.x >> 4, cols = z ? f.cols[1] : f.cols[0], column = (at - z * b0) * 16 + c;
+  const float* p = (z ? f.col[1] : f.col[0]) + min(column, cols - 1);
+  const int pieces = z || !f.band ? (z ? f.pieces[1] : f.pieces[0]) : (int)(((long long)f.B * n + f.band - 1) / f.band);
+  float s = 0.f;
+  int k = group;
+  for (; k + 48 < pieces; k += 64) {
+    float v[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v[u] = p[(long long)(k + 16 * u) * cols];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) s += v[u];
+  }
+  for (; k < pieces; k += 16) s += p[(long long)k * cols];
+  red[group][c] = s;
+  __syncthreads();
+  if (group == 0 && column < cols) {
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += red[i][c];
+    void* db = z ? f.db[1] : f.db[0];
+    if (f.bf16) ((bf16_t*)db)[column] = f2bf(s);
+    else ((float*)db)[column] = s;
   }
 }
 
@@ -192,16 +373,78 @@ int check_sizes(int B, int n, int d, int f, int dtype) {
   if (dtype == VARDROP_BF16 && (d % 64 != 0 || f % 64 != 0)) return VARDROP_EUNSUPPORTED;
   return VARDROP_OK;
 }
-// K slices of the two weight gradients: tiles for two workgroups a compute unit, at least 256 tokens each.  Grows with T.
-int grad_slices(long long T, int d, int f) {
-  const long long tiles = 2ll * vd_ceil_div(d, 128) * vd_ceil_div(f, 128);
-  long long s = (512 + tiles - 1) / tiles;
-  if (s > 16) s = 16;
-  if (s > T / 256) s = T / 256;
-  return s < 1 ? 1 : (int)s;
+// ---- plans: which tile, how many slices.  What a tile of BM x BN over K costs beside others of its kind, in products of 32 x 32 x 1 of a
+// chip whose every place is taken; its start and end cost as much as kEnds of K.
+constexpr double kEnds = 200;
+struct ShapeCost {
+  int BM, BN, places;          // places: workgroups that are resident together on 256 compute units
+  double rate;                 // of the largest tile's
+};
+constexpr ShapeCost kShapes[3] = {{64, 128, 512, 0.62}, {128, 128, 512, 0.87}, {256, 256, 256, 1.0}};
+double tile_time(const ShapeCost& c, double K) { return c.BM * c.BN / 1024.0 * (K + kEnds) * c.places / 512.0 / c.rate; }
+long long tiles_of(const ShapeCost& c, long long M, int N) { return (M + c.BM - 1) / c.BM * vd_ceil_div(N, c.BN); }
+int product_shape(long long T, int N, int K) {
+  int best = 0;
+  double least = 0;
+  for (int i = 0; i < 3; ++i) {
+    const long long rounds = (tiles_of(kShapes[i], T, N) + kShapes[i].places - 1) / kShapes[i].places;
+    const double t = rounds * tile_time(kShapes[i], K);
+    if (i == 0 || t < least) {
+      least = t;
+      best = i;
+    }
+  }
+  return best;
 }
+// The launch of dx (T x d over f) and of the weight gradients (2 d f over T in slices): time until the last place is done when the longer
+// tiles come first, and the sum of the slices behind it.
+constexpr int kMostSlices = 16, kLeastSlice = 256;
+struct GradPlan {
+  int shape, slices;
+};
+int most_slices(long long T) {
+  const long long s = T / kLeastSlice;
+  return s < 1 ? 1 : (s > kMostSlices ? kMostSlices : (int)s);
+}
+GradPlan plan_grads(long long T, int d, int f) {
+  GradPlan best = {0, 1};
+  double least = -1;
+  for (int i = 0; i < 3; ++i) {
+    const ShapeCost& c = kShapes[i];
+    const long long nx = tiles_of(c, T, d);
+    for (int s = 1; s <= most_slices(T); ++s) {
+      const long long nw = (tiles_of(c, d, f) + tiles_of(c, f, d)) * s;
+      const double tw = tile_time(c, (double)T / s), tx = tile_time(c, f);
+      const double tl = tw > tx ? tw : tx, ts = tw > tx ? tx : tw;
+      const long long nl = tw > tx ? nw : nx, ns = tw > tx ? nx : nw;
+      const long long full = nl / c.places, rest = nl % c.places;              // `rest` places have a long tile more than the others
+      double end = (full + (rest ? 1 : 0)) * tl;
+      if (ns > 0) {
+        // short tiles fill the places up: level at which all fit
+        double level = (nl * tl + ns * ts) / c.places;
+        long long fit = -1;
+        while (true) {
+          const double over = level - full * tl, under = level - (full + 1) * tl;
+          fit = (c.places - rest) * (long long)(over > 0 ? over / ts + 1e-9 : 0) + rest * (long long)(under > 0 ? under / ts + 1e-9 : 0);
+          if (fit >= ns) break;
+          level += 0.25 * ts;
+        }
+        end = end > level ? end : level;
+      }
+      if (s > 1) end += 2.0 * d * f * s * 2e-4 + 400;                          // (written and read at memory's rate; a launch)
+      if (least < 0 || end < least) {
+        least = end;
+        best = {i, s};
+      }
+    }
+  }
+  return best;
+}
+
+constexpr int kColPieces = 256;
+int column_pieces(long long T) { return T < 64 ? 1 : (T / 32 > kColPieces ? kColPieces : (int)(T / 32)); }
 struct FfnWorkspace {        // bytes from its start
-  size_t wide, act, x, part, second, col, total;
+  size_t wide, act, x, part, second, col, col2, total;
 };
 FfnWorkspace ffn_workspace(long long T, int d, int f, int dtype) {
   const size_t es = dtype == VARDROP_BF16 ? 2 : 4;
@@ -215,10 +458,11 @@ FfnWorkspace ffn_workspace(long long T, int d, int f, int dtype) {
   w.wide = take((size_t)T * f * es);       // a in the forward (fp32: h); dh in the backward
   w.act = take((size_t)T * f * es);        // act(h')
   w.x = take((size_t)T * d * es);          // x'
-  const size_t slices = dtype == VARDROP_BF16 ? grad_slices(T, d, f) : vd_f32_splitk(d, f, 1, T);
+  const size_t slices = dtype == VARDROP_BF16 ? most_slices(T) : vd_f32_splitk(d, f, 1, T);
   w.part = take(slices * d * f * 4);
   w.second = take(slices * d * f * 4);
-  w.col = take((size_t)kColRanges * (d + f) * 4);
+  w.col = take((dtype == VARDROP_BF16 ? (size_t)(T + 63) / 64 * 2 : (size_t)kColPieces) * f * 4);
+  w.col2 = take((size_t)kColPieces * d * 4);
   w.total = at;
   return w;
 }
@@ -231,37 +475,133 @@ struct FfnCall {
   hipStream_t s;
 };
 
-template <bool BKC, typename Epi>
-int product(const FfnCall& c, int kid, const void* A, const void* Bm, int K, int N, const typename Epi::Args& epi, bool status) {
+// C [T][N] = A B, over the tokens
+TileArgs rows_product(const FfnCall& c, const void* A, const void* Bm, bool bkc, int K, int N, bool status) {
   TileArgs g = {};
   g.A = A; g.B = Bm;
-  g.lda = (long long)K * 2; g.ldb = (long long)(BKC ? K : N) * 2;
+  g.lda = (long long)K * 2; g.ldb = (long long)(bkc ? K : N) * 2;
   g.M = (int)c.T; g.N = N; g.K = K; g.slices = 1;
   g.n_dev = c.dn.dev; g.status = status ? c.dn.status : nullptr; g.n_max = c.n; g.n_mul = c.B; g.n_role = 0;
-  const long long t128 = (long long)vd_ceil_div(N, 128) * vd_ceil_div(g.M, 128);
-  if (t128 >= 512) return launch_tile_gemm<false, true, BKC, 128, 2, Epi>(c.ctx, kid, g, epi, c.s);
-  return launch_tile_gemm<false, true, BKC, 64, 3, Epi>(c.ctx, kid, g, epi, c.s);
+  return g;
 }
-// C [M][N] = A^T B over the tokens
-int weight_gradient(const FfnCall& c, const void* A, const void* Bm, int M, int N, int slices, void* C, float* part, int grad_dtype) {
+// C [M][N] = A^T B, summed over the tokens
+TileArgs tokens_product(const FfnCall& c, const void* A, const void* Bm, int M, int N, int slices) {
   TileArgs g = {};
   g.A = A; g.B = Bm;
   g.lda = (long long)M * 2; g.ldb = (long long)N * 2;
   g.M = M; g.N = N; g.K = (int)c.T; g.slices = slices;
   g.n_dev = c.dn.dev; g.n_max = c.n; g.n_mul = c.B; g.n_role = 1;
-  const EpiGrad::Args epi = {C, slices > 1 ? part : nullptr, M, N, grad_dtype == VARDROP_BF16};
-  return launch_tile_gemm<false, false, false, 128, 2, EpiGrad>(c.ctx, VARDROP_K_FFN_WEIGHTS, g, epi, c.s);
+  return g;
+}
+// workgroups for `groups` of eight elements, about four each a thread
+int pieces_8(long long groups, int threads) {
+  const long long p = (groups + threads * 4 - 1) / (threads * 4);
+  return p > 1024 ? 1024 : (int)p;
+}
+
+#define VD_FFN_LAUNCH(KID, KERNEL, S, GRID, ...)                                                     \
+  {                                                                                                  \
+    static int configured = -1;                                                                      \
+    const int rc_ = tile_allow_lds(c.ctx, (const void*)KERNEL, S::lds, configured);                  \
+    if (rc_) return rc_;                                                                             \
+    if ((GRID) >= (1ll << 31)) return VARDROP_EUNSUPPORTED;                                          \
+    VdTimer timer(c.ctx, KID, c.s);                                                                  \
+    VD_KERNEL(c.ctx, (KERNEL), dim3((unsigned)(GRID)), dim3(S::THREADS), S::lds, c.s, __VA_ARGS__);  \
+    VD_LAUNCH_CHECK(c.ctx);                                                                          \
+    return VARDROP_OK;                                                                               \
+  }
+template <typename S, int ACT, bool KEEP>
+int launch_up(const FfnCall& c, const TileArgs& g, const typename EpiAct<ACT, KEEP>::Args& e, PieceArgs p) {
+  p.pieces = KEEP ? pieces_8(c.T * c.d / 8, S::THREADS) : 0;
+  VD_FFN_LAUNCH(VARDROP_K_FFN_UP, (ffn_up_kernel<S, ACT, KEEP>), S, tile_count<S>(g, g.M) + p.pieces, g, e, p)
+}
+template <typename S, int ACT>
+int launch_dh(const FfnCall& c, const TileArgs& g, const typename EpiActBwd<ACT, S::NJ>::Args& e, PieceArgs p, const ColArgs<bf16_t>& col, int* band) {
+  p.pieces = pieces_8(c.T * c.d / 8, S::THREADS);
+  *band = S::MI * 32;
+  VD_FFN_LAUNCH(VARDROP_K_FFN_DH, (ffn_dh_kernel<S, ACT>), S, tile_count<S>(g, g.M) + p.pieces + col.pieces, g, e, p, col)
+}
+template <typename S>
+int launch_grads(const FfnCall& c, const TileArgs& gx, const EpiOut::Args& ax, const TileArgs& g1, const EpiGrad::Args& a1, const TileArgs& g2,
+                 const EpiGrad::Args& a2) {
+  VD_FFN_LAUNCH(VARDROP_K_FFN_GRADS, ffn_grads_kernel<S>, S, (gx.A ? tile_count<S>(gx, gx.M) : 0) + tile_count<S>(g1, g1.M) + tile_count<S>(g2, g2.M), gx, ax, g1,
+                a1, g2, a2)
+}
+#undef VD_FFN_LAUNCH
+// a call of CALL<Tile64>, <Tile128> or <Tile256>
+#define VD_BY_SHAPE(SHAPE, CALL) ((SHAPE) == 0 ? CALL(Tile64) : (SHAPE) == 1 ? CALL(Tile128) : CALL(Tile256))
+
+template <int ACT>
+int fwd_bf16(const FfnCall& c, const void* x, const void* W1, const void* b1, const void* W2, const void* b2, void* y, uint8_t* kept, uint8_t* hc,
+             uint8_t* he, char* ws) {
+  const FfnWorkspace w = ffn_workspace(c.T, c.d, c.f, c.dtype);
+  bf16_t* a = (bf16_t*)(ws + w.wide);
+  PieceArgs p = {};
+  p.x = (const bf16_t*)x; p.codes = kept; p.exps = kept ? kept + pack_exponents_at(c.T, c.d) : nullptr;
+  p.B = c.B; p.n = c.n; p.d = c.d; p.n_dev = c.dn.dev;
+  const TileArgs up = rows_product(c, x, W1, false, c.d, c.f, true);
+  const int shape = product_shape(c.T, c.f, c.d);
+  int rc;
+  if (kept) {
+    const typename EpiAct<ACT, true>::Args e = {a, (const bf16_t*)b1, hc, he, c.f};
+#define VD_CALL(S) launch_up<S, ACT, true>(c, up, e, p)
+    rc = VD_BY_SHAPE(shape, VD_CALL);
+#undef VD_CALL
+  } else {
+    const typename EpiAct<ACT, false>::Args e = {a, (const bf16_t*)b1, nullptr, nullptr, c.f};
+#define VD_CALL(S) launch_up<S, ACT, false>(c, up, e, p)
+    rc = VD_BY_SHAPE(shape, VD_CALL);
+#undef VD_CALL
+  }
+  if (rc) return rc;
+  const TileArgs down = rows_product(c, a, W2, false, c.f, c.d, false);
+  const EpiOut::Args e = {(bf16_t*)y, (const bf16_t*)b2, c.d};
+#define VD_CALL(S) launch_tile_gemm<false, true, false, S, EpiOut>(c.ctx, VARDROP_K_FFN_DOWN, down, e, c.s)
+  return VD_BY_SHAPE(product_shape(c.T, c.d, c.f), VD_CALL);
+#undef VD_CALL
 }
 
 template <int ACT>
-int fwd_bf16(const FfnCall& c, const void* x, const void* W1, const void* b1, const void* W2, const void* b2, void* y, uint8_t* hc, uint8_t* he,
-             char* ws) {
+int bwd_bf16(const FfnCall& c, const void* dy, const void* W1, const void* W2, const uint8_t* saved, void* dx, void* dW1, void* dW2, bool db1, bool db2,
+             int grad_dtype, char* ws, FinishArgs& fin) {
   const FfnWorkspace w = ffn_workspace(c.T, c.d, c.f, c.dtype);
-  const bf16_t* bias = (const bf16_t*)b1;
-  bf16_t* a = (bf16_t*)(ws + w.wide);
-  const int rc = hc ? product<false, EpiAct<ACT, true>>(c, VARDROP_K_FFN_UP, x, W1, c.d, c.f, {a, bias, hc, he, c.f}, true)
-                    : product<false, EpiAct<ACT, false>>(c, VARDROP_K_FFN_UP, x, W1, c.d, c.f, {a, bias, nullptr, nullptr, c.f}, true);
-  return rc ? rc : product<false, EpiOut>(c, VARDROP_K_FFN_DOWN, a, W2, c.f, c.d, {(bf16_t*)y, (const bf16_t*)b2, c.d}, false);
+  const uint8_t* hc = saved + pack_bytes(c.T, c.d);
+  bf16_t *dh = (bf16_t*)(ws + w.wide), *a = (bf16_t*)(ws + w.act), *xv = (bf16_t*)(ws + w.x);
+  float *part = (float*)(ws + w.part), *second = (float*)(ws + w.second), *col = (float*)(ws + w.col), *col2 = (float*)(ws + w.col2);
+  int rc;
+  if (c.T > 0) {
+    PieceArgs p = {};
+    p.values = xv; p.codes = const_cast<uint8_t*>(saved); p.exps = const_cast<uint8_t*>(saved) + pack_exponents_at(c.T, c.d);
+    p.B = c.B; p.n = c.n; p.d = c.d; p.n_dev = c.dn.dev;
+    const ColArgs<bf16_t> cols = {(const bf16_t*)dy, col2, c.B, c.n, c.d, db2 ? column_pieces(c.T) : 0, c.dn.dev};
+    const TileArgs g = rows_product(c, dy, W2, true, c.d, c.f, true);
+    const typename EpiActBwd<ACT, 2>::Args e2 = {dh, a, hc, hc + pack_exponents_at(c.T, c.f), db1 ? col : nullptr, c.f};
+    static_assert(Tile64::NJ == 2 && Tile128::NJ == 2 && Tile256::NJ == 2, "one form of the epilogue");
+#define VD_CALL(S) launch_dh<S, ACT>(c, g, e2, p, cols, &fin.band)
+    rc = VD_BY_SHAPE(product_shape(c.T, c.f, c.d), VD_CALL);
+#undef VD_CALL
+    if (rc) return rc;
+    fin.col[0] = db1 ? col : nullptr;
+    fin.col[1] = db2 ? col2 : nullptr;
+    fin.pieces[1] = cols.pieces;
+  } else {                       // (no tokens: sums over no pieces)
+    fin.col[0] = db1 ? col : nullptr;
+    fin.col[1] = db2 ? col2 : nullptr;
+  }
+  const GradPlan plan = plan_grads(c.T, c.d, c.f);
+  fin.slices = plan.slices;
+  if (plan.slices > 1) {
+    fin.part[0] = part;
+    fin.part[1] = second;
+  }
+  const bool split = plan.slices > 1, low = grad_dtype == VARDROP_BF16;
+  const TileArgs gx = dx && c.T > 0 ? rows_product(c, dh, W1, true, c.f, c.d, false) : TileArgs{};
+  const TileArgs g1 = tokens_product(c, xv, dh, c.d, c.f, plan.slices), g2 = tokens_product(c, a, dy, c.f, c.d, plan.slices);
+  const EpiOut::Args ax = {(bf16_t*)dx, nullptr, c.d};
+  const EpiGrad::Args a1 = {dW1, split ? part : nullptr, c.d, c.f, low}, a2 = {dW2, split ? second : nullptr, c.f, c.d, low};
+#define VD_CALL(S) launch_grads<S>(c, gx, ax, g1, a1, g2, a2)
+  return VD_BY_SHAPE(plan.shape, VD_CALL);
+#undef VD_CALL
 }
 
 int fwd_f32(const FfnCall& c, const float* x, const float* W1, const float* b1, const float* W2, const float* b2, float* y, uint8_t* hc, uint8_t* he,
@@ -282,6 +622,50 @@ int fwd_f32(const FfnCall& c, const float* x, const float* W1, const float* b1, 
   return vd_gemm_f32(c.ctx, VARDROP_K_FFN_DOWN, g, false, c.s);
 }
 
+int bwd_f32(const FfnCall& c, const float* dy, const float* W1, const float* W2, const uint8_t* saved, float* dx, float* dW1, float* dW2, bool db1, bool db2,
+            char* ws, FinishArgs& fin) {
+  const FfnWorkspace w = ffn_workspace(c.T, c.d, c.f, c.dtype);
+  const uint8_t* hc = saved + pack_bytes(c.T, c.d);
+  float *dh = (float*)(ws + w.wide), *a = (float*)(ws + w.act), *xv = (float*)(ws + w.x);
+  const VdDevCount quiet = {c.dn.dev, nullptr};
+  int rc;
+  GemmF32 g = {};
+  g.nz = 1; g.nseg = 1;
+  if (c.T > 0) {
+    if ((rc = vd_unpack8(c.ctx, VARDROP_K_UNPACK8, saved, saved + pack_exponents_at(c.T, c.d), c.B, c.n, c.d, VARDROP_F32, xv, c.s, c.dn))) return rc;
+    g.set(0, dy, W2, dh, nullptr);
+    g.lda = c.d; g.ldb = c.d; g.ldc = c.f; g.M = (int)c.T; g.N = c.f; g.K = c.d;
+    g.count(c.dn, false, c.n, c.B, 0);
+    if ((rc = vd_gemm_f32(c.ctx, VARDROP_K_FFN_DH, g, true, c.s))) return rc;
+    if ((rc = vd_act_bwd_f32(c.ctx, VARDROP_K_FFN_ACT, dh, hc, hc + pack_exponents_at(c.T, c.f), c.B, c.n, c.f, c.act, dh, a, c.s, quiet))) return rc;
+    if (dx) {
+      g.set(0, dh, W1, dx, nullptr);
+      g.lda = c.f; g.ldb = c.f; g.ldc = c.d; g.N = c.d; g.K = c.f;
+      if ((rc = vd_gemm_f32(c.ctx, VARDROP_K_FFN_GRADS, g, true, c.s))) return rc;
+    }
+  }
+  g.count(c.dn, false, c.n, c.B, 1);
+  g.K = (int)c.T;
+  g.set(0, xv, dh, dW1, nullptr);
+  g.lda = c.d; g.ldb = c.f; g.ldc = c.f; g.M = c.d; g.N = c.f; g.part = (float*)(ws + w.part);
+  if ((rc = vd_gemm_f32_wgrad(c.ctx, VARDROP_K_FFN_GRADS, g, c.s))) return rc;
+  g.set(0, a, dy, dW2, nullptr);
+  g.lda = c.f; g.ldb = c.d; g.ldc = c.d; g.M = c.f; g.N = c.d; g.part = (float*)(ws + w.second);
+  if ((rc = vd_gemm_f32_wgrad(c.ctx, VARDROP_K_FFN_GRADS, g, c.s))) return rc;
+  if (!db1 && !db2) return VARDROP_OK;
+  const int pieces = column_pieces(c.T);
+  fin.col[0] = db1 ? (float*)(ws + w.col) : nullptr;
+  fin.col[1] = db2 ? (float*)(ws + w.col2) : nullptr;
+  if (c.T == 0) return VARDROP_OK;       // (sums over no pieces)
+  fin.pieces[0] = fin.pieces[1] = pieces;
+  const ColArgs<float> c0 = {db1 ? dh : nullptr, (float*)(ws + w.col), c.B, c.n, c.f, pieces, c.dn.dev};
+  const ColArgs<float> c1 = {db2 ? dy : nullptr, (float*)(ws + w.col2), c.B, c.n, c.d, pieces, c.dn.dev};
+  VdTimer timer(c.ctx, VARDROP_K_FFN_BIAS, c.s);
+  VD_KERNEL(c.ctx, ffn_columns_f32_kernel, dim3((unsigned)vd_ceil_div(c.d > c.f ? c.d : c.f, 64), (unsigned)pieces, 2), dim3(256), 0, c.s, c0, c1);
+  VD_LAUNCH_CHECK(c.ctx);
+  return VARDROP_OK;
+}
+
 int forward(vardrop_ctx* ctx, const void* x, int B, int n, int d, int f, int dtype, int act, const void* W1, const void* b1, const void* W2,
             const void* b2, void* y, void* saved, void* ws, size_t ws_bytes, hipStream_t s, VdDevCount dn) {
   if (!ctx || !is_act(act)) return VARDROP_EINVAL;
@@ -300,8 +684,9 @@ int forward(vardrop_ctx* ctx, const void* x, int B, int n, int d, int f, int dty
   if (dtype == VARDROP_F32) {
     rc = fwd_f32(c, (const float*)x, (const float*)W1, (const float*)b1, (const float*)W2, (const float*)b2, (float*)y, hc, he, (char*)ws);
   } else {
-    rc = act == VARDROP_ACT_RELU ? fwd_bf16<kActRelu>(c, x, W1, b1, W2, b2, y, hc, he, (char*)ws)
-                                 : fwd_bf16<kActGelu>(c, x, W1, b1, W2, b2, y, hc, he, (char*)ws);
+    uint8_t* kept = (uint8_t*)saved;
+    return act == VARDROP_ACT_RELU ? fwd_bf16<kActRelu>(c, x, W1, b1, W2, b2, y, kept, hc, he, (char*)ws)
+                                   : fwd_bf16<kActGelu>(c, x, W1, b1, W2, b2, y, kept, hc, he, (char*)ws);
   }
   if (rc || !saved) return rc;
   return vd_pack8(ctx, VARDROP_K_PACK8, x, B, n, d, dtype, VARDROP_ACT_NONE, saved, (char*)saved + pack_exponents_at(T, d), nullptr, s, {dn.dev, nullptr});
@@ -319,82 +704,28 @@ int backward(vardrop_ctx* ctx, const void* dy, int B, int n, int d, int f, int d
   const uintptr_t all = (uintptr_t)dy | (uintptr_t)W1 | (uintptr_t)W2 | (uintptr_t)dx | (uintptr_t)dW1 | (uintptr_t)dW2;
   if (all % (dtype == VARDROP_BF16 ? 16 : 4) != 0) return VARDROP_EINVAL;
   if (((uintptr_t)db1 | (uintptr_t)db2) % (grad_dtype == VARDROP_BF16 ? 2 : 4) != 0) return VARDROP_EINVAL;
-  const FfnWorkspace w = ffn_workspace(T, d, f, dtype);
-  if (!vd_aligned(saved, 256) || !ws || !vd_aligned(ws, 256) || ws_bytes < w.total) return VARDROP_EWORKSPACE;
+  if (!vd_aligned(saved, 256) || !ws || !vd_aligned(ws, 256) || ws_bytes < ffn_workspace(T, d, f, dtype).total) return VARDROP_EWORKSPACE;
   const FfnCall c = {ctx, B, n, d, f, dtype, act, T, dn, s};
   char* at = (char*)ws;
   const uint8_t* xc = (const uint8_t*)saved;
-  const uint8_t* xe = xc + pack_exponents_at(T, d);
-  const uint8_t* hc = xc + pack_bytes(T, d);
-  const uint8_t* he = hc + pack_exponents_at(T, f);
-  void *dh = at + w.wide, *a = at + w.act, *xv = at + w.x;
-  float *part = (float*)(at + w.part), *second = (float*)(at + w.second), *col = (float*)(at + w.col);
-  const VdDevCount quiet = {dn.dev, nullptr};
   FinishArgs fin = {};
   fin.slices = 1;
-  if (T > 0 && (rc = vd_unpack8(ctx, VARDROP_K_UNPACK8, xc, xe, B, n, d, dtype, xv, s, dn))) return rc;
+  fin.cols[0] = f; fin.cols[1] = d;
   if (dtype == VARDROP_BF16) {
-    if (T > 0) {
-      rc = act == VARDROP_ACT_RELU ? product<true, EpiActBwd<kActRelu>>(c, VARDROP_K_FFN_DH, dy, W2, d, f, {(bf16_t*)dh, (bf16_t*)a, hc, he, f}, false)
-                                   : product<true, EpiActBwd<kActGelu>>(c, VARDROP_K_FFN_DH, dy, W2, d, f, {(bf16_t*)dh, (bf16_t*)a, hc, he, f}, false);
-      if (rc) return rc;
-      if (dx && (rc = product<true, EpiOut>(c, VARDROP_K_FFN_DX, dh, W1, f, d, {(bf16_t*)dx, nullptr, d}, false))) return rc;
-    }
-    const int slices = grad_slices(T, d, f);
-    if ((rc = weight_gradient(c, xv, dh, d, f, slices, dW1, part, grad_dtype))) return rc;
-    if ((rc = weight_gradient(c, a, dy, f, d, slices, dW2, second, grad_dtype))) return rc;
-    fin.slices = slices;
-    if (slices > 1) {
-      fin.part[0] = part;
-      fin.part[1] = second;
-    }
+    rc = act == VARDROP_ACT_RELU ? bwd_bf16<kActRelu>(c, dy, W1, W2, xc, dx, dW1, dW2, db1 != nullptr, db2 != nullptr, grad_dtype, at, fin)
+                                 : bwd_bf16<kActGelu>(c, dy, W1, W2, xc, dx, dW1, dW2, db1 != nullptr, db2 != nullptr, grad_dtype, at, fin);
   } else {
-    GemmF32 g = {};
-    g.nz = 1; g.nseg = 1;
-    if (T > 0) {
-      g.set(0, (const float*)dy, (const float*)W2, (float*)dh, nullptr);
-      g.lda = d; g.ldb = d; g.ldc = f; g.M = (int)T; g.N = f; g.K = d;
-      g.count(dn, false, n, B, 0);
-      if ((rc = vd_gemm_f32(ctx, VARDROP_K_FFN_DH, g, true, s))) return rc;
-      if ((rc = vd_act_bwd_f32(ctx, VARDROP_K_FFN_ACT, (const float*)dh, hc, he, B, n, f, act, (float*)dh, (float*)a, s, quiet))) return rc;
-      if (dx) {
-        g.set(0, (const float*)dh, (const float*)W1, (float*)dx, nullptr);
-        g.lda = f; g.ldb = f; g.ldc = d; g.N = d; g.K = f;
-        if ((rc = vd_gemm_f32(ctx, VARDROP_K_FFN_DX, g, true, s))) return rc;
-      }
-    }
-    g.count(dn, false, n, B, 1);
-    g.K = (int)T;
-    g.set(0, (const float*)xv, (const float*)dh, (float*)dW1, nullptr);
-    g.lda = d; g.ldb = f; g.ldc = f; g.M = d; g.N = f; g.part = part;
-    if ((rc = vd_gemm_f32_wgrad(ctx, VARDROP_K_FFN_WEIGHTS, g, s))) return rc;
-    g.set(0, (const float*)a, (const float*)dy, (float*)dW2, nullptr);
-    g.lda = f; g.ldb = d; g.ldc = d; g.M = f; g.N = d; g.part = second;
-    if ((rc = vd_gemm_f32_wgrad(ctx, VARDROP_K_FFN_WEIGHTS, g, s))) return rc;
+    rc = bwd_f32(c, (const float*)dy, (const float*)W1, (const float*)W2, xc, (float*)dx, (float*)dW1, (float*)dW2, db1 != nullptr, db2 != nullptr, at, fin);
   }
-  fin.ranges = T < 64 ? 1 : (T / 64 > kColRanges ? kColRanges : (int)(T / 64));
-  if (db1 || db2) {
-    ColArgs ca = {};
-    ca.src[0] = db1 ? dh : nullptr; ca.src[1] = db2 ? dy : nullptr;
-    ca.cols[0] = f; ca.cols[1] = d;
-    ca.part = col; ca.B = B; ca.n = n; ca.ranges = fin.ranges; ca.n_dev = dn.dev;
-    const dim3 grid((unsigned)vd_ceil_div(d > f ? d : f, 64), (unsigned)fin.ranges, 2);
-    if (T > 0) {
-      VdTimer timer(ctx, VARDROP_K_FFN_BIAS, s);
-      if (dtype == VARDROP_BF16) VD_KERNEL(ctx, ffn_colsum_kernel<bf16_t>, grid, dim3(256), 0, s, ca);
-      else VD_KERNEL(ctx, ffn_colsum_kernel<float>, grid, dim3(256), 0, s, ca);
-      VD_LAUNCH_CHECK(ctx);
-    } else {
-      fin.ranges = 0;          // (no tokens: zeros)
-    }
-  }
-  if (!fin.part[0] && !db1 && !db2) return VARDROP_OK;
+  if (rc || (!fin.part[0] && !db1 && !db2)) return rc;
   fin.dW[0] = dW1; fin.dW[1] = dW2; fin.db[0] = db1; fin.db[1] = db2;
-  fin.colpart = col; fin.cols[0] = f; fin.cols[1] = d; fin.count = (long long)d * f;
-  fin.bf16 = grad_dtype == VARDROP_BF16; fin.n_dev = dn.dev; fin.n = n;
-  const long long blocks = (fin.count + 255) / 256;
+  fin.count = (long long)d * f;
+  fin.bf16 = grad_dtype == VARDROP_BF16; fin.n_dev = dn.dev; fin.B = B; fin.n = n;
+  const long long blocks = (fin.count / 4 + 255) / 256;
+  fin.blocks = blocks > 1024 ? 1024 : (int)blocks;
+  const int grid = (fin.part[0] ? 2 * fin.blocks : 0) + (db1 ? vd_ceil_div(f, 16) : 0) + (db2 ? vd_ceil_div(d, 16) : 0);
   VdTimer timer(ctx, VARDROP_K_REDUCE_DW, s);
-  VD_KERNEL(ctx, ffn_finish_kernel, dim3((unsigned)(blocks > 2048 ? 2048 : blocks), 4), dim3(256), 0, s, fin);
+  VD_KERNEL(ctx, ffn_finish_kernel, dim3((unsigned)grid), dim3(256), 0, s, fin);
   VD_LAUNCH_CHECK(ctx);
   return VARDROP_OK;
 }

@@ -129,6 +129,7 @@ struct EpiI8 {
       b[e] = a.bias && n + e < N ? to_float(a.bias[n + e]) : 0.f;
     }
   }
+  __device__ void done(int, int, bool) {}
   __device__ void row(int, int m, int n, bool live, float (&v)[8]) {
     if (!live) return;
     const float s = a.sx[m];
@@ -155,8 +156,8 @@ int i8_product(vardrop_ctx* ctx, const void* q, const float* sx, int rows, int K
   g.M = rows; g.N = N; g.slices = 1;
   const typename EpiI8<T, ACT>::Args epi = {(T*)y, sx, sw, (const T*)bias, N, N % 8 == 0 && vd_aligned(y, 16)};
   const long long t128 = (long long)vd_ceil_div(N, 128) * vd_ceil_div(rows, 128);
-  if (t128 >= 512) return launch_tile_gemm<true, true, true, 128, 2, EpiI8<T, ACT>>(ctx, VARDROP_K_LINEAR_I8, g, epi, s);
-  return launch_tile_gemm<true, true, true, 64, 3, EpiI8<T, ACT>>(ctx, VARDROP_K_LINEAR_I8, g, epi, s);
+  if (t128 >= 512) return launch_tile_gemm<true, true, true, Tile128, EpiI8<T, ACT>>(ctx, VARDROP_K_LINEAR_I8, g, epi, s);
+  return launch_tile_gemm<true, true, true, Tile64, EpiI8<T, ACT>>(ctx, VARDROP_K_LINEAR_I8, g, epi, s);
 }
 
 template <typename T>
@@ -209,7 +210,7 @@ extern "C" int vardrop_linear_i8(vardrop_ctx* ctx, const void* x, const float* s
                                  const float* scale, const void* bias, int act, void* y, int dtype, void* ws, size_t ws_bytes, void* stream) {
   if (!ctx || rows < 0 || K < 1 || N < 1 || !is_type(dtype) || (!is_type(x_dtype) && x_dtype != VARDROP_I8)) return VARDROP_EINVAL;
   if (act != VARDROP_ACT_NONE && act != VARDROP_ACT_RELU && act != VARDROP_ACT_GELU) return VARDROP_EINVAL;
-  if (K > kMaxI8K || (long long)vd_ceil_div(rows, 64) * vd_ceil_div(N, kTileN) >= (1ll << 31)) return VARDROP_EUNSUPPORTED;
+  if (K > kMaxI8K || (long long)vd_ceil_div(rows, 64) * vd_ceil_div(N, 128) >= (1ll << 31)) return VARDROP_EUNSUPPORTED;
   if ((x_dtype == VARDROP_I8) != (sx != nullptr) && rows > 0) return VARDROP_EINVAL;
   if (rows == 0) return VARDROP_OK;
   if (!x || !codes || !scale || !y || x == y) return VARDROP_EINVAL;

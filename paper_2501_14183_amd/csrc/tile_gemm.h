@@ -32,18 +32,38 @@ struct TileArgs {
   int n_max, n_mul, n_role;
 };
 
-constexpr int kTileThreads = 256, kTileN = 128, kTilePitch = 64 * 4 + 16;
+// Shape of a tile and its workgroup: BM x BN, WR x WC wavefronts, BKB bytes of k a stage (of a k-contiguous operand), NS stages.
+template <int BM_, int BN_, int WR_, int WC_, int BKB_, int NS_>
+struct TileShape {
+  static constexpr int BM = BM_, BN = BN_, WR = WR_, WC = WC_, BKB = BKB_, NS = NS_;
+  static constexpr int WAVES = WR * WC, THREADS = WAVES * 64;
+  static constexpr int MI = BM / WR / 32, NJ = BN / WC / 32;       // 32 x 32 blocks of a wavefront
+  static constexpr int PITCH = NJ * 128 + 16;                      // LDS row of 32 x (32 NJ) sums
+  static constexpr int A_BYTES = BM * BKB, B_BYTES = BN * BKB, STAGE = A_BYTES + B_BYTES;
+  static constexpr int ring = NS * STAGE, out = WAVES * 32 * PITCH, lds = ring > out ? ring : out;
+  static constexpr int per_cu = (160 << 10) / lds;                 // workgroups of a compute unit
+  static constexpr int simd = per_cu * WAVES / 4 > 0 ? per_cu * WAVES / 4 : 1;
+};
 
-template <int BM, int NS>
-constexpr int tile_lds() {
-  constexpr int ring = NS * (BM + kTileN) * 128, out = 4 * 32 * kTilePitch;
-  return ring > out ? ring : out;
-}
+typedef TileShape<64, 128, 2, 2, 128, 3> Tile64;
+typedef TileShape<128, 128, 2, 2, 128, 2> Tile128;
+typedef TileShape<256, 256, 2, 4, 128, 2> Tile256;
 
 // Descriptor of the memory from p on, `bytes` long (none: every load gives zero).
 __device__ inline copy_src tile_source(const void* p, long long bytes) {
   const long long most = 0xfffffff0ll;
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)(uint32_t)(bytes < 0 ? 0 : (bytes > most ? most : bytes)), 0x00020000);
+}
+template <int N> struct Int { static constexpr int value = N; };
+// waits until at most min(younger, A) * LPS of this wavefront's copies are in flight
+template <int A, int LPS>
+__device__ __forceinline__ void wait_stages(int younger) {
+  if constexpr (A <= 0) {
+    wait_vm<0>();
+  } else {
+    if (younger >= A) wait_vm<A * LPS>();
+    else wait_stages<A - 1, LPS>(younger);
+  }
 }
 // (keeps uses of an LDS read behind the wait before this)
 __device__ inline void tie(Frag& f) { asm volatile("" : "+v"(f.q)); }
@@ -57,104 +77,89 @@ __device__ inline intx16 tile_mfma(const Frag& a, const Frag& b, intx16 c) {
   return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(intx4, a.q), __builtin_bit_cast(intx4, b.q), c, 0, 0, 0);
 }
 
-// AKC, BKC: operand contiguous along k.  Epi: `columns(n, live)` once, then `row(slice, m, live, v)` with eight sums of row m for
-// every row of the tile; `live` is false outside the result, lanes of one row and block of 32 columns come together.
-template <bool I8, bool AKC, bool BKC, int BM, int NS, typename Epi>
-__global__ __launch_bounds__(kTileThreads, 2) void tile_gemm_kernel(TileArgs g, typename Epi::Args args) {
+// AKC, BKC: operand contiguous along k.  Epi: `columns(n, N)` once, then `row(slice, m, n, live, v)` with eight sums of row m from
+// column n on, for every row of the tile; `live` is false outside the result, lanes of one row and block of 32 columns come together.  Last
+// `done(band, n, live)`: the wavefront's rows were those of this band of 32 MI rows; lanes 8 / NJ .. apart hold the same columns.
+// t: the tile, n fastest, then m, then slice.
+template <bool I8, bool AKC, bool BKC, typename S, typename Epi>
+__device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi::Args& args, int M, int K, int t) {
   static_assert(!I8 || (AKC && BKC), "8-bit operands are contiguous along k");
   typedef typename TileSum<I8>::type Sum;
-  constexpr int BN = kTileN, MI = BM / 64, A_BYTES = BM * 128, STAGE = A_BYTES + BN * 128;
-  constexpr int IA = A_BYTES / 4096, IB = BN * 128 / 4096, LPS = IA + IB;        // 1 KB copies per wavefront and stage
-  constexpr int OPK = (AKC ? MI : 2 * MI) + (BKC ? 2 : 4);                       // LDS reads per step
+  constexpr int BM = S::BM, BN = S::BN, MI = S::MI, NJ = S::NJ, NS = S::NS, A_BYTES = S::A_BYTES, STAGE = S::STAGE, W = S::WAVES;
+  constexpr int BK = S::BKB / 2, KS = S::BKB / 32;                               // k-rows of a stage, steps of a stage
+  constexpr int IA = A_BYTES / (1024 * W), IB = S::B_BYTES / (1024 * W), LPS = IA + IB;   // 1 KB copies per wavefront and stage
+  constexpr int OPK = (AKC ? MI : 2 * MI) + (BKC ? NJ : 2 * NJ);                 // LDS reads per step
+  constexpr int CHK = S::BKB / 16, CHA = AKC ? CHK : BM / 8, CHB = BKC ? CHK : BN / 8;    // 16-byte chunks of an LDS row
+  static_assert(IA * 1024 * W == A_BYTES && IB * 1024 * W == S::B_BYTES, "whole copies");
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  int M = g.M, K = g.K;
-  if (g.n_dev) {
-    int n;
-    if (!vd_count(g.n_dev, g.n_max, n, g.status)) return;
-    if (g.n_role == 0) M = g.n_mul * n;
-    else K = g.n_mul * n;
-  }
-  const int gx = (g.N + BN - 1) / BN, gy = (M + BM - 1) / BM, total = gx * gy * g.slices;
-  if ((int)blockIdx.x >= total) return;                 // (a grid sized for the bound of a device-side count)
-  // tiles in the order n fastest, then m, then slice: a die's range shares its rows of A
-  const int t = xcd_contiguous(blockIdx.x, total);
+  const int gx = (g.N + BN - 1) / BN, gy = (M + BM - 1) / BM;
   const int n0 = t % gx * BN, m0 = t / gx % gy * BM, slice = t / (gx * gy);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
-  const int wm = wave >> 1, wn = wave & 1;
+  const int wm = wave / S::WC, wn = wave % S::WC;
   // this slice's stages
-  constexpr int ES = I8 ? 1 : 2, KU = 128 / ES;         // bytes of an element, k of a stage
+  constexpr int ES = I8 ? 1 : 2, KU = S::BKB / ES;      // bytes of an element, k of a stage
   const int stages = (K + KU - 1) / KU, per = (stages + g.slices - 1) / g.slices, s0 = min(stages, slice * per);
   const int nk = min(stages, s0 + per) - s0;
 
   // ---- sources: descriptors from the tile's first byte of the slice to the end of the matrix
-  const unsigned char* pa = (const unsigned char*)g.A + (AKC ? m0 * g.lda + s0 * 128ll : (long long)s0 * KU * g.lda + m0 * 2ll);
-  const unsigned char* pb = (const unsigned char*)g.B + (BKC ? n0 * g.ldb + s0 * 128ll : (long long)s0 * KU * g.ldb + n0 * 2ll);
-  const long long ea = AKC ? (M - m0 - 1) * g.lda + (long long)K * ES - s0 * 128ll : (K - s0 * KU - 1) * g.lda + (M - m0) * 2ll;
-  const long long eb = BKC ? (g.N - n0 - 1) * g.ldb + (long long)K * ES - s0 * 128ll : (K - s0 * KU - 1) * g.ldb + (g.N - n0) * 2ll;
+  const unsigned char* pa = (const unsigned char*)g.A + (AKC ? m0 * g.lda + (long long)s0 * S::BKB : (long long)s0 * KU * g.lda + m0 * 2ll);
+  const unsigned char* pb = (const unsigned char*)g.B + (BKC ? n0 * g.ldb + (long long)s0 * S::BKB : (long long)s0 * KU * g.ldb + n0 * 2ll);
+  const long long ea = AKC ? (M - m0 - 1) * g.lda + (long long)K * ES - (long long)s0 * S::BKB : (K - s0 * KU - 1) * g.lda + (M - m0) * 2ll;
+  const long long eb = BKC ? (g.N - n0 - 1) * g.ldb + (long long)K * ES - (long long)s0 * S::BKB : (K - s0 * KU - 1) * g.ldb + (g.N - n0) * 2ll;
   const copy_src srcA = tile_source(pa, nk > 0 ? ea : 0), srcB = tile_source(pb, nk > 0 ? eb : 0);
   uint32_t offA[IA], offB[IB];
 #pragma unroll
   for (int u = 0; u < IA; ++u) {
-    if constexpr (AKC) {
-      const int row = (u * 4 + wave) * 8 + (lane >> 3);
-      offA[u] = (uint32_t)row * (uint32_t)g.lda + (((lane & 7) ^ swz_kc<64>(row)) * 16);
-    } else {
-      constexpr int CH = BM / 8;
-      const int krow = (u * 4 + wave) * (64 / CH) + lane / CH;
-      offA[u] = (uint32_t)krow * (uint32_t)g.lda + ((lane % CH) ^ swz_nc<BM>(krow)) * 16;
-    }
+    const int row = (u * W + wave) * (64 / CHA) + lane / CHA;
+    const int c = (lane % CHA) ^ (AKC ? swz_kc<BK>(row) : swz_nc<BM>(row));
+    offA[u] = (uint32_t)row * (uint32_t)g.lda + c * 16;
   }
 #pragma unroll
   for (int u = 0; u < IB; ++u) {
-    if constexpr (BKC) {
-      const int row = (u * 4 + wave) * 8 + (lane >> 3);
-      offB[u] = (uint32_t)row * (uint32_t)g.ldb + (((lane & 7) ^ swz_kc<64>(row)) * 16);
-    } else {
-      constexpr int CH = BN / 8;
-      const int krow = (u * 4 + wave) * (64 / CH) + lane / CH;
-      offB[u] = (uint32_t)krow * (uint32_t)g.ldb + ((lane % CH) ^ swz_nc<BN>(krow)) * 16;
-    }
+    const int row = (u * W + wave) * (64 / CHB) + lane / CHB;
+    const int c = (lane % CHB) ^ (BKC ? swz_kc<BK>(row) : swz_nc<BN>(row));
+    offB[u] = (uint32_t)row * (uint32_t)g.ldb + c * 16;
   }
-  const uint32_t stepA = AKC ? 128u : 64u * (uint32_t)g.lda, stepB = BKC ? 128u : 64u * (uint32_t)g.ldb;
+  const uint32_t stepA = AKC ? (uint32_t)S::BKB : BK * (uint32_t)g.lda, stepB = BKC ? (uint32_t)S::BKB : BK * (uint32_t)g.ldb;
   auto issue = [&](int k, int buf) {
     unsigned char* sp = smem + buf * STAGE + wave * 1024;
 #pragma unroll
-    for (int u = 0; u < IA; ++u) dma16_buf(srcA, offA[u], k * stepA, sp + u * 4096);
+    for (int u = 0; u < IA; ++u) dma16_buf(srcA, offA[u], k * stepA, sp + u * W * 1024);
 #pragma unroll
-    for (int u = 0; u < IB; ++u) dma16_buf(srcB, offB[u], k * stepB, sp + A_BYTES + u * 4096);
+    for (int u = 0; u < IB; ++u) dma16_buf(srcB, offB[u], k * stepB, sp + A_BYTES + u * W * 1024);
   };
   // ---- fragment addresses (LDS bytes relative to a stage): one for every step of a k-contiguous operand (blocks of 32 rows are a
   // fixed distance apart), one for every block of the other kind (steps are)
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-  uint32_t addrA[AKC ? 4 : MI], addrB[BKC ? 4 : 2];
+  uint32_t addrA[AKC ? KS : MI], addrB[BKC ? KS : NJ];
   const int krow = 8 * half + ((lane & 15) >> 2), mn = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
   if constexpr (AKC) {
-    const int ra = wm * (BM / 2) + col;
+    const int ra = wm * (MI * 32) + col;
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) addrA[ks] = lds0 + ra * 128 + (((2 * ks + half) ^ swz_kc<64>(ra)) * 16);
+    for (int ks = 0; ks < KS; ++ks) addrA[ks] = lds0 + ra * S::BKB + (((2 * ks + half) ^ swz_kc<BK>(ra)) * 16);
   } else {
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      const int c = wm * (BM / 2) + i * 32 + mn;
+      const int c = wm * (MI * 32) + i * 32 + mn;
       addrA[i] = lds0 + krow * (BM * 2) + (((c >> 3) ^ swz_nc<BM>(krow)) * 16) + ((c >> 2) & 1) * 8;
     }
   }
   if constexpr (BKC) {
-    const int rb = wn * 64 + col;
+    const int rb = wn * (NJ * 32) + col;
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) addrB[ks] = lds0 + A_BYTES + rb * 128 + (((2 * ks + half) ^ swz_kc<64>(rb)) * 16);
+    for (int ks = 0; ks < KS; ++ks) addrB[ks] = lds0 + A_BYTES + rb * S::BKB + (((2 * ks + half) ^ swz_kc<BK>(rb)) * 16);
   } else {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int c = wn * 64 + j * 32 + mn;
+    for (int j = 0; j < NJ; ++j) {
+      const int c = wn * (NJ * 32) + j * 32 + mn;
       addrB[j] = lds0 + A_BYTES + krow * (BN * 2) + (((c >> 3) ^ swz_nc<BN>(krow)) * 16) + ((c >> 2) & 1) * 8;
     }
   }
-  Sum acc[MI][2];
+  Sum acc[MI][NJ];
 #pragma unroll
   for (int i = 0; i < MI; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
 
@@ -166,83 +171,89 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_gemm_kernel(TileArgs g, 
     for (int s = 0; s < NS; ++s) {
       const int k = t0 + s;
       if (k < nk) {
-        // stage k has landed once at most NS - 2 younger ones are in flight
-        if (NS == 3 && k + 1 < nk) wait_vm<LPS>(); else wait_vm<0>();
-        __builtin_amdgcn_s_barrier();       // everyone has seen stage k land and is done with stage k - 1, whose buffer is next
+        wait_stages<NS - 2, LPS>(nk - 1 - k);     // stage k has landed once at most NS - 2 younger ones are in flight
+        __builtin_amdgcn_s_barrier();             // everyone has seen it land and is done with stage k - 1, whose buffer is next
         if (k + NS - 1 < nk) issue(k + NS - 1, (s + NS - 1) % NS);
         const uint32_t so = s * STAGE;
-        Frag fa[2][MI], fb[2][2];
-#define VD_TILE_READ(KS_, SET)                                                                      \
-  {                                                                                                 \
-    if constexpr (AKC) {                                                                            \
-      const uint32_t p = addrA[AKC ? (KS_) : 0] + so;                                               \
-      lds_read16_at<0>(fa[SET][0].q, p);                                                            \
-      if constexpr (MI > 1) lds_read16_at<4096>(fa[SET][MI > 1 ? 1 : 0].q, p);                      \
-    } else {                                                                                        \
-      _Pragma("unroll") for (int i = 0; i < MI; ++i) {                                              \
-        lds_read8_tr<(KS_) * 16 * BM * 2>(fa[SET][i].d[0], addrA[i] + so);                          \
-        lds_read8_tr<(KS_) * 16 * BM * 2 + 4 * BM * 2>(fa[SET][i].d[1], addrA[i] + so);             \
-      }                                                                                             \
-    }                                                                                               \
-    if constexpr (BKC) {                                                                            \
-      const uint32_t p = addrB[BKC ? (KS_) : 0] + so;                                               \
-      lds_read16_at<0>(fb[SET][0].q, p);                                                            \
-      lds_read16_at<4096>(fb[SET][1].q, p);                                                         \
-    } else {                                                                                        \
-      _Pragma("unroll") for (int j = 0; j < 2; ++j) {                                               \
-        lds_read8_tr<(KS_) * 16 * BN * 2>(fb[SET][j].d[0], addrB[j] + so);                          \
-        lds_read8_tr<(KS_) * 16 * BN * 2 + 4 * BN * 2>(fb[SET][j].d[1], addrB[j] + so);             \
-      }                                                                                             \
-    }                                                                                               \
-  }
-#define VD_TILE_MFMA(SET, PENDING)                                                                  \
-  {                                                                                                 \
-    wait_lds_count<PENDING>();                                                                      \
-    _Pragma("unroll") for (int i = 0; i < MI; ++i) tie(fa[SET][i]);                                 \
-    tie(fb[SET][0]);                                                                                \
-    tie(fb[SET][1]);                                                                                \
-    _Pragma("unroll") for (int i = 0; i < MI; ++i)                                                  \
-      _Pragma("unroll") for (int j = 0; j < 2; ++j) acc[i][j] = tile_mfma(fb[SET][j], fa[SET][i], acc[i][j]); \
-    __builtin_amdgcn_sched_barrier(0);                                                              \
-  }
-        VD_TILE_READ(0, 0)
-        VD_TILE_READ(1, 1)
-        VD_TILE_MFMA(0, OPK)
-        VD_TILE_READ(2, 0)
-        VD_TILE_MFMA(1, OPK)
-        VD_TILE_READ(3, 1)
-        VD_TILE_MFMA(0, OPK)
-        VD_TILE_MFMA(1, 0)
-#undef VD_TILE_READ
-#undef VD_TILE_MFMA
+        Frag fa[2][MI], fb[2][NJ];
+        auto read = [&](auto step, int set) {
+          constexpr int ks = decltype(step)::value;
+          if constexpr (AKC) {
+            const uint32_t p = addrA[AKC ? ks : 0] + so;
+            lds_read16_at<0>(fa[set][0].q, p);
+            if constexpr (MI > 1) lds_read16_at<32 * S::BKB>(fa[set][MI > 1 ? 1 : 0].q, p);
+            if constexpr (MI > 2) lds_read16_at<64 * S::BKB>(fa[set][MI > 2 ? 2 : 0].q, p);
+            if constexpr (MI > 3) lds_read16_at<96 * S::BKB>(fa[set][MI > 3 ? 3 : 0].q, p);
+          } else {
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+              lds_read8_tr<ks * 16 * BM * 2>(fa[set][i].d[0], addrA[i] + so);
+              lds_read8_tr<ks * 16 * BM * 2 + 4 * BM * 2>(fa[set][i].d[1], addrA[i] + so);
+            }
+          }
+          if constexpr (BKC) {
+            const uint32_t p = addrB[BKC ? ks : 0] + so;
+            lds_read16_at<0>(fb[set][0].q, p);
+            if constexpr (NJ > 1) lds_read16_at<32 * S::BKB>(fb[set][NJ > 1 ? 1 : 0].q, p);
+          } else {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+              lds_read8_tr<ks * 16 * BN * 2>(fb[set][j].d[0], addrB[j] + so);
+              lds_read8_tr<ks * 16 * BN * 2 + 4 * BN * 2>(fb[set][j].d[1], addrB[j] + so);
+            }
+          }
+        };
+        auto multiply = [&](auto pending, int set) {
+          wait_lds_count<decltype(pending)::value>();
+#pragma unroll
+          for (int i = 0; i < MI; ++i) tie(fa[set][i]);
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) tie(fb[set][j]);
+#pragma unroll
+          for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) acc[i][j] = tile_mfma(fb[set][j], fa[set][i], acc[i][j]);
+          __builtin_amdgcn_sched_barrier(0);
+        };
+        read(Int<0>{}, 0);
+        read(Int<1>{}, 1);
+        multiply(Int<OPK>{}, 0);
+        if constexpr (KS == 4) {
+          read(Int<2>{}, 0);
+          multiply(Int<OPK>{}, 1);
+          read(Int<3>{}, 1);
+          multiply(Int<OPK>{}, 0);
+        }
+        multiply(Int<0>{}, 1);
       }
     }
   }
-  // ---- 32 rows x 64 columns of a wavefront at a time through its own part of LDS.  acc[i][j] element 4 q + e is row i * 32 + col,
-  // column j * 32 + 8 q + 4 half + e; back comes row (lane >> 3) + 8 u, columns 8 (lane & 7) ..
-  __syncthreads();                          // every wavefront is done reading the last stage
-  unsigned char* own = smem + wave * (32 * kTilePitch);
-  const int n = n0 + wn * 64 + 8 * (lane & 7);
+  // ---- 32 rows x 32 NJ columns of a wavefront at a time through its own part of LDS.  acc[i][j] element 4 q + e is row i * 32 + col,
+  // column j * 32 + 8 q + 4 half + e; back come eight columns a lane, the lanes of a row beside each other
+  __syncthreads();                                // every wavefront is done reading the last stage
+  constexpr int LPR = NJ * 4, RPS = 64 / LPR;     // lanes of a row, rows of a step
+  unsigned char* own = smem + wave * (32 * S::PITCH);
+  const int n = n0 + wn * (NJ * 32) + 8 * (lane % LPR);
   Epi epi{args};
   epi.columns(n, g.N);
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         u32x4 v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = sum_bits(acc[i][j][4 * q + e]);
-        *reinterpret_cast<u32x4*>(own + col * kTilePitch + (j * 32 + 8 * q + 4 * half) * 4) = v;
+        *reinterpret_cast<u32x4*>(own + col * S::PITCH + (j * 32 + 8 * q + 4 * half) * 4) = v;
       }
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int row = 8 * u + (lane >> 3), m = m0 + wm * (BM / 2) + i * 32 + row;
-      const u32x4 lo = *reinterpret_cast<const u32x4*>(own + row * kTilePitch + (lane & 7) * 32);
-      const u32x4 hi = *reinterpret_cast<const u32x4*>(own + row * kTilePitch + (lane & 7) * 32 + 16);
+    for (int u = 0; u < 32 / RPS; ++u) {
+      const int row = RPS * u + lane / LPR, m = m0 + wm * (MI * 32) + i * 32 + row;
+      const u32x4 lo = *reinterpret_cast<const u32x4*>(own + row * S::PITCH + (lane % LPR) * 32);
+      const u32x4 hi = *reinterpret_cast<const u32x4*>(own + row * S::PITCH + (lane % LPR) * 32 + 16);
       float v[8];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -259,23 +270,53 @@ __global__ __launch_bounds__(kTileThreads, 2) void tile_gemm_kernel(TileArgs g, 
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
   }
+  epi.done(m0 / (MI * 32) + wm, n, n < g.N);
 }
 
-template <bool I8, bool AKC, bool BKC, int BM, int NS, typename Epi>
+// A product's dimensions with a device-side count resolved; false: the count is invalid.
+__device__ __forceinline__ bool tile_dims(const TileArgs& g, int& M, int& K) {
+  M = g.M;
+  K = g.K;
+  if (!g.n_dev) return true;
+  int n;
+  if (!vd_count(g.n_dev, g.n_max, n, g.status)) return false;
+  (g.n_role == 0 ? M : K) = g.n_mul * n;
+  return true;
+}
+template <typename S>
+__host__ __device__ inline long long tile_count(const TileArgs& g, int M) {
+  return (long long)((g.N + S::BN - 1) / S::BN) * ((M + S::BM - 1) / S::BM) * g.slices;
+}
+
+template <bool I8, bool AKC, bool BKC, typename S, typename Epi>
+__global__ __launch_bounds__(S::THREADS, S::simd) void tile_gemm_kernel(TileArgs g, typename Epi::Args args) {
+  int M, K;
+  if (!tile_dims(g, M, K)) return;
+  const int total = (int)tile_count<S>(g, M);
+  if ((int)blockIdx.x >= total) return;           // (a grid sized for the bound of a device-side count)
+  // a die's range of the tiles shares its rows of A
+  tile_gemm<I8, AKC, BKC, S, Epi>(g, args, M, K, xcd_contiguous(blockIdx.x, total));
+}
+
+// Raises the dynamic LDS limit of a kernel (a setting of a function on a device): `configured` remembers the device.
+inline int tile_allow_lds(vardrop_ctx* ctx, const void* fn, int lds, int& configured) {
+  if (lds <= 65536 || configured == ctx->device) return VARDROP_OK;
+  VD_HIP(ctx, hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+  configured = ctx->device;
+  return VARDROP_OK;
+}
+
+template <bool I8, bool AKC, bool BKC, typename S, typename Epi>
 int launch_tile_gemm(vardrop_ctx* ctx, int kid, const TileArgs& g, const typename Epi::Args& epi, hipStream_t s) {
-  constexpr int lds = tile_lds<BM, NS>();
-  const void* fn = (const void*)tile_gemm_kernel<I8, AKC, BKC, BM, NS, Epi>;
-  static int configured_device = -1;        // (a setting of a function on a device)
-  if (lds > 65536 && configured_device != ctx->device) {
-    VD_HIP(ctx, hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
-    configured_device = ctx->device;
-  }
-  const long long grid = (long long)vd_ceil_div(g.N, kTileN) * vd_ceil_div(g.M, BM) * g.slices;
+  static int configured = -1;
+  const int rc = tile_allow_lds(ctx, (const void*)tile_gemm_kernel<I8, AKC, BKC, S, Epi>, S::lds, configured);
+  if (rc) return rc;
+  const long long grid = tile_count<S>(g, g.M);
   if (grid >= (1ll << 31)) return VARDROP_EUNSUPPORTED;
   if (grid == 0) return VARDROP_OK;
   {
     VdTimer timer(ctx, kid, s);
-    VD_KERNEL(ctx, (tile_gemm_kernel<I8, AKC, BKC, BM, NS, Epi>), dim3((unsigned)grid), dim3(kTileThreads), lds, s, g, epi);
+    VD_KERNEL(ctx, (tile_gemm_kernel<I8, AKC, BKC, S, Epi>), dim3((unsigned)grid), dim3(S::THREADS), S::lds, s, g, epi);
   }
   VD_LAUNCH_CHECK(ctx);
   return VARDROP_OK;
