@@ -5,6 +5,7 @@ are torch tensors on the GPU; torch provides device memory and the current HIP s
 nothing else.  There is no fallback: if the shared library is missing, loading fails.
 """
 import ctypes
+import functools
 import os
 
 import torch
@@ -852,19 +853,8 @@ def vardrop_adamw_dev(ctx, tensors, lr_dev, step_dev, beta1=0.9, beta2=0.999, ep
 
 
 # ---------------------------------------------------------------- activations in 8 bits, feed-forward block, 8-bit products
-def _tensor(name, t, numel, dtype, dev):
-    """Address of a contiguous tensor on device `dev` (None: not given)."""
-    if t is None:
-        return None
-    if t.dtype is dtype and t.numel() == numel and t.is_contiguous() and t.get_device() == dev:
-        return t.data_ptr()
-    _refuse(name, t, numel, dtype)
-
-
+# (checks in line, as for the block norms; sizes are asked of the library once for each shape)
 def _bytes(name, t, least, dev):
-    """Address of a byte buffer of at least `least` bytes on device `dev`."""
-    if t.dtype is torch.uint8 and t.numel() >= least and t.is_contiguous() and t.get_device() == dev:
-        return t.data_ptr()
     raise TypeError("%s must be contiguous uint8, of %d bytes at least, on device %d: got %s %s on %s"
                     % (name, least, dev, t.dtype, list(t.shape), t.device))
 
@@ -873,65 +863,65 @@ def _room(nbytes, device):
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
+@functools.lru_cache(maxsize=4096)
 def vardrop_pack8_bytes(B, n, d):
     """Bytes of an 8-bit checkpoint of a [B, n, d] tensor (a multiple of 256)."""
     return load_library().vardrop_pack8_bytes(B, n, d)
+
+
+def _packed(ctx, where, x, saved, need, dev, stream, n_dev, status):
+    """vardrop_pack8 or vardrop_unpack8 with a checkpoint that is there; x: the tensor packed, or written."""
+    B, n, d = x.shape
+    dt = x.dtype
+    p_x = x.data_ptr() if x.is_contiguous() else _refuse("x" if where == "vardrop_pack8" else "out", x, B * n * d, dt)
+    p_saved = saved.data_ptr() if (saved.dtype is torch.uint8 and saved.numel() >= need and saved.is_contiguous()
+                                   and saved.get_device() == dev) else _bytes("saved", saved, need, dev)
+    on = _device_stream(dev, stream)
+    a, b = (p_x, p_saved) if where == "vardrop_pack8" else (p_saved, p_x)
+    if n_dev is None:
+        rc = getattr(ctx._lib, where)(ctx.handle, a, B, n, d, _CODES.get(dt, -1), b, on)
+    else:
+        rc = getattr(ctx._lib, where + "_dev")(ctx.handle, a, B, _scalar("n_dev", n_dev, torch.int32, dev), n,
+                                               _scalar("status", status, torch.int32, dev), d, _CODES.get(dt, -1), b, on)
+    if rc:
+        ctx.check(rc, where)
 
 
 def vardrop_pack8(ctx, x, out=None, stream=None, n_dev=None, status=None):
     """x [B, n, d] in 8 bits: 33/32 bytes an element -> uint8 buffer (`out` when given; 256-byte aligned).
 
     n_dev (int32 [1] on the device): x is a buffer for x.shape[1] tokens that holds [B, N', d] packed."""
-    B, n, d = x.shape
-    dev, need = x.get_device(), ctx._lib.vardrop_pack8_bytes(B, n, d)
-    on = _device_stream(dev, stream)
+    need = vardrop_pack8_bytes(*x.shape)
     if out is None:
         _own_buffers(stream, "vardrop_pack8", out=out)
         out = _room(need, x.device)
-    p_x, p_out = _tensor("x", x, B * n * d, x.dtype, dev), _bytes("out", out, need, dev)
-    if n_dev is None:
-        rc = ctx._lib.vardrop_pack8(ctx.handle, p_x, B, n, d, _CODES.get(x.dtype, -1), p_out, on)
-    else:
-        rc = ctx._lib.vardrop_pack8_dev(ctx.handle, p_x, B, _scalar("n_dev", n_dev, torch.int32, dev), n,
-                                        _scalar("status", status, torch.int32, dev), d, _CODES.get(x.dtype, -1), p_out, on)
-    if rc:
-        ctx.check(rc, "vardrop_pack8")
+    _packed(ctx, "vardrop_pack8", x, out, need, x.get_device(), stream, n_dev, status)
     return out
 
 
 def vardrop_unpack8(ctx, saved, out, stream=None, n_dev=None, status=None):
     """What the checkpoint `saved` of vardrop_pack8 stands for, into out [B, n, d] (float32 or bfloat16)."""
-    B, n, d = out.shape
-    dev = out.get_device()
-    on = _device_stream(dev, stream)
-    p_out, p_saved = _tensor("out", out, B * n * d, out.dtype, dev), _bytes("saved", saved, ctx._lib.vardrop_pack8_bytes(B, n, d), dev)
-    if n_dev is None:
-        rc = ctx._lib.vardrop_unpack8(ctx.handle, p_saved, B, n, d, _CODES.get(out.dtype, -1), p_out, on)
-    else:
-        rc = ctx._lib.vardrop_unpack8_dev(ctx.handle, p_saved, B, _scalar("n_dev", n_dev, torch.int32, dev), n,
-                                          _scalar("status", status, torch.int32, dev), d, _CODES.get(out.dtype, -1), p_out, on)
-    if rc:
-        ctx.check(rc, "vardrop_unpack8")
+    _packed(ctx, "vardrop_unpack8", out, saved, vardrop_pack8_bytes(*out.shape), out.get_device(), stream, n_dev, status)
     return out
 
 
+@functools.lru_cache(maxsize=4096)
 def vardrop_ffn_saved_bytes(B, n, d, f):
     """Bytes of what vardrop_ffn_fwd keeps for the backward: the checkpoints of x [B, n, d] and of x W1 + b1 [B, n, f]."""
     return load_library().vardrop_ffn_saved_bytes(B, n, d, f)
 
 
+@functools.lru_cache(maxsize=4096)
 def vardrop_ffn_workspace_bytes(B, n, d, f, dtype):
     """Bytes of the workspace of vardrop_ffn_fwd and vardrop_ffn_bwd for tokens of a torch dtype."""
     return load_library().vardrop_ffn_workspace_bytes(B, n, d, f, _CODES.get(dtype, -1))
 
 
-def _ffn_weights(W1, W2, d, dt, dev):
+def _ffn_shapes(W1, W2, d):
     if W1.dim() != 2 or W1.shape[0] != d:
         raise TypeError("W1 must be [d, f] for tokens of d = %d channels: got %s" % (d, list(W1.shape)))
-    f = W1.shape[1]
-    if W2.dim() != 2 or W2.shape[0] != f or W2.shape[1] != d:
-        raise TypeError("W2 must be [%d, %d]: got %s" % (f, d, list(W2.shape)))
-    return f, _tensor("W1", W1, d * f, dt, dev), _tensor("W2", W2, d * f, dt, dev)
+    if W2.dim() != 2 or W2.shape[0] != W1.shape[1] or W2.shape[1] != d:
+        raise TypeError("W2 must be [%d, %d]: got %s" % (W1.shape[1], d, list(W2.shape)))
 
 
 def vardrop_ffn_fwd(ctx, x, W1, W2, b1=None, b2=None, act=ACT_GELU, train=True, saved=None, ws=None, out=None, stream=None, n_dev=None,
@@ -941,22 +931,32 @@ def vardrop_ffn_fwd(ctx, x, W1, W2, b1=None, b2=None, act=ACT_GELU, train=True, 
     saved: uint8 buffer for the backward, x and x W1 + b1 in 8 bits (made when missing; with train=False nothing is kept and it is
     None).  ws: uint8 workspace, free again once the call's work is done.  n_dev: as in vardrop_pack8."""
     B, n, d = x.shape
-    dt, dev = x.dtype, x.get_device()
-    on = _device_stream(dev, stream)
-    f, p_W1, p_W2 = _ffn_weights(W1, W2, d, dt, dev)
-    code = _CODES.get(dt, -1)
-    need, room = ctx._lib.vardrop_ffn_saved_bytes(B, n, d, f), ctx._lib.vardrop_ffn_workspace_bytes(B, n, d, f, code)
-    if not train and saved is not None:
+    dt, dev, k = x.dtype, x.get_device(), B * n * d
+    if W1.dim() != 2 or W1.shape[-1:] + (d,) != W2.shape or W1.shape[0] != d:
+        _ffn_shapes(W1, W2, d)
+    f = W1.shape[1]
+    if saved is not None and not train:
         raise TypeError("saved is for train=True")
     if out is None or ws is None or (train and saved is None):
         _own_buffers(stream, "vardrop_ffn_fwd", out=out, ws=ws, **({"saved": saved} if train else {}))
         out = torch.empty_like(x) if out is None else out
-        ws = _room(room, x.device) if ws is None else ws
-        saved = _room(need, x.device) if train and saved is None else saved
-    p_x, p_y = _tensor("x", x, B * n * d, dt, dev), _tensor("out", out, B * n * d, dt, dev)
-    p_b1, p_b2 = _tensor("b1", b1, f, dt, dev), _tensor("b2", b2, d, dt, dev)
-    p_saved = None if saved is None else _bytes("saved", saved, need, dev)
-    p_ws = _bytes("ws", ws, 0, dev)
+        ws = _room(vardrop_ffn_workspace_bytes(B, n, d, f, dt), x.device) if ws is None else ws
+        saved = _room(vardrop_ffn_saved_bytes(B, n, d, f), x.device) if train and saved is None else saved
+    p_x = x.data_ptr() if x.is_contiguous() else _refuse("x", x, k, dt)
+    p_y = out.data_ptr() if (out.dtype is dt and out.numel() == k and out.is_contiguous() and out.get_device() == dev) else _refuse("out", out, k, dt)
+    p_W1 = W1.data_ptr() if W1.dtype is dt and W1.is_contiguous() and W1.get_device() == dev else _refuse("W1", W1, d * f, dt)
+    p_W2 = W2.data_ptr() if W2.dtype is dt and W2.is_contiguous() and W2.get_device() == dev else _refuse("W2", W2, d * f, dt)
+    p_b1 = None if b1 is None else (b1.data_ptr() if b1.dtype is dt and b1.numel() == f and b1.is_contiguous() and b1.get_device() == dev
+                                    else _refuse("b1", b1, f, dt))
+    p_b2 = None if b2 is None else (b2.data_ptr() if b2.dtype is dt and b2.numel() == d and b2.is_contiguous() and b2.get_device() == dev
+                                    else _refuse("b2", b2, d, dt))
+    p_saved = None
+    if saved is not None:
+        need = vardrop_ffn_saved_bytes(B, n, d, f)
+        p_saved = saved.data_ptr() if (saved.dtype is torch.uint8 and saved.numel() >= need and saved.is_contiguous()
+                                       and saved.get_device() == dev) else _bytes("saved", saved, need, dev)
+    p_ws = ws.data_ptr() if ws.dtype is torch.uint8 and ws.is_contiguous() and ws.get_device() == dev else _bytes("ws", ws, 0, dev)
+    code, on = _CODES.get(dt, -1), _device_stream(dev, stream)
     if n_dev is None:
         rc = ctx._lib.vardrop_ffn_fwd(ctx.handle, p_x, B, n, d, f, code, act, p_W1, p_b1, p_W2, p_b2, p_y, p_saved, p_ws, ws.numel(), on)
     else:
@@ -975,10 +975,11 @@ def vardrop_ffn_bwd(ctx, dy, W1, W2, saved, act=ACT_GELU, bias_grads=False, grad
     dx in dy's type, the others in grad_dtype (float32, or bfloat16 beside bfloat16 tokens); db1 and db2 with bias_grads.  `out`, when
     given, is that tuple of preallocated tensors, whose dW1 says the type; dx, db1 and db2 may be None: not wanted."""
     B, n, d = dy.shape
-    dt, dev = dy.dtype, dy.get_device()
-    on = _device_stream(dev, stream)
-    f, p_W1, p_W2 = _ffn_weights(W1, W2, d, dt, dev)
-    code = _CODES.get(dt, -1)
+    dt, dev, k = dy.dtype, dy.get_device(), B * n * d
+    if W1.dim() != 2 or W1.shape[-1:] + (d,) != W2.shape or W1.shape[0] != d:
+        _ffn_shapes(W1, W2, d)
+    f = W1.shape[1]
+    kw = d * f
     if out is None:
         _own_buffers(stream, "vardrop_ffn_bwd", out=out)
 
@@ -990,12 +991,24 @@ def vardrop_ffn_bwd(ctx, dy, W1, W2, saved, act=ACT_GELU, bias_grads=False, grad
     gt = dW1.dtype
     if ws is None:
         _own_buffers(stream, "vardrop_ffn_bwd", ws=ws)
-        ws = _room(ctx._lib.vardrop_ffn_workspace_bytes(B, n, d, f, code), dy.device)
-    p_dy, p_dx = _tensor("dy", dy, B * n * d, dt, dev), _tensor("dx", dx, B * n * d, dt, dev)
-    p_dW1, p_dW2 = _tensor("dW1", dW1, d * f, gt, dev), _tensor("dW2", dW2, d * f, gt, dev)
-    p_db1, p_db2 = _tensor("db1", db1, f, gt, dev), _tensor("db2", db2, d, gt, dev)
-    p_saved = _bytes("saved", saved, ctx._lib.vardrop_ffn_saved_bytes(B, n, d, f), dev)
-    p_ws = _bytes("ws", ws, 0, dev)
+        ws = _room(vardrop_ffn_workspace_bytes(B, n, d, f, dt), dy.device)
+    p_dy = dy.data_ptr() if dy.is_contiguous() else _refuse("dy", dy, k, dt)
+    p_W1 = W1.data_ptr() if W1.dtype is dt and W1.is_contiguous() and W1.get_device() == dev else _refuse("W1", W1, kw, dt)
+    p_W2 = W2.data_ptr() if W2.dtype is dt and W2.is_contiguous() and W2.get_device() == dev else _refuse("W2", W2, kw, dt)
+    p_dx = None if dx is None else (dx.data_ptr() if dx.dtype is dt and dx.numel() == k and dx.is_contiguous() and dx.get_device() == dev
+                                    else _refuse("dx", dx, k, dt))
+    p_dW1 = dW1.data_ptr() if dW1.numel() == kw and dW1.is_contiguous() and dW1.get_device() == dev else _refuse("dW1", dW1, kw, gt)
+    p_dW2 = (dW2.data_ptr() if dW2.dtype is gt and dW2.numel() == kw and dW2.is_contiguous() and dW2.get_device() == dev
+             else _refuse("dW2", dW2, kw, gt))
+    p_db1 = None if db1 is None else (db1.data_ptr() if db1.dtype is gt and db1.numel() == f and db1.is_contiguous()
+                                      and db1.get_device() == dev else _refuse("db1", db1, f, gt))
+    p_db2 = None if db2 is None else (db2.data_ptr() if db2.dtype is gt and db2.numel() == d and db2.is_contiguous()
+                                      and db2.get_device() == dev else _refuse("db2", db2, d, gt))
+    need = vardrop_ffn_saved_bytes(B, n, d, f)
+    p_saved = saved.data_ptr() if (saved.dtype is torch.uint8 and saved.numel() >= need and saved.is_contiguous()
+                                   and saved.get_device() == dev) else _bytes("saved", saved, need, dev)
+    p_ws = ws.data_ptr() if ws.dtype is torch.uint8 and ws.is_contiguous() and ws.get_device() == dev else _bytes("ws", ws, 0, dev)
+    code, on = _CODES.get(dt, -1), _device_stream(dev, stream)
     if n_dev is None:
         rc = ctx._lib.vardrop_ffn_bwd(ctx.handle, p_dy, B, n, d, f, code, act, p_W1, p_W2, p_saved, p_dx, p_dW1, p_dW2, p_db1, p_db2,
                                       _CODES.get(gt, -1), p_ws, ws.numel(), on)
@@ -1008,41 +1021,46 @@ def vardrop_ffn_bwd(ctx, dy, W1, W2, saved, act=ACT_GELU, bias_grads=False, grad
     return out
 
 
+@functools.lru_cache(maxsize=4096)
+def _i8_pitch(K):
+    return load_library().vardrop_i8_pitch(K)
+
+
+def _quantized(ctx, where, t, rows, K, lines, out, stream):
+    """vardrop_quantize_rows or vardrop_quantize_weight: codes of `lines` lines along K of t, and a scale each."""
+    dev, pitch = t.get_device(), _i8_pitch(K)
+    if out is None:
+        _own_buffers(stream, where, out=out)
+        out = (torch.empty(lines, pitch, dtype=torch.int8, device=t.device), torch.empty(lines, dtype=torch.float32, device=t.device))
+    codes, scale = out
+    p_t = t.data_ptr() if t.is_contiguous() else _refuse("W" if lines != rows else "x", t, t.numel(), t.dtype)
+    p_codes = (codes.data_ptr() if codes.dtype is torch.int8 and codes.numel() == lines * pitch and codes.is_contiguous() and codes.get_device() == dev
+               else _refuse("codes", codes, lines * pitch, torch.int8))
+    p_scale = (scale.data_ptr() if scale.dtype is torch.float32 and scale.numel() == lines and scale.is_contiguous() and scale.get_device() == dev
+               else _refuse("scale", scale, lines, torch.float32))
+    rc = getattr(ctx._lib, where)(ctx.handle, p_t, *((rows, K) if where == "vardrop_quantize_rows" else (K, lines)), _CODES.get(t.dtype, -1),
+                                  p_codes, p_scale, _device_stream(dev, stream))
+    if rc:
+        ctx.check(rc, where)
+    return codes, scale
+
+
 def vardrop_quantize_rows(ctx, x, out=None, stream=None):
     """Rows of x [..., K] as 8-bit integers and a scale each -> (codes int8 [rows, pitch], scale float32 [rows]).
 
     pitch is K up to a multiple of 128, with zeros behind K.  The pair can be given to vardrop_linear_i8 in x's place."""
     K = x.shape[-1]
     rows = x.numel() // K if K else 0
-    dev, pitch = x.get_device(), ctx._lib.vardrop_i8_pitch(K)
-    on = _device_stream(dev, stream)
-    if out is None:
-        _own_buffers(stream, "vardrop_quantize_rows", out=out)
-        out = (torch.empty(rows, pitch, dtype=torch.int8, device=x.device), torch.empty(rows, dtype=torch.float32, device=x.device))
-    codes, scale = out
-    rc = ctx._lib.vardrop_quantize_rows(ctx.handle, _tensor("x", x, x.numel(), x.dtype, dev), rows, K, _CODES.get(x.dtype, -1),
-                                        _tensor("codes", codes, rows * pitch, torch.int8, dev), _tensor("scale", scale, rows, torch.float32, dev), on)
-    if rc:
-        ctx.check(rc, "vardrop_quantize_rows")
-    return codes, scale
+    return _quantized(ctx, "vardrop_quantize_rows", x, rows, K, rows, out, stream)
 
 
 def vardrop_quantize_weight(ctx, W, out=None, stream=None):
     """A weight W [K, N] (y = x W) laid out for vardrop_linear_i8, once -> (codes int8 [N, pitch], scale float32 [N])."""
     K, N = W.shape
-    dev, pitch = W.get_device(), ctx._lib.vardrop_i8_pitch(K)
-    on = _device_stream(dev, stream)
-    if out is None:
-        _own_buffers(stream, "vardrop_quantize_weight", out=out)
-        out = (torch.empty(N, pitch, dtype=torch.int8, device=W.device), torch.empty(N, dtype=torch.float32, device=W.device))
-    codes, scale = out
-    rc = ctx._lib.vardrop_quantize_weight(ctx.handle, _tensor("W", W, K * N, W.dtype, dev), K, N, _CODES.get(W.dtype, -1),
-                                          _tensor("codes", codes, N * pitch, torch.int8, dev), _tensor("scale", scale, N, torch.float32, dev), on)
-    if rc:
-        ctx.check(rc, "vardrop_quantize_weight")
-    return codes, scale
+    return _quantized(ctx, "vardrop_quantize_weight", W, -1, K, N, out, stream)
 
 
+@functools.lru_cache(maxsize=4096)
 def vardrop_linear_i8_workspace_bytes(rows, K, N):
     """Bytes of the workspace of vardrop_linear_i8 for rows that it quantises itself."""
     return load_library().vardrop_linear_i8_workspace_bytes(rows, K, N)
@@ -1053,31 +1071,40 @@ def vardrop_linear_i8(ctx, x, codes, scale, bias=None, act=ACT_NONE, dtype=None,
 
     x [..., K] float32 or bfloat16, or the pair of vardrop_quantize_rows (then y is [rows, N]).  y is of type `dtype`: that of `out`, of
     the bias or of x where it is not given.  ws: uint8 workspace for rows that the call quantises."""
-    given = isinstance(x, tuple)
-    first = x[0] if given else x
-    dev, N = first.get_device(), scale.numel()
-    on = _device_stream(dev, stream)
-    K = first.shape[-1]
-    pitch = ctx._lib.vardrop_i8_pitch(K)
-    rows = first.numel() // K if K else 0
+    given = type(x) is tuple
+    if given:
+        x, sx = x
+        if sx.dtype is not torch.float32 or not sx.is_contiguous() or sx.get_device() != x.get_device() or sx.numel() != x.shape[0]:
+            _refuse("sx", sx, x.shape[0], torch.float32)
+    dev, N, K = x.get_device(), scale.numel(), x.shape[-1]
+    pitch = _i8_pitch(K)
+    rows = x.numel() // K if K else 0
     if codes.dim() != 2 or codes.shape[1] != pitch:
         raise TypeError("codes must be [N, %d] for rows of %d: got %s" % (pitch, K, list(codes.shape)))
     if dtype is None:
         dtype = out.dtype if out is not None else bias.dtype if bias is not None else torch.bfloat16 if given else x.dtype
     if out is None:
         _own_buffers(stream, "vardrop_linear_i8", out=out)
-        out = torch.empty((rows, N) if given else (*x.shape[:-1], N), dtype=dtype, device=first.device)
+        out = torch.empty((rows, N) if given else (*x.shape[:-1], N), dtype=dtype, device=x.device)
     if ws is None and not given:
         _own_buffers(stream, "vardrop_linear_i8", ws=ws)
-        ws = _room(ctx._lib.vardrop_linear_i8_workspace_bytes(rows, K, N), first.device)
-    if given:
-        p_x, p_sx, code = _tensor("x", first, rows * pitch, torch.int8, dev), _tensor("sx", x[1], rows, torch.float32, dev), I8
-    else:
-        p_x, p_sx, code = _tensor("x", x, rows * K, x.dtype, dev), None, _CODES.get(x.dtype, -1)
-    rc = ctx._lib.vardrop_linear_i8(ctx.handle, p_x, p_sx, rows, K, N, code, _tensor("codes", codes, N * pitch, torch.int8, dev),
-                                    _tensor("scale", scale, N, torch.float32, dev), _tensor("bias", bias, N, dtype, dev), act,
-                                    _tensor("out", out, rows * N, dtype, dev), _CODES.get(dtype, -1),
-                                    None if ws is None else _bytes("ws", ws, 0, dev), 0 if ws is None else ws.numel(), on)
+        ws = _room(vardrop_linear_i8_workspace_bytes(rows, K, N), x.device)
+    code = _CODES.get(x.dtype, -1) if not given else I8 if x.dtype is torch.int8 else -1
+    p_x = x.data_ptr() if x.is_contiguous() else _refuse("x", x, rows * K, x.dtype)
+    p_codes = (codes.data_ptr() if codes.dtype is torch.int8 and codes.numel() == N * pitch and codes.is_contiguous() and codes.get_device() == dev
+               else _refuse("codes", codes, N * pitch, torch.int8))
+    p_scale = (scale.data_ptr() if scale.dtype is torch.float32 and scale.is_contiguous() and scale.get_device() == dev
+               else _refuse("scale", scale, N, torch.float32))
+    p_bias = None if bias is None else (bias.data_ptr() if bias.dtype is dtype and bias.numel() == N and bias.is_contiguous()
+                                        and bias.get_device() == dev else _refuse("bias", bias, N, dtype))
+    p_y = (out.data_ptr() if out.dtype is dtype and out.numel() == rows * N and out.is_contiguous() and out.get_device() == dev
+           else _refuse("out", out, rows * N, dtype))
+    p_ws, room = None, 0
+    if ws is not None:
+        p_ws = ws.data_ptr() if ws.dtype is torch.uint8 and ws.is_contiguous() and ws.get_device() == dev else _bytes("ws", ws, 0, dev)
+        room = ws.numel()
+    rc = ctx._lib.vardrop_linear_i8(ctx.handle, p_x, sx.data_ptr() if given else None, rows, K, N, code, p_codes, p_scale, p_bias, act, p_y,
+                                    _CODES.get(dtype, -1), p_ws, room, _device_stream(dev, stream))
     if rc:
         ctx.check(rc, "vardrop_linear_i8")
     return out

@@ -20,7 +20,8 @@ __device__ inline void bias_eight(const bf16_t* b, int n, int N, float (&v)[8]) 
   if (b && n < N) load_eight(b + n, v);
 }
 
-struct EpiOut {              // C = sums + bias, bf16
+struct EpiOut {
+  static constexpr bool kFetch = false;              // C = sums + bias, bf16
   struct Args {
     bf16_t* C;
     const bf16_t* bias;
@@ -29,7 +30,7 @@ struct EpiOut {              // C = sums + bias, bf16
   float b[8];
   __device__ void columns(int n, int N) { bias_eight(a.bias, n, N, b); }
   __device__ void done(int, int, bool) {}
-  __device__ void row(int, int m, int n, bool live, float (&v)[8]) {
+  __device__ void row(int, int, int m, int n, bool live, float (&v)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += b[e];
     if (live) store_eight(a.C + (long long)m * a.N + n, v);
@@ -37,7 +38,8 @@ struct EpiOut {              // C = sums + bias, bf16
 };
 
 template <int ACT, bool KEEP>
-struct EpiAct {              // h = sums + bias, packed with KEEP; a = act(h)
+struct EpiAct {
+  static constexpr bool kFetch = false;              // h = sums + bias, packed with KEEP; a = act(h)
   struct Args {
     bf16_t* C;
     const bf16_t* bias;
@@ -47,7 +49,7 @@ struct EpiAct {              // h = sums + bias, packed with KEEP; a = act(h)
   float b[8];
   __device__ void columns(int n, int N) { bias_eight(a.bias, n, N, b); }
   __device__ void done(int, int, bool) {}
-  __device__ void row(int, int m, int n, bool live, float (&v)[8]) {
+  __device__ void row(int, int, int m, int n, bool live, float (&v)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += b[e];
     const long long at = (long long)m * a.N + n;
@@ -65,24 +67,34 @@ struct EpiAct {              // h = sums + bias, packed with KEEP; a = act(h)
   }
 };
 
-template <int ACT, int NJ>
-struct EpiActBwd {           // sums = da; dh = da act'(h'), a = act(h'); column sums of dh over a wavefront's rows
-  struct Args {
-    bf16_t *dh, *act;
-    const uint8_t *codes, *exps;
-    float* sums;             // [bands][N], null: not wanted
-    int N;
-  } a;
+struct ActBwdArgs {
+  bf16_t *dh, *act;
+  const uint8_t *codes, *exps;
+  float* sums;               // [bands][N], null: not wanted
+  int N;
+};
+template <int ACT, int MI, int NJ>
+struct EpiActBwd {
+  static constexpr bool kFetch = true;           // sums = da; dh = da act'(h'), a = act(h'); column sums of dh over a wavefront's rows
+  typedef ActBwdArgs Args;
+  Args a;
   float c[8];
+  u32x2 codes[2 * MI * NJ];
+  uint32_t exps[2 * MI * NJ];
+  __device__ void fetch(int k, int m, int n, bool live) {
+    const long long at = live ? (long long)m * a.N + n : 0;
+    codes[k] = *reinterpret_cast<const u32x2*>(a.codes + at);
+    exps[k] = a.exps[at >> 5];
+  }
   __device__ void columns(int, int) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) c[e] = 0.f;
   }
-  __device__ void row(int, int m, int n, bool live, float (&v)[8]) {
+  __device__ void row(int, int k, int m, int n, bool live, float (&v)[8]) {
     if (!live) return;
     const long long at = (long long)m * a.N + n;
     float h[8];
-    unpack_eight(*reinterpret_cast<const u32x2*>(a.codes + at), a.exps[at >> 5], h);
+    unpack_eight(codes[k], exps[k], h);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       float slope;
@@ -103,7 +115,8 @@ struct EpiActBwd {           // sums = da; dh = da act'(h'), a = act(h'); column
   }
 };
 
-struct EpiGrad {             // weight gradients: the result in the type of the gradients, or a slice's fp32 partial product
+struct EpiGrad {
+  static constexpr bool kFetch = false;             // weight gradients: the result in the type of the gradients, or a slice's fp32 partial product
   struct Args {
     void* C;
     float* part;
@@ -111,7 +124,7 @@ struct EpiGrad {             // weight gradients: the result in the type of the 
   } a;
   __device__ void columns(int, int) {}
   __device__ void done(int, int, bool) {}
-  __device__ void row(int slice, int m, int n, bool live, float (&v)[8]) {
+  __device__ void row(int slice, int, int m, int n, bool live, float (&v)[8]) {
     if (!live) return;
     const long long at = (long long)m * a.N + n;
     if (a.part) store_eight(a.part + (long long)slice * a.M * a.N + at, v);
@@ -235,7 +248,7 @@ __global__ __launch_bounds__(S::THREADS, S::simd) void ffn_up_kernel(TileArgs g,
 }
 
 template <typename S, int ACT>
-__global__ __launch_bounds__(S::THREADS, S::simd) void ffn_dh_kernel(TileArgs g, typename EpiActBwd<ACT, S::NJ>::Args args, PieceArgs p, ColArgs<bf16_t> c) {
+__global__ __launch_bounds__(S::THREADS, S::simd) void ffn_dh_kernel(TileArgs g, ActBwdArgs args, PieceArgs p, ColArgs<bf16_t> c) {
   const int tiles = gridDim.x - p.pieces - c.pieces;
   if ((int)blockIdx.x >= tiles) {
     const int piece = blockIdx.x - tiles;
@@ -246,7 +259,7 @@ __global__ __launch_bounds__(S::THREADS, S::simd) void ffn_dh_kernel(TileArgs g,
   int M, K;
   if (!tile_dims(g, M, K)) return;
   const int total = (int)tile_count<S>(g, M);
-  if ((int)blockIdx.x < total) tile_gemm<false, true, true, S, EpiActBwd<ACT, S::NJ>>(g, args, M, K, xcd_contiguous(blockIdx.x, total));
+  if ((int)blockIdx.x < total) tile_gemm<false, true, true, S, EpiActBwd<ACT, S::MI, S::NJ>>(g, args, M, K, xcd_contiguous(blockIdx.x, total));
 }
 
 // dx, dW1 and dW2 need the results of the launch before and nothing of each other.  The kind whose tiles are longer comes first; a die takes
@@ -516,7 +529,7 @@ int launch_up(const FfnCall& c, const TileArgs& g, const typename EpiAct<ACT, KE
   VD_FFN_LAUNCH(VARDROP_K_FFN_UP, (ffn_up_kernel<S, ACT, KEEP>), S, tile_count<S>(g, g.M) + p.pieces, g, e, p)
 }
 template <typename S, int ACT>
-int launch_dh(const FfnCall& c, const TileArgs& g, const typename EpiActBwd<ACT, S::NJ>::Args& e, PieceArgs p, const ColArgs<bf16_t>& col, int* band) {
+int launch_dh(const FfnCall& c, const TileArgs& g, const ActBwdArgs& e, PieceArgs p, const ColArgs<bf16_t>& col, int* band) {
   p.pieces = pieces_8(c.T * c.d / 8, S::THREADS);
   *band = S::MI * 32;
   VD_FFN_LAUNCH(VARDROP_K_FFN_DH, (ffn_dh_kernel<S, ACT>), S, tile_count<S>(g, g.M) + p.pieces + col.pieces, g, e, p, col)
@@ -575,8 +588,7 @@ int bwd_bf16(const FfnCall& c, const void* dy, const void* W1, const void* W2, c
     p.B = c.B; p.n = c.n; p.d = c.d; p.n_dev = c.dn.dev;
     const ColArgs<bf16_t> cols = {(const bf16_t*)dy, col2, c.B, c.n, c.d, db2 ? column_pieces(c.T) : 0, c.dn.dev};
     const TileArgs g = rows_product(c, dy, W2, true, c.d, c.f, true);
-    const typename EpiActBwd<ACT, 2>::Args e2 = {dh, a, hc, hc + pack_exponents_at(c.T, c.f), db1 ? col : nullptr, c.f};
-    static_assert(Tile64::NJ == 2 && Tile128::NJ == 2 && Tile256::NJ == 2, "one form of the epilogue");
+    const ActBwdArgs e2 = {dh, a, hc, hc + pack_exponents_at(c.T, c.f), db1 ? col : nullptr, c.f};
 #define VD_CALL(S) launch_dh<S, ACT>(c, g, e2, p, cols, &fin.band)
     rc = VD_BY_SHAPE(product_shape(c.T, c.f, c.d), VD_CALL);
 #undef VD_CALL

@@ -113,13 +113,20 @@ __global__ __launch_bounds__(256) void i8_weight_kernel(const T* W, int K, int N
   }
 }
 
-template <typename T, int ACT>
+// act(v) chosen at run time: what it costs beside the product is a branch
+template <typename T>
+__device__ inline float i8_act(float v, int act) {
+  return act == kActNone ? v : act == kActRelu ? act_value<kActRelu, true>(v) : act_value<kActGelu, sizeof(T) == 4>(v);
+}
+
+template <typename T>
 struct EpiI8 {
+  static constexpr bool kFetch = false;
   struct Args {
     T* y;
-    const float *sx, *sw;
+    const float *sx, *sw;      // sx[0] is row m0's
     const T* bias;
-    int N, whole;              // whole: rows of y can be stored in groups of eight
+    int m0, N, act, whole;     // whole: rows of y can be stored in groups of eight
   } a;
   float w[8], b[8];
   __device__ void columns(int n, int N) {
@@ -130,11 +137,18 @@ struct EpiI8 {
     }
   }
   __device__ void done(int, int, bool) {}
-  __device__ void row(int, int m, int n, bool live, float (&v)[8]) {
+  __device__ void row(int, int, int m, int n, bool live, float (&v)[8]) {
     if (!live) return;
-    const float s = a.sx[m];
+    const float s = a.sx[m - a.m0];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = act_value<ACT, sizeof(T) == 4>(v[e] * s * w[e] + b[e]);
+    for (int e = 0; e < 8; ++e) v[e] = v[e] * s * w[e] + b[e];
+    if (a.act == kActRelu) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = act_value<kActRelu, true>(v[e]);
+    } else if (a.act == kActGelu) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = act_value<kActGelu, sizeof(T) == 4>(v[e]);
+    }
     T* p = a.y + (long long)m * a.N + n;
     if (a.whole) {
       store_eight(p, v);
@@ -146,18 +160,242 @@ struct EpiI8 {
   }
 };
 
-template <typename T, int ACT>
-int i8_product(vardrop_ctx* ctx, const void* q, const float* sx, int rows, int K, int N, const void* wq, const float* sw, const void* bias, void* y,
-               hipStream_t s) {
+// What a call has in hand.
+struct I8Call {
+  vardrop_ctx* ctx;
+  const void* x;
+  const float* sx;
+  int rows, K, N;
+  const uint8_t* codes;
+  const float* scale;
+  const void* bias;
+  int act;
+  void* y;
+  hipStream_t s;
+};
+
+template <typename T>
+int i8_product(const I8Call& c) {
   TileArgs g = {};
-  g.A = q; g.B = wq;
-  g.K = i8_pitch(K);
+  g.A = c.x; g.B = c.codes;
+  g.K = i8_pitch(c.K);
   g.lda = g.ldb = g.K;
-  g.M = rows; g.N = N; g.slices = 1;
-  const typename EpiI8<T, ACT>::Args epi = {(T*)y, sx, sw, (const T*)bias, N, N % 8 == 0 && vd_aligned(y, 16)};
-  const long long t128 = (long long)vd_ceil_div(N, 128) * vd_ceil_div(rows, 128);
-  if (t128 >= 512) return launch_tile_gemm<true, true, true, Tile128, EpiI8<T, ACT>>(ctx, VARDROP_K_LINEAR_I8, g, epi, s);
-  return launch_tile_gemm<true, true, true, Tile64, EpiI8<T, ACT>>(ctx, VARDROP_K_LINEAR_I8, g, epi, s);
+  g.M = c.rows; g.N = c.N; g.slices = 1;
+  const typename EpiI8<T>::Args epi = {(T*)c.y, c.sx, c.scale, (const T*)c.bias, 0, c.N, c.act, c.N % 8 == 0 && vd_aligned(c.y, 16)};
+  const long long t128 = (long long)vd_ceil_div(c.N, 128) * vd_ceil_div(c.rows, 128);
+  if (t128 >= 512) return launch_tile_gemm<true, true, true, Tile128, EpiI8<T>>(c.ctx, VARDROP_K_LINEAR_I8, g, epi, c.s);
+  return launch_tile_gemm<true, true, true, Tile64, EpiI8<T>>(c.ctx, VARDROP_K_LINEAR_I8, g, epi, c.s);
+}
+
+// ---- quantisation and product in one launch, while a tile's rows of codes fit LDS beside the stages of the weight: every workgroup makes
+// the codes of its own 32 rows (16 lanes a row), which the workgroups of the other columns make again.  32 and not 64 rows: twice the
+// workgroups, half the rows for each to wait for.
+template <typename X>
+__device__ inline void load_some(const X* row, int k, int K, bool whole, float (&v)[8]) {
+  if (whole && k + 8 <= K) {
+    load_eight(row + k, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = k + e < K ? to_float(row[k + e]) : 0.f;
+  }
+}
+typedef TileShape<32, 128, 1, 4, 128, 3> I8Shape;
+constexpr int kI8Ring = I8Shape::NS * I8Shape::B_BYTES;
+inline int i8_fused_lds(int K) { return kI8Ring + 256 + I8Shape::BM * i8_pitch(K); }
+template <typename X, typename T, int J>
+__global__ __launch_bounds__(256, 2) void i8_fused_kernel(const X* x, int rows, int K, int N, const uint8_t* codes, typename EpiI8<T>::Args args, int whole_x) {
+  typedef I8Shape S;
+  constexpr int NS = S::NS, LPS = S::B_BYTES / 4096;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  float* sx = reinterpret_cast<float*>(smem + kI8Ring);
+  unsigned char* tile = smem + kI8Ring + 256;             // [stage][32 rows][128 bytes], swizzled
+  const int pitch = i8_pitch(K), nk = pitch >> 7, gx = (N + 127) >> 7, total = gx * ((rows + 31) >> 5);
+  const int t = xcd_contiguous(blockIdx.x, total), n0 = t % gx * 128, m0 = t / gx * 32;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+  const copy_src src = tile_source(codes + (long long)n0 * pitch, (long long)(N - n0) * pitch);
+  uint32_t off[LPS];
+#pragma unroll
+  for (int u = 0; u < LPS; ++u) {
+    const int row = (u * 4 + wave) * 8 + (lane >> 3);
+    off[u] = (uint32_t)row * (uint32_t)pitch + (((lane & 7) ^ swz_kc<64>(row)) * 16);
+  }
+  auto issue = [&](int k, int buf) {
+#pragma unroll
+    for (int u = 0; u < LPS; ++u) dma16_buf(src, off[u], k * 128u, smem + buf * S::B_BYTES + (u * 4 + wave) * 1024);
+  };
+#pragma unroll
+  for (int s = 0; s < NS - 1; ++s)
+    if (s < nk) issue(s, s);
+  // ---- codes of the tile's rows
+  const int l = threadIdx.x & 15;
+  float v[2][J][8];
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const int m = m0 + p * 16 + (threadIdx.x >> 4);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      if (m < rows && j < nk) {
+        load_some(x + (long long)m * K, (l + 16 * j) * 8, K, whole_x != 0, v[p][j]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[p][j][e] = 0.f;
+      }
+    }
+  }
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const int r = p * 16 + (threadIdx.x >> 4);
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most = max(most, magnitude(v[p][j][e]));
+#pragma unroll
+    for (int i = 1; i < 16; i <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, i, 64));
+    float scale, up;
+    i8_scales(most, scale, up);
+    if (l == 0) sx[r] = scale;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      if (j < nk) {
+        uint32_t c[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) c[e] = i8_code(up == 0.f ? 0.f : v[p][j][e], up);
+        *reinterpret_cast<u32x2*>(tile + j * S::A_BYTES + r * 128 + (((l >> 1) ^ swz_kc<64>(r)) * 16) + (l & 1) * 8) =
+            u32x2{pack_four(c[0], c[1], c[2], c[3]), pack_four(c[4], c[5], c[6], c[7])};
+      }
+    }
+  }
+  __syncthreads();
+  // ---- product
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
+  const int rb = wave * 32 + col;
+  uint32_t addrA[4], addrB[4];
+#pragma unroll
+  for (int ks = 0; ks < 4; ++ks) {
+    addrA[ks] = lds0 + kI8Ring + 256 + col * 128 + (((2 * ks + half) ^ swz_kc<64>(col)) * 16);
+    addrB[ks] = lds0 + rb * 128 + (((2 * ks + half) ^ swz_kc<64>(rb)) * 16);
+  }
+  intx16 acc[1][1];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) acc[0][0][e] = 0;
+  for (int t0 = 0; t0 < nk; t0 += NS) {
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const int k = t0 + s;
+      if (k < nk) {
+        wait_stages<NS - 2, LPS>(nk - 1 - k);
+        __builtin_amdgcn_s_barrier();
+        if (k + NS - 1 < nk) issue(k + NS - 1, (s + NS - 1) % NS);
+        Frag fa[4], fb[4];
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          lds_read16(fa[ks].q, addrA[ks] + k * S::A_BYTES);
+          lds_read16(fb[ks].q, addrB[ks] + s * S::B_BYTES);
+        }
+        wait_lds<6>(fa[0], fb[0]);
+        acc[0][0] = tile_mfma(fb[0], fa[0], acc[0][0]);
+        wait_lds<4>(fa[1], fb[1]);
+        acc[0][0] = tile_mfma(fb[1], fa[1], acc[0][0]);
+        wait_lds<2>(fa[2], fb[2]);
+        acc[0][0] = tile_mfma(fb[2], fa[2], acc[0][0]);
+        wait_lds<0>(fa[3], fb[3]);
+        acc[0][0] = tile_mfma(fb[3], fa[3], acc[0][0]);
+      }
+    }
+  }
+  __syncthreads();
+  args.sx = sx;
+  args.m0 = m0;
+  EpiI8<T> epi{args};
+  tile_finish<S, EpiI8<T>>(acc, smem, epi, 0, rows, N, m0, n0);
+}
+
+// ---- up to eight rows: a workgroup makes their codes and takes 16 columns, 16 lanes each, with the byte dot product; it is as long as
+// reading a few rows of weights takes.
+constexpr int kFewRows = 8, kFewPitch = 2048;
+template <typename X, typename T, int R>
+__global__ __launch_bounds__(256) void i8_few_kernel(const X* x, int rows, int K, int N, const uint8_t* codes, typename EpiI8<T>::Args a) {
+  __shared__ __attribute__((aligned(16))) uint8_t q[R][kFewPitch];
+  __shared__ float sx[R];
+  constexpr int J = kFewPitch / 256;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 15, pitch = i8_pitch(K);
+  const int n = blockIdx.x * 16 + wave * 4 + (lane >> 4);
+  u32x4 w[J];
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int at = (l + 16 * j) * 16;
+    w[j] = n < N && at < pitch ? *reinterpret_cast<const u32x4*>(codes + (long long)n * pitch + at) : u32x4{0, 0, 0, 0};
+  }
+  for (int r = wave; r < R; r += 4) {
+    if (r >= rows) break;
+    uint32_t most = 0;
+    for (int k = lane; k < K; k += 64) most = max(most, magnitude(to_float(x[(long long)r * K + k])));
+    most = wave_max(most);
+    float scale, up;
+    i8_scales(most, scale, up);
+    for (int k = lane; k < pitch; k += 64) q[r][k] = k < K && up != 0.f ? (uint8_t)i8_code(to_float(x[(long long)r * K + k]), up) : 0;
+    if (lane == 0) sx[r] = scale;
+  }
+  __syncthreads();
+  int sum[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) sum[r] = 0;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int at = (l + 16 * j) * 16;
+    if (at < pitch) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(&q[r][at]);       // (rows behind the last: whatever is there, not stored)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[r] = __builtin_amdgcn_sdot4((int)v[e], (int)w[j][e], sum[r], false);
+      }
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 1; i < 16; i <<= 1) sum[r] += __shfl_xor(sum[r], i, 64);
+  if (n >= N) return;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (l == r && r < rows)
+      from_float(a.y + (long long)r * N + n, i8_act<T>((float)sum[r] * sx[r] * a.sw[n] + (a.bias ? to_float(a.bias[n]) : 0.f), a.act));
+}
+
+template <typename X, typename T>
+int i8_one_launch(const I8Call& c) {
+  const typename EpiI8<T>::Args a = {(T*)c.y, nullptr, c.scale, (const T*)c.bias, 0, c.N, c.act, c.N % 8 == 0 && vd_aligned(c.y, 16)};
+  const X* x = (const X*)c.x;
+  if (c.rows <= kFewRows && i8_pitch(c.K) <= kFewPitch) {
+    const dim3 grid((unsigned)vd_ceil_div(c.N, 16));
+    VdTimer timer(c.ctx, VARDROP_K_LINEAR_I8, c.s);
+    if (c.rows == 1) VD_KERNEL(c.ctx, (i8_few_kernel<X, T, 1>), grid, dim3(256), 0, c.s, x, c.rows, c.K, c.N, c.codes, a);
+    else if (c.rows <= 4) VD_KERNEL(c.ctx, (i8_few_kernel<X, T, 4>), grid, dim3(256), 0, c.s, x, c.rows, c.K, c.N, c.codes, a);
+    else VD_KERNEL(c.ctx, (i8_few_kernel<X, T, 8>), grid, dim3(256), 0, c.s, x, c.rows, c.K, c.N, c.codes, a);
+    VD_LAUNCH_CHECK(c.ctx);
+    return VARDROP_OK;
+  }
+  const int lds = i8_fused_lds(c.K), whole = c.K % 8 == 0 && vd_aligned(x, 16);
+  const dim3 grid((unsigned)(vd_ceil_div(c.N, 128) * vd_ceil_div(c.rows, 32)));
+  static int narrow = -1, wide = -1;
+  const bool small = i8_pitch(c.K) <= 512;
+  const int rc = small ? tile_allow_lds(c.ctx, (const void*)i8_fused_kernel<X, T, 4>, i8_fused_lds(512), narrow)
+                       : tile_allow_lds(c.ctx, (const void*)i8_fused_kernel<X, T, 8>, i8_fused_lds(1024), wide);
+  if (rc) return rc;
+  VdTimer timer(c.ctx, VARDROP_K_LINEAR_I8, c.s);
+  if (small) VD_KERNEL(c.ctx, (i8_fused_kernel<X, T, 4>), grid, dim3(256), lds, c.s, x, c.rows, c.K, c.N, c.codes, a, whole);
+  else VD_KERNEL(c.ctx, (i8_fused_kernel<X, T, 8>), grid, dim3(256), lds, c.s, x, c.rows, c.K, c.N, c.codes, a, whole);
+  VD_LAUNCH_CHECK(c.ctx);
+  return VARDROP_OK;
+}
+// One launch: few rows, or rows whose codes fit beside the stages while all tiles are resident together (two workgroups a compute unit up to
+// K = 512, one above).
+bool i8_is_one_launch(const I8Call& c) {
+  if (c.rows <= kFewRows && i8_pitch(c.K) <= kFewPitch) return true;
+  if (i8_pitch(c.K) > 1024) return false;
+  return (long long)vd_ceil_div(c.rows, 32) * vd_ceil_div(c.N, 128) <= 2 * c.ctx->num_cus;
 }
 
 template <typename T>
@@ -217,20 +455,18 @@ extern "C" int vardrop_linear_i8(vardrop_ctx* ctx, const void* x, const float* s
   if (!vd_aligned(x, x_dtype == VARDROP_I8 ? 16 : element(x_dtype)) || !vd_aligned(codes, 16) || !vd_aligned(scale, 4) || !vd_aligned(sx, 4) ||
       !vd_aligned(y, element(dtype)) || !vd_aligned(bias, element(dtype)))
     return VARDROP_EINVAL;
-  hipStream_t s = (hipStream_t)stream;
-  const void* q = x;
+  I8Call c = {ctx, x, sx, rows, K, N, (const uint8_t*)codes, scale, bias, act, y, (hipStream_t)stream};
   if (x_dtype != VARDROP_I8) {
     if (!ws || !vd_aligned(ws, 256) || ws_bytes < vardrop_linear_i8_workspace_bytes(rows, K, N)) return VARDROP_EWORKSPACE;
+    if (i8_is_one_launch(c)) {
+      if (x_dtype == VARDROP_BF16) return dtype == VARDROP_BF16 ? i8_one_launch<bf16_t, bf16_t>(c) : i8_one_launch<bf16_t, float>(c);
+      return dtype == VARDROP_BF16 ? i8_one_launch<float, bf16_t>(c) : i8_one_launch<float, float>(c);
+    }
     float* made = (float*)((char*)ws + vd_align_up((size_t)rows * i8_pitch(K), 256));
     const int rc = vardrop_quantize_rows(ctx, x, rows, K, x_dtype, ws, made, stream);
     if (rc) return rc;
-    q = ws;
-    sx = made;
+    c.x = ws;
+    c.sx = made;
   }
-#define VD_I8(T)                                                                                                       \
-  (act == VARDROP_ACT_NONE ? i8_product<T, kActNone>(ctx, q, sx, rows, K, N, codes, scale, bias, y, s)                 \
-   : act == VARDROP_ACT_RELU ? i8_product<T, kActRelu>(ctx, q, sx, rows, K, N, codes, scale, bias, y, s)               \
-                             : i8_product<T, kActGelu>(ctx, q, sx, rows, K, N, codes, scale, bias, y, s))
-  return dtype == VARDROP_BF16 ? VD_I8(bf16_t) : VD_I8(float);
-#undef VD_I8
+  return dtype == VARDROP_BF16 ? i8_product<bf16_t>(c) : i8_product<float>(c);
 }

@@ -28,26 +28,30 @@ __device__ inline uint32_t pack_exponent(uint32_t most) {
 }
 __device__ inline float pack_up(uint32_t e) { return __uint_as_float((254u - min(e, 253u)) << 23); }
 __device__ inline float pack_step(uint32_t e) { return __uint_as_float(e == 255u ? 0x7fc00000u : e << 23); }
-// Code of v in the low byte: 1.5 * 2^23 has steps of one, and the product with a power of two is exact.
-__device__ inline uint32_t pack_code(float v, float up) {
-  return __float_as_uint(__builtin_amdgcn_fmed3f(v * up, -127.f, 127.f) + 12582912.f);
-}
+// Code of v in the low byte: 1.5 * 2^23 has steps of one, and the product with a power of two is exact.  (Only the largest exponent's can
+// be above 127.)
+__device__ inline uint32_t pack_code(float v, float up) { return __float_as_uint(fmaf(v, up, 12582912.f)); }
+__device__ inline float pack_limit(float v) { return __builtin_amdgcn_fmed3f(v, -127.f * 0x1p121f, 127.f * 0x1p121f); }
+// the larger of two magnitudes, NaN if one is
+__device__ inline float most_of(float a, float b) { return __builtin_elementwise_maximum(__builtin_fabsf(a), __builtin_fabsf(b)); }
 __device__ inline uint32_t pack_four(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x0c0c0400u), hi = __builtin_amdgcn_perm(d, c, 0x0c0c0400u);
   return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
 }
 // Codes of eight neighbouring values; the four lanes of a block come together, `e` is the block's.
 __device__ inline u32x2 pack_eight(const float (&v)[8], uint32_t& e) {
-  uint32_t most = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) most = max(most, magnitude(v[i]));
-  most = max(most, (uint32_t)__builtin_amdgcn_mov_dpp((int)most, 0xb1, 0xf, 0xf, true));      // lanes ^ 1
-  most = max(most, (uint32_t)__builtin_amdgcn_mov_dpp((int)most, 0x4e, 0xf, 0xf, true));      // lanes ^ 2
-  e = pack_exponent(most);
+  float top = most_of(most_of(most_of(v[0], v[1]), most_of(v[2], v[3])), most_of(most_of(v[4], v[5]), most_of(v[6], v[7])));
+  top = most_of(top, __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(top), 0xb1, 0xf, 0xf, true)));      // lanes ^ 1
+  top = most_of(top, __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(top), 0x4e, 0xf, 0xf, true)));      // lanes ^ 2
+  e = pack_exponent(__float_as_uint(top));
   const float up = pack_up(e);
   uint32_t c[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) c[i] = pack_code(v[i], up);
+  if (e >= 248u) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = pack_code(pack_limit(v[i]), up);
+  }
   return u32x2{pack_four(c[0], c[1], c[2], c[3]), pack_four(c[4], c[5], c[6], c[7])};
 }
 // Values of four codes (one conversion with sign extension and one product each)
@@ -63,16 +67,31 @@ __device__ inline void unpack_eight(u32x2 codes, uint32_t e, float (&v)[8]) {
   unpack_four(codes.y, step, v + 4);
 }
 
-// ---- GELU(x) = x Phi(x), and its derivative Phi(x) + x phi(x)
-// Upper tail Q(|x|) of the normal distribution and phi(x) sqrt(2 pi): Abramowitz and Stegun, Handbook of Mathematical Functions,
-// 7.1.26 (erf to 1.5e-7), whose exponential the derivative needs as well.  For results in bf16.
-__device__ inline float normal_tail(float x, float& bell) {
-  const float z = fabsf(x) * 0.70710678118f;
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, z, 1.f));
-  bell = fast_exp2(z * z * -1.44269504089f);
-  const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-  return 0.5f * p * bell;
+// ---- GELU(x) = x Phi(x), and its derivative Phi(x) + x phi(x).  With u = |x| and the upper tail Q = 1 - Phi,
+//   GELU = max(x, 0) - u Q(u),   GELU' = 1/2 +- (1/2 - S(u)),   S = Q - u phi = Q R
+// where log2 Q and R are smooth: polynomials of degrees 6 and 5 fitted to them over 0 <= u <= 5.5 (Q to 2.7e-5 of itself, u Q to
+// 3.9e-6, S to 1.5e-5; from 5.5 on u Q is below 1.1e-7).  One exponential, no reciprocal: 13 and 22 vector issues an
+// element; by the formula 7.1.26 of Abramowitz and Stegun 22 and 30, which the products cannot hide.  For results in bf16.
+__device__ inline float tail_of(float u) {
+  float p = 2.6153800718020648e-05f;
+  p = fmaf(p, u, -0.0006609821575693786f);
+  p = fmaf(p, u, 0.007488316390663385f);
+  p = fmaf(p, u, -0.05197042599320412f);
+  p = fmaf(p, u, -0.46032944321632385f);
+  p = fmaf(p, u, -1.1505839824676514f);
+  p = fmaf(p, u, -1.0000361204147339f);
+  return fast_exp2(p);
 }
+__device__ inline float slope_factor(float u) {
+  float r = -0.0016836859285831451f;
+  r = fmaf(r, u, 0.01988912560045719f);
+  r = fmaf(r, u, -0.1082354485988617f);
+  r = fmaf(r, u, -0.6373599171638489f);
+  r = fmaf(r, u, -0.7977257370948792f);
+  return fmaf(r, u, 0.9999952912330627f);
+}
+// |x|, at most 5.5 (NaN stays)
+__device__ inline float tail_argument(float x) { return __builtin_elementwise_minimum(__builtin_fabsf(x), 5.5f); }
 enum { kActNone = VARDROP_ACT_NONE, kActRelu = VARDROP_ACT_RELU, kActGelu = VARDROP_ACT_GELU };
 // `exact`: with the library's erf, for fp32 results
 template <int ACT, bool EXACT>
@@ -80,9 +99,8 @@ __device__ inline float act_value(float x) {
   if constexpr (ACT == kActNone) return x;
   if constexpr (ACT == kActRelu) return x < 0.f ? 0.f : x;              // (NaN stays)
   if constexpr (EXACT) return x * 0.5f * erfcf(x * -0.70710678118654752f);
-  float bell;
-  const float q = normal_tail(x, bell);
-  return x * (x < 0.f ? q : 1.f - q);
+  const float u = tail_argument(x);
+  return fmaf(-u, tail_of(u), __builtin_elementwise_maximum(x, 0.f));
 }
 // value and derivative
 template <int ACT, bool EXACT>
@@ -91,16 +109,15 @@ __device__ inline float act_both(float x, float& slope) {
     slope = x > 0.f ? 1.f : (x <= 0.f ? 0.f : x);
     return x < 0.f ? 0.f : x;
   }
-  float below, bell;
   if constexpr (EXACT) {
-    below = 0.5f * erfcf(x * -0.70710678118654752f);
-    bell = expf(-0.5f * x * x);
-  } else {
-    const float q = normal_tail(x, bell);
-    below = x < 0.f ? q : 1.f - q;
+    const float below = 0.5f * erfcf(x * -0.70710678118654752f);
+    slope = fmaf(x * 0.39894228040f, expf(-0.5f * x * x), below);
+    return x * below;
   }
-  slope = fmaf(x * 0.39894228040f, bell, below);
-  return x * below;
+  const float u = tail_argument(x), q = tail_of(u);
+  const float t = fmaf(-slope_factor(u), q, 0.5f);
+  slope = 0.5f + __uint_as_float(__float_as_uint(t) ^ (__float_as_uint(x) & 0x80000000u));
+  return fmaf(-u, q, __builtin_elementwise_maximum(x, 0.f));
 }
 
 // eight neighbouring elements

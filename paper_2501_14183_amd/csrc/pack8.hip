@@ -95,7 +95,7 @@ __global__ __launch_bounds__(256) void pack8_any_kernel(PackArgs p) {
 #pragma unroll
         for (int m = 1; m < 32; m <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, m, 64));
         const uint32_t e = pack_exponent(most);
-        if (live) p.codes[row[u] * p.d + c[u]] = (uint8_t)pack_code(v[u], pack_up(e));
+        if (live) p.codes[row[u] * p.d + c[u]] = (uint8_t)pack_code(e >= 248u ? pack_limit(v[u]) : v[u], pack_up(e));
         if (live && l == 0) p.exps[b] = (uint8_t)e;
       }
       if constexpr (ACT != kActNone) {

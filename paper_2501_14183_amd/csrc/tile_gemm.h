@@ -77,8 +77,65 @@ __device__ inline intx16 tile_mfma(const Frag& a, const Frag& b, intx16 c) {
   return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(intx4, a.q), __builtin_bit_cast(intx4, b.q), c, 0, 0, 0);
 }
 
-// AKC, BKC: operand contiguous along k.  Epi: `columns(n, N)` once, then `row(slice, m, n, live, v)` with eight sums of row m from
-// column n on, for every row of the tile; `live` is false outside the result, lanes of one row and block of 32 columns come together.  Last
+// The end of a tile: 32 rows x 32 NJ columns of a wavefront at a time through its own part of LDS (`smem`: 32 PITCH bytes a wavefront).
+// acc[i][j] element 4 q + e is row i * 32 + lane % 32, column j * 32 + 8 q + 4 (lane / 32) + e; back come eight columns a lane, the lanes of
+// a row beside each other.
+template <typename S, typename Epi, typename Sum>
+__device__ __forceinline__ void tile_finish(const Sum (&acc)[S::MI][S::NJ], unsigned char* smem, Epi& epi, int slice, int M, int N, int m0, int n0) {
+  constexpr int MI = S::MI, NJ = S::NJ, LPR = NJ * 4, RPS = 64 / LPR;     // lanes of a row, rows of a step
+  constexpr bool I8 = __is_same(Sum, intx16);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 31, half = lane >> 5;
+  const int wm = wave / S::WC, wn = wave % S::WC;
+  unsigned char* own = smem + wave * (32 * S::PITCH);
+  const int n = n0 + wn * (NJ * 32) + 8 * (lane % LPR);
+  auto row_of = [&](int i, int u) { return m0 + wm * (MI * 32) + i * 32 + RPS * u + lane / LPR; };
+  if constexpr (Epi::kFetch) {
+    // what the rows need from memory is on its way while the sums go through LDS
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int u = 0; u < 32 / RPS; ++u) epi.fetch(i * (32 / RPS) + u, row_of(i, u), n, row_of(i, u) < M && n < N);
+  }
+  epi.columns(n, N);
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        u32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = sum_bits(acc[i][j][4 * q + e]);
+        *reinterpret_cast<u32x4*>(own + col * S::PITCH + (j * 32 + 8 * q + 4 * half) * 4) = v;
+      }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int u = 0; u < 32 / RPS; ++u) {
+      const int row = RPS * u + lane / LPR, m = row_of(i, u);
+      const u32x4 lo = *reinterpret_cast<const u32x4*>(own + row * S::PITCH + (lane % LPR) * 32);
+      const u32x4 hi = *reinterpret_cast<const u32x4*>(own + row * S::PITCH + (lane % LPR) * 32 + 16);
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (I8) {
+          v[e] = (float)(int)lo[e];
+          v[4 + e] = (float)(int)hi[e];
+        } else {
+          v[e] = __uint_as_float(lo[e]);
+          v[4 + e] = __uint_as_float(hi[e]);
+        }
+      }
+      epi.row(slice, i * (32 / RPS) + u, m, n, m < M && n < N, v);
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  }
+  epi.done(m0 / (MI * 32) + wm, n, n < N);
+}
+
+// AKC, BKC: operand contiguous along k.  Epi: `columns(n, N)` once, then `row(slice, k, m, n, live, v)` with eight sums of row m from
+// column n on, for every row of the tile (k counts a wavefront's); `live` is false outside the result, lanes of one row and block of 32 columns come together.  Last
 // `done(band, n, live)`: the wavefront's rows were those of this band of 32 MI rows; lanes 8 / NJ .. apart hold the same columns.
 // t: the tile, n fastest, then m, then slice.
 template <bool I8, bool AKC, bool BKC, typename S, typename Epi>
@@ -228,49 +285,9 @@ __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi:
       }
     }
   }
-  // ---- 32 rows x 32 NJ columns of a wavefront at a time through its own part of LDS.  acc[i][j] element 4 q + e is row i * 32 + col,
-  // column j * 32 + 8 q + 4 half + e; back come eight columns a lane, the lanes of a row beside each other
   __syncthreads();                                // every wavefront is done reading the last stage
-  constexpr int LPR = NJ * 4, RPS = 64 / LPR;     // lanes of a row, rows of a step
-  unsigned char* own = smem + wave * (32 * S::PITCH);
-  const int n = n0 + wn * (NJ * 32) + 8 * (lane % LPR);
   Epi epi{args};
-  epi.columns(n, g.N);
-#pragma unroll
-  for (int i = 0; i < MI; ++i) {
-#pragma unroll
-    for (int j = 0; j < NJ; ++j)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        u32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = sum_bits(acc[i][j][4 * q + e]);
-        *reinterpret_cast<u32x4*>(own + col * S::PITCH + (j * 32 + 8 * q + 4 * half) * 4) = v;
-      }
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int u = 0; u < 32 / RPS; ++u) {
-      const int row = RPS * u + lane / LPR, m = m0 + wm * (MI * 32) + i * 32 + row;
-      const u32x4 lo = *reinterpret_cast<const u32x4*>(own + row * S::PITCH + (lane % LPR) * 32);
-      const u32x4 hi = *reinterpret_cast<const u32x4*>(own + row * S::PITCH + (lane % LPR) * 32 + 16);
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if constexpr (I8) {
-          v[e] = (float)(int)lo[e];
-          v[4 + e] = (float)(int)hi[e];
-        } else {
-          v[e] = __uint_as_float(lo[e]);
-          v[4 + e] = __uint_as_float(hi[e]);
-        }
-      }
-      epi.row(slice, m, n, m < M && n < g.N, v);
-    }
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
-  }
-  epi.done(m0 / (MI * 32) + wm, n, n < g.N);
+  tile_finish<S, Epi>(acc, smem, epi, slice, M, g.N, m0, n0);
 }
 
 // A product's dimensions with a device-side count resolved; false: the count is invalid.

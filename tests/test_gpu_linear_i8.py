@@ -47,7 +47,7 @@ def bound(x, W, b, act, dtype):
     return want, e if dtype == "fp32" else e + BF * (np.abs(want) + e)
 
 
-SIZES = [(1, 1, 1), (1, 512, 512), (2, 3, 5), (5, 97, 33), (1, 128, 64), (3, 129, 127), (16, 64, 128), (17, 200, 129), (63, 96, 321), (64, 128, 8), (65, 257, 130),
+SIZES = [(7, 512, 100), (8, 2048, 33), (9, 1024, 130), (64, 1025, 128), (129, 600, 200), (862, 512, 720), (1, 1, 1), (1, 512, 512), (2, 3, 5), (5, 97, 33), (1, 128, 64), (3, 129, 127), (16, 64, 128), (17, 200, 129), (63, 96, 321), (64, 128, 8), (65, 257, 130),
          (130, 1000, 72), (200, 2048, 40), (300, 2050, 24), (257, 31, 700)]
 
 

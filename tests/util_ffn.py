@@ -2,8 +2,9 @@
 
 u = 2^-24 is the error of one fp32 operation.  A sum of K products is off by at most (K + 4) 2 u times the sum of their magnitudes,
 in any order (a product of three-part numbers by itself: 2 u); GELU and its derivative have slopes of at most 1.13 and 0.8 and are
-themselves off by 8 u of their magnitude, in the bf16 form by 1.5e-7 |x| + 16 u (1 + |x|) (the table's formula, its reciprocal and its
-exponential).  A rounding to bf16 is off by at most 2^-8 of the value.  These are followed through the block.
+themselves off by 8 u of their magnitude.  In the bf16 form a fitted Q = 1 - Phi(|x|) is off by 2.7e-5 of itself and by 16 u (a polynomial of
+degree 6 and the exponential; its argument of up to 25 costs 25 * 7 u more), and S = Q - |x| phi by 1.5e-5 beside that; from |x| = 5.5 on
+both are held, which is off by 1.1e-7 and 6e-7.  test_ffn_host.py evaluates the fits.  A rounding to bf16 is off by at most 2^-8 of the value.  These are followed through the block.
 """
 import numpy as np
 
@@ -24,7 +25,11 @@ def act_error(x, ex, dtype, act, slope=False):
     ex = ex + 0.0 * x
     if act == "relu":
         return 0.0 * x if slope else ex
-    own = 8 * U * (1 + np.abs(x)) if dtype == "fp32" else 1.5e-7 * (1 + np.abs(x)) + 16 * U * (1 + np.abs(x))
+    if dtype == "fp32":
+        own = 8 * U * (1 + np.abs(x))
+    else:
+        tail = o.cdf(-np.abs(x)) * (2.7e-5 + 200 * U)
+        own = (tail + 1.5e-5 + 6e-7 if slope else np.abs(x) * tail + 1.1e-7) + 8 * U * (1 + np.abs(x))
     return own + (0.8 if slope else 1.13) * ex
 
 
