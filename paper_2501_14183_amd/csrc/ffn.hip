@@ -21,34 +21,32 @@ __device__ inline void bias_eight(const bf16_t* b, int n, int N, float (&v)[8]) 
 }
 
 struct EpiOut {
-  static constexpr bool kFetch = false;              // C = sums + bias, bf16
+  static constexpr bool kFetch = false, kSums = false;              // C = sums + bias, bf16
   struct Args {
     bf16_t* C;
     const bf16_t* bias;
-    int N;
+    int N, past;
   } a;
   float b[8];
   __device__ void columns(int n, int N) { bias_eight(a.bias, n, N, b); }
-  __device__ void done(int, int, bool) {}
   __device__ void row(int, int, int m, int n, bool live, float (&v)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += b[e];
-    if (live) store_eight(a.C + (long long)m * a.N + n, v);
+    if (live) store_eight(a.C + (long long)m * a.N + n, v, a.past);
   }
 };
 
 template <int ACT, bool KEEP>
 struct EpiAct {
-  static constexpr bool kFetch = false;              // h = sums + bias, packed with KEEP; a = act(h)
+  static constexpr bool kFetch = false, kSums = false;              // h = sums + bias, packed with KEEP; a = act(h)
   struct Args {
     bf16_t* C;
     const bf16_t* bias;
     uint8_t *codes, *exps;
-    int N;
+    int N, past;
   } a;
   float b[8];
   __device__ void columns(int n, int N) { bias_eight(a.bias, n, N, b); }
-  __device__ void done(int, int, bool) {}
   __device__ void row(int, int, int m, int n, bool live, float (&v)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += b[e];
@@ -57,28 +55,26 @@ struct EpiAct {
       uint32_t e;
       const u32x2 c = pack_eight(v, e);
       if (live) {
-        *reinterpret_cast<u32x2*>(a.codes + at) = c;
+        store_past(reinterpret_cast<u32x2*>(a.codes + at), c, a.past);
         if ((n & 31) == 0) a.exps[at >> 5] = (uint8_t)e;
       }
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = act_value<ACT, false>(v[e]);
-    if (live) store_eight(a.C + at, v);
+    if (live) store_eight(a.C + at, v, a.past);
   }
 };
 
 struct ActBwdArgs {
   bf16_t *dh, *act;
   const uint8_t *codes, *exps;
-  float* sums;               // [bands][N], null: not wanted
-  int N;
+  int N, past;
 };
 template <int ACT, int MI, int NJ>
 struct EpiActBwd {
-  static constexpr bool kFetch = true;           // sums = da; dh = da act'(h'), a = act(h'); column sums of dh over a wavefront's rows
+  static constexpr bool kFetch = true, kSums = false;           // sums = da; dh = da act'(h'), a = act(h')
   typedef ActBwdArgs Args;
   Args a;
-  float c[8];
   u32x2 codes[2 * MI * NJ];
   uint32_t exps[2 * MI * NJ];
   __device__ void fetch(int k, int m, int n, bool live) {
@@ -86,10 +82,7 @@ struct EpiActBwd {
     codes[k] = *reinterpret_cast<const u32x2*>(a.codes + at);
     exps[k] = a.exps[at >> 5];
   }
-  __device__ void columns(int, int) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c[e] = 0.f;
-  }
+  __device__ void columns(int, int) {}
   __device__ void row(int, int k, int m, int n, bool live, float (&v)[8]) {
     if (!live) return;
     const long long at = (long long)m * a.N + n;
@@ -100,30 +93,24 @@ struct EpiActBwd {
       float slope;
       h[e] = act_both<ACT, false>(h[e], slope);
       v[e] *= slope;
-      c[e] += v[e];
     }
-    store_eight(a.dh + at, v);
-    store_eight(a.act + at, h);
-  }
-  __device__ void done(int band, int n, bool live) {
-    if (!a.sums) return;
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-#pragma unroll
-      for (int m = 4 * NJ; m < 64; m <<= 1) c[e] += __shfl_xor(c[e], m, 64);
-    if (live && (threadIdx.x & 63) < 4 * NJ) store_eight(a.sums + (long long)band * a.N + n, c);
+    store_eight(a.dh + at, v, a.past);
+    store_eight(a.act + at, h, a.past);
   }
 };
 
 struct EpiGrad {
-  static constexpr bool kFetch = false;             // weight gradients: the result in the type of the gradients, or a slice's fp32 partial product
+  static constexpr bool kFetch = false, kSums = true;             // weight gradients: the result in the type of the gradients, or a slice's fp32 partial product
   struct Args {
     void* C;
     float* part;
+    float* sums;             // column sums of B, [pieces][N]; null: not wanted
     int M, N, bf16;
   } a;
+  __device__ void sums(int piece, int n, bool live, float v) {
+    if (live && a.sums) a.sums[(long long)piece * a.N + n] = v;
+  }
   __device__ void columns(int, int) {}
-  __device__ void done(int, int, bool) {}
   __device__ void row(int slice, int, int m, int n, bool live, float (&v)[8]) {
     if (!live) return;
     const long long at = (long long)m * a.N + n;
@@ -133,7 +120,8 @@ struct EpiGrad {
   }
 };
 
-// ---- what else a launch carries: element-wise work in workgroups behind those of the product, which has no need of it
+// ---- what else a launch carries: element-wise work in workgroups behind those of the product, which has no need of it.  (Between them, eight
+// pieces and so many tiles in turn, the activation of 65 536 x 768 x 1536 took 250 us instead of 215, of 2784 x 512 x 512 11.3 instead of 8.6.)
 // x into 8 bits, or x' out of them: groups of eight elements, `pieces` workgroups (d is a multiple of 32)
 struct PieceArgs {
   const bf16_t* x;
@@ -179,61 +167,6 @@ __device__ __forceinline__ void piece_8(const PieceArgs& p, int piece) {
     }
   }
 }
-// Column sums of src [B n][d] over a range of rows for each of `pieces` workgroups: a wavefront takes every WAVES-th row, the sums of the
-// wavefronts are added in order
-template <typename T>
-struct ColArgs {
-  const T* src;
-  float* part;                 // [pieces][d]
-  int B, n, d, pieces;
-  const int32_t* n_dev;
-};
-template <int THREADS>
-__device__ __forceinline__ void piece_columns(const ColArgs<bf16_t>& c, int piece) {
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  float(*red)[64][9] = reinterpret_cast<float(*)[64][9]>(smem);
-  constexpr int W = THREADS / 64;
-  int n;
-  if (!vd_count(c.n_dev, c.n, n)) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, units = c.d >> 3;
-  const long long rows = (long long)c.B * n, per = (rows + c.pieces - 1) / c.pieces, r0 = piece * per, r1 = min(rows, r0 + per);
-  for (int u0 = 0; u0 < units; u0 += 64) {
-    float s[8] = {};
-    if (u0 + lane < units) {
-      const bf16_t* p = c.src + (u0 + lane) * 8;
-      long long r = r0 + wave;
-      for (; r + 7 * W < r1; r += 8 * W) {
-        u32x4 q[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = *reinterpret_cast<const u32x4*>(p + (r + i * W) * c.d);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            s[2 * w] += __uint_as_float(q[i][w] << 16);
-            s[2 * w + 1] += __uint_as_float(q[i][w] & 0xffff0000u);
-          }
-      }
-      for (; r < r1; r += W) {
-        float v[8];
-        load_eight(p + r * c.d, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] += v[e];
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int e = 0; e < 8; ++e) red[wave][lane][e] = s[e];
-    __syncthreads();
-    for (int i = threadIdx.x; i < 512; i += THREADS) {
-      float sum = 0.f;
-#pragma unroll
-      for (int w = 0; w < W; ++w) sum += red[w][i >> 3][i & 7];
-      if (u0 * 8 + i < c.d) c.part[(long long)piece * c.d + u0 * 8 + i] = sum;
-    }
-  }
-}
-
 template <typename S, int ACT, bool KEEP>
 __global__ __launch_bounds__(S::THREADS, S::simd) void ffn_up_kernel(TileArgs g, typename EpiAct<ACT, KEEP>::Args args, PieceArgs p) {
   const int tiles = gridDim.x - p.pieces;
@@ -248,12 +181,10 @@ __global__ __launch_bounds__(S::THREADS, S::simd) void ffn_up_kernel(TileArgs g,
 }
 
 template <typename S, int ACT>
-__global__ __launch_bounds__(S::THREADS, S::simd) void ffn_dh_kernel(TileArgs g, ActBwdArgs args, PieceArgs p, ColArgs<bf16_t> c) {
-  const int tiles = gridDim.x - p.pieces - c.pieces;
+__global__ __launch_bounds__(S::THREADS, S::simd) void ffn_dh_kernel(TileArgs g, ActBwdArgs args, PieceArgs p) {
+  const int tiles = gridDim.x - p.pieces;
   if ((int)blockIdx.x >= tiles) {
-    const int piece = blockIdx.x - tiles;
-    if (piece < p.pieces) piece_8<S::THREADS, false>(p, piece);
-    else piece_columns<S::THREADS>(c, piece - p.pieces);
+    piece_8<S::THREADS, false>(p, blockIdx.x - tiles);
     return;
   }
   int M, K;
@@ -282,8 +213,14 @@ __global__ __launch_bounds__(S::THREADS, S::simd) void ffn_grads_kernel(TileArgs
 }
 
 // ---- fp32: column sums of dh and dy (grid: columns / 64, pieces, matrices), rows in order
-__global__ __launch_bounds__(256) void ffn_columns_f32_kernel(ColArgs<float> c0, ColArgs<float> c1) {
-  const ColArgs<float> c = blockIdx.z ? c1 : c0;
+struct ColArgs {
+  const float* src;
+  float* part;                 // [pieces][d]
+  int B, n, d, pieces;
+  const int32_t* n_dev;
+};
+__global__ __launch_bounds__(256) void ffn_columns_f32_kernel(ColArgs c0, ColArgs c1) {
+  const ColArgs c = blockIdx.z ? c1 : c0;
   int n;
   if (!c.src || !vd_count(c.n_dev, c.n, n)) return;
   const int col = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
@@ -313,15 +250,14 @@ __global__ __launch_bounds__(256) void ffn_columns_f32_kernel(ColArgs<float> c0,
 // threads for each)
 struct FinishArgs {
   const float* part[2];        // [slices][count]; null: already there
-  const float* col[2];         // [pieces][cols]; null: not wanted
+  float* col[2];               // [pieces][cols]; null: not wanted
   void* dW[2];
   void* db[2];
   int cols[2], pieces[2];
-  int band;                    // rows of a piece of db1 (0: pieces[0] of them whatever the count)
   long long count;
   int slices, blocks, bf16;    // blocks: workgroups of a weight
   const int32_t* n_dev;
-  int B, n;
+  int n;
 };
 __global__ __launch_bounds__(256) void ffn_finish_kernel(FinishArgs f) {
   int n;
@@ -354,8 +290,8 @@ __global__ __launch_bounds__(256) void ffn_finish_kernel(FinishArgs f) {
   __shared__ float red[16][17];
   const int at = blockIdx.x - weights, b0 = f.col[0] ? (f.cols[0] + 15) / 16 : 0, z = at >= b0;
   const int c = threadIdx.x & 15, group = threadIdx.x >> 4, cols = z ? f.cols[1] : f.cols[0], column = (at - z * b0) * 16 + c;
+  const int pieces = z ? f.pieces[1] : f.pieces[0];
   const float* p = (z ? f.col[1] : f.col[0]) + min(column, cols - 1);
-  const int pieces = z || !f.band ? (z ? f.pieces[1] : f.pieces[0]) : (int)(((long long)f.B * n + f.band - 1) / f.band);
   float s = 0.f;
   int k = group;
   for (; k + 48 < pieces; k += 64) {
@@ -388,20 +324,25 @@ int check_sizes(int B, int n, int d, int f, int dtype) {
 }
 // ---- plans: which tile, how many slices.  What a tile of BM x BN over K costs beside others of its kind, in products of 32 x 32 x 1 of a
 // chip whose every place is taken; its start and end cost as much as kEnds of K.
-constexpr double kEnds = 200;
+constexpr double kEnds = 250;
 struct ShapeCost {
   int BM, BN, places;          // places: workgroups that are resident together on 256 compute units
   double rate;                 // of the largest tile's
 };
-constexpr ShapeCost kShapes[3] = {{64, 128, 512, 0.62}, {128, 128, 512, 0.87}, {256, 256, 256, 1.0}};
+// Products whose rows are worked on take 256 x 128 as their largest, two workgroups a compute unit: while one is at its end the other
+// multiplies.  us, 256 x 256 -> 256 x 128: activation 240 -> 192 (65 536 x 768 x 1536), 103 -> 88 (27 584 x 512 x 2048), its gradient 233 -> 223 and 110 -> 97;
+// but dx 137 -> 161 and 53 -> 69.
+typedef TileShape<256, 128, 4, 2, 64, 3> TileWide;
+constexpr ShapeCost kShapes[3] = {{64, 128, 512, 0.62}, {128, 128, 512, 0.93}, {256, 256, 256, 1.0}};
+constexpr ShapeCost kRowShapes[3] = {{64, 128, 512, 0.62}, {128, 128, 512, 0.93}, {256, 128, 512, 1.0}};
 double tile_time(const ShapeCost& c, double K) { return c.BM * c.BN / 1024.0 * (K + kEnds) * c.places / 512.0 / c.rate; }
 long long tiles_of(const ShapeCost& c, long long M, int N) { return (M + c.BM - 1) / c.BM * vd_ceil_div(N, c.BN); }
-int product_shape(long long T, int N, int K) {
+int product_shape(const ShapeCost (&shapes)[3], long long T, int N, int K) {
   int best = 0;
   double least = 0;
   for (int i = 0; i < 3; ++i) {
-    const long long rounds = (tiles_of(kShapes[i], T, N) + kShapes[i].places - 1) / kShapes[i].places;
-    const double t = rounds * tile_time(kShapes[i], K);
+    const long long rounds = (tiles_of(shapes[i], T, N) + shapes[i].places - 1) / shapes[i].places;
+    const double t = rounds * tile_time(shapes[i], K);
     if (i == 0 || t < least) {
       least = t;
       best = i;
@@ -474,8 +415,9 @@ FfnWorkspace ffn_workspace(long long T, int d, int f, int dtype) {
   const size_t slices = dtype == VARDROP_BF16 ? most_slices(T) : vd_f32_splitk(d, f, 1, T);
   w.part = take(slices * d * f * 4);
   w.second = take(slices * d * f * 4);
-  w.col = take((dtype == VARDROP_BF16 ? (size_t)(T + 63) / 64 * 2 : (size_t)kColPieces) * f * 4);
-  w.col2 = take((size_t)kColPieces * d * 4);
+  // column sums: two pieces for each slice and row of tiles at most
+  w.col = take((dtype == VARDROP_BF16 ? slices * vd_ceil_div(d, 64) * 2 : (size_t)kColPieces) * f * 4);
+  w.col2 = take((dtype == VARDROP_BF16 ? slices * vd_ceil_div(f, 64) * 2 : (size_t)kColPieces) * d * 4);
   w.total = at;
   return w;
 }
@@ -486,6 +428,7 @@ struct FfnCall {
   long long T;
   VdDevCount dn;
   hipStream_t s;
+  int past(int N) const { return T * N * 2 >= kPastCaches; }
 };
 
 // C [T][N] = A B, over the tokens
@@ -529,20 +472,21 @@ int launch_up(const FfnCall& c, const TileArgs& g, const typename EpiAct<ACT, KE
   VD_FFN_LAUNCH(VARDROP_K_FFN_UP, (ffn_up_kernel<S, ACT, KEEP>), S, tile_count<S>(g, g.M) + p.pieces, g, e, p)
 }
 template <typename S, int ACT>
-int launch_dh(const FfnCall& c, const TileArgs& g, const ActBwdArgs& e, PieceArgs p, const ColArgs<bf16_t>& col, int* band) {
+int launch_dh(const FfnCall& c, const TileArgs& g, const ActBwdArgs& e, PieceArgs p) {
   p.pieces = pieces_8(c.T * c.d / 8, S::THREADS);
-  *band = S::MI * 32;
-  VD_FFN_LAUNCH(VARDROP_K_FFN_DH, (ffn_dh_kernel<S, ACT>), S, tile_count<S>(g, g.M) + p.pieces + col.pieces, g, e, p, col)
+  VD_FFN_LAUNCH(VARDROP_K_FFN_DH, (ffn_dh_kernel<S, ACT>), S, tile_count<S>(g, g.M) + p.pieces, g, e, p)
 }
 template <typename S>
 int launch_grads(const FfnCall& c, const TileArgs& gx, const EpiOut::Args& ax, const TileArgs& g1, const EpiGrad::Args& a1, const TileArgs& g2,
-                 const EpiGrad::Args& a2) {
+                 const EpiGrad::Args& a2, int (&pieces)[2]) {
+  pieces[0] = tile_pieces<S>(g1);
+  pieces[1] = tile_pieces<S>(g2);
   VD_FFN_LAUNCH(VARDROP_K_FFN_GRADS, ffn_grads_kernel<S>, S, (gx.A ? tile_count<S>(gx, gx.M) : 0) + tile_count<S>(g1, g1.M) + tile_count<S>(g2, g2.M), gx, ax, g1,
                 a1, g2, a2)
 }
 #undef VD_FFN_LAUNCH
-// a call of CALL<Tile64>, <Tile128> or <Tile256>
-#define VD_BY_SHAPE(SHAPE, CALL) ((SHAPE) == 0 ? CALL(Tile64) : (SHAPE) == 1 ? CALL(Tile128) : CALL(Tile256))
+// a call of CALL for the tile of kShapes, or with WIDE = TileWide of kRowShapes
+#define VD_BY_SHAPE(SHAPE, CALL, WIDE) ((SHAPE) == 0 ? CALL(Tile64) : (SHAPE) == 1 ? CALL(Tile128) : CALL(WIDE))
 
 template <int ACT>
 int fwd_bf16(const FfnCall& c, const void* x, const void* W1, const void* b1, const void* W2, const void* b2, void* y, uint8_t* kept, uint8_t* hc,
@@ -553,66 +497,61 @@ int fwd_bf16(const FfnCall& c, const void* x, const void* W1, const void* b1, co
   p.x = (const bf16_t*)x; p.codes = kept; p.exps = kept ? kept + pack_exponents_at(c.T, c.d) : nullptr;
   p.B = c.B; p.n = c.n; p.d = c.d; p.n_dev = c.dn.dev;
   const TileArgs up = rows_product(c, x, W1, false, c.d, c.f, true);
-  const int shape = product_shape(c.T, c.f, c.d);
+  const int shape = product_shape(kRowShapes, c.T, c.f, c.d);
   int rc;
   if (kept) {
-    const typename EpiAct<ACT, true>::Args e = {a, (const bf16_t*)b1, hc, he, c.f};
+    const typename EpiAct<ACT, true>::Args e = {a, (const bf16_t*)b1, hc, he, c.f, c.past(c.f)};
 #define VD_CALL(S) launch_up<S, ACT, true>(c, up, e, p)
-    rc = VD_BY_SHAPE(shape, VD_CALL);
+    rc = VD_BY_SHAPE(shape, VD_CALL, TileWide);
 #undef VD_CALL
   } else {
-    const typename EpiAct<ACT, false>::Args e = {a, (const bf16_t*)b1, nullptr, nullptr, c.f};
+    const typename EpiAct<ACT, false>::Args e = {a, (const bf16_t*)b1, nullptr, nullptr, c.f, c.past(c.f)};
 #define VD_CALL(S) launch_up<S, ACT, false>(c, up, e, p)
-    rc = VD_BY_SHAPE(shape, VD_CALL);
+    rc = VD_BY_SHAPE(shape, VD_CALL, TileWide);
 #undef VD_CALL
   }
   if (rc) return rc;
   const TileArgs down = rows_product(c, a, W2, false, c.f, c.d, false);
-  const EpiOut::Args e = {(bf16_t*)y, (const bf16_t*)b2, c.d};
+  const EpiOut::Args e = {(bf16_t*)y, (const bf16_t*)b2, c.d, c.past(c.d)};
 #define VD_CALL(S) launch_tile_gemm<false, true, false, S, EpiOut>(c.ctx, VARDROP_K_FFN_DOWN, down, e, c.s)
-  return VD_BY_SHAPE(product_shape(c.T, c.d, c.f), VD_CALL);
+  return VD_BY_SHAPE(product_shape(kShapes, c.T, c.d, c.f), VD_CALL, Tile256);
 #undef VD_CALL
 }
 
 template <int ACT>
-int bwd_bf16(const FfnCall& c, const void* dy, const void* W1, const void* W2, const uint8_t* saved, void* dx, void* dW1, void* dW2, bool db1, bool db2,
+int bwd_bf16(const FfnCall& c, const void* dy, const void* W1, const void* W2, const uint8_t* saved, void* dx, void* dW1, void* dW2, void* db1, void* db2,
              int grad_dtype, char* ws, FinishArgs& fin) {
   const FfnWorkspace w = ffn_workspace(c.T, c.d, c.f, c.dtype);
   const uint8_t* hc = saved + pack_bytes(c.T, c.d);
   bf16_t *dh = (bf16_t*)(ws + w.wide), *a = (bf16_t*)(ws + w.act), *xv = (bf16_t*)(ws + w.x);
   float *part = (float*)(ws + w.part), *second = (float*)(ws + w.second), *col = (float*)(ws + w.col), *col2 = (float*)(ws + w.col2);
-  int rc;
   if (c.T > 0) {
     PieceArgs p = {};
     p.values = xv; p.codes = const_cast<uint8_t*>(saved); p.exps = const_cast<uint8_t*>(saved) + pack_exponents_at(c.T, c.d);
     p.B = c.B; p.n = c.n; p.d = c.d; p.n_dev = c.dn.dev;
-    const ColArgs<bf16_t> cols = {(const bf16_t*)dy, col2, c.B, c.n, c.d, db2 ? column_pieces(c.T) : 0, c.dn.dev};
     const TileArgs g = rows_product(c, dy, W2, true, c.d, c.f, true);
-    const ActBwdArgs e2 = {dh, a, hc, hc + pack_exponents_at(c.T, c.f), db1 ? col : nullptr, c.f};
-#define VD_CALL(S) launch_dh<S, ACT>(c, g, e2, p, cols, &fin.band)
-    rc = VD_BY_SHAPE(product_shape(c.T, c.f, c.d), VD_CALL);
+    const ActBwdArgs e = {dh, a, hc, hc + pack_exponents_at(c.T, c.f), c.f, c.past(c.f)};
+#define VD_CALL(S) launch_dh<S, ACT>(c, g, e, p)
+    const int rc = VD_BY_SHAPE(product_shape(kRowShapes, c.T, c.f, c.d), VD_CALL, TileWide);
 #undef VD_CALL
     if (rc) return rc;
-    fin.col[0] = db1 ? col : nullptr;
-    fin.col[1] = db2 ? col2 : nullptr;
-    fin.pieces[1] = cols.pieces;
-  } else {                       // (no tokens: sums over no pieces)
-    fin.col[0] = db1 ? col : nullptr;
-    fin.col[1] = db2 ? col2 : nullptr;
   }
   const GradPlan plan = plan_grads(c.T, c.d, c.f);
-  fin.slices = plan.slices;
-  if (plan.slices > 1) {
+  const bool split = plan.slices > 1, low = grad_dtype == VARDROP_BF16;
+  if (split) {
     fin.part[0] = part;
     fin.part[1] = second;
+    fin.slices = plan.slices;
   }
-  const bool split = plan.slices > 1, low = grad_dtype == VARDROP_BF16;
+  fin.col[0] = db1 ? col : nullptr;
+  fin.col[1] = db2 ? col2 : nullptr;
   const TileArgs gx = dx && c.T > 0 ? rows_product(c, dh, W1, true, c.f, c.d, false) : TileArgs{};
   const TileArgs g1 = tokens_product(c, xv, dh, c.d, c.f, plan.slices), g2 = tokens_product(c, a, dy, c.f, c.d, plan.slices);
-  const EpiOut::Args ax = {(bf16_t*)dx, nullptr, c.d};
-  const EpiGrad::Args a1 = {dW1, split ? part : nullptr, c.d, c.f, low}, a2 = {dW2, split ? second : nullptr, c.f, c.d, low};
-#define VD_CALL(S) launch_grads<S>(c, gx, ax, g1, a1, g2, a2)
-  return VD_BY_SHAPE(plan.shape, VD_CALL);
+  const EpiOut::Args ax = {(bf16_t*)dx, nullptr, c.d, c.past(c.d)};
+  const EpiGrad::Args a1 = {dW1, split ? part : nullptr, fin.col[0], c.d, c.f, low};
+  const EpiGrad::Args a2 = {dW2, split ? second : nullptr, fin.col[1], c.f, c.d, low};
+#define VD_CALL(S) launch_grads<S>(c, gx, ax, g1, a1, g2, a2, fin.pieces)
+  return VD_BY_SHAPE(plan.shape, VD_CALL, Tile256);
 #undef VD_CALL
 }
 
@@ -670,8 +609,8 @@ int bwd_f32(const FfnCall& c, const float* dy, const float* W1, const float* W2,
   fin.col[1] = db2 ? (float*)(ws + w.col2) : nullptr;
   if (c.T == 0) return VARDROP_OK;       // (sums over no pieces)
   fin.pieces[0] = fin.pieces[1] = pieces;
-  const ColArgs<float> c0 = {db1 ? dh : nullptr, (float*)(ws + w.col), c.B, c.n, c.f, pieces, c.dn.dev};
-  const ColArgs<float> c1 = {db2 ? dy : nullptr, (float*)(ws + w.col2), c.B, c.n, c.d, pieces, c.dn.dev};
+  const ColArgs c0 = {db1 ? dh : nullptr, (float*)(ws + w.col), c.B, c.n, c.f, pieces, c.dn.dev};
+  const ColArgs c1 = {db2 ? dy : nullptr, (float*)(ws + w.col2), c.B, c.n, c.d, pieces, c.dn.dev};
   VdTimer timer(c.ctx, VARDROP_K_FFN_BIAS, c.s);
   VD_KERNEL(c.ctx, ffn_columns_f32_kernel, dim3((unsigned)vd_ceil_div(c.d > c.f ? c.d : c.f, 64), (unsigned)pieces, 2), dim3(256), 0, c.s, c0, c1);
   VD_LAUNCH_CHECK(c.ctx);
@@ -724,18 +663,18 @@ int backward(vardrop_ctx* ctx, const void* dy, int B, int n, int d, int f, int d
   fin.slices = 1;
   fin.cols[0] = f; fin.cols[1] = d;
   if (dtype == VARDROP_BF16) {
-    rc = act == VARDROP_ACT_RELU ? bwd_bf16<kActRelu>(c, dy, W1, W2, xc, dx, dW1, dW2, db1 != nullptr, db2 != nullptr, grad_dtype, at, fin)
-                                 : bwd_bf16<kActGelu>(c, dy, W1, W2, xc, dx, dW1, dW2, db1 != nullptr, db2 != nullptr, grad_dtype, at, fin);
+    rc = act == VARDROP_ACT_RELU ? bwd_bf16<kActRelu>(c, dy, W1, W2, xc, dx, dW1, dW2, db1, db2, grad_dtype, at, fin)
+                                 : bwd_bf16<kActGelu>(c, dy, W1, W2, xc, dx, dW1, dW2, db1, db2, grad_dtype, at, fin);
   } else {
     rc = bwd_f32(c, (const float*)dy, (const float*)W1, (const float*)W2, xc, (float*)dx, (float*)dW1, (float*)dW2, db1 != nullptr, db2 != nullptr, at, fin);
   }
-  if (rc || (!fin.part[0] && !db1 && !db2)) return rc;
+  if (rc || (!fin.part[0] && !fin.col[0] && !fin.col[1])) return rc;
   fin.dW[0] = dW1; fin.dW[1] = dW2; fin.db[0] = db1; fin.db[1] = db2;
   fin.count = (long long)d * f;
-  fin.bf16 = grad_dtype == VARDROP_BF16; fin.n_dev = dn.dev; fin.B = B; fin.n = n;
+  fin.bf16 = grad_dtype == VARDROP_BF16; fin.n_dev = dn.dev; fin.n = n;
   const long long blocks = (fin.count / 4 + 255) / 256;
   fin.blocks = blocks > 1024 ? 1024 : (int)blocks;
-  const int grid = (fin.part[0] ? 2 * fin.blocks : 0) + (db1 ? vd_ceil_div(f, 16) : 0) + (db2 ? vd_ceil_div(d, 16) : 0);
+  const int grid = (fin.part[0] ? 2 * fin.blocks : 0) + (fin.col[0] ? vd_ceil_div(f, 16) : 0) + (fin.col[1] ? vd_ceil_div(d, 16) : 0);
   VdTimer timer(ctx, VARDROP_K_REDUCE_DW, s);
   VD_KERNEL(ctx, ffn_finish_kernel, dim3((unsigned)grid), dim3(256), 0, s, fin);
   VD_LAUNCH_CHECK(ctx);

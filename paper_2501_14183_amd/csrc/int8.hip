@@ -121,12 +121,13 @@ __device__ inline float i8_act(float v, int act) {
 
 template <typename T>
 struct EpiI8 {
-  static constexpr bool kFetch = false;
+  static constexpr bool kFetch = false, kSums = false;
   struct Args {
     T* y;
     const float *sx, *sw;      // sx[0] is row m0's
     const T* bias;
     int m0, N, act, whole;     // whole: rows of y can be stored in groups of eight
+    int past;
   } a;
   float w[8], b[8];
   __device__ void columns(int n, int N) {
@@ -136,7 +137,6 @@ struct EpiI8 {
       b[e] = a.bias && n + e < N ? to_float(a.bias[n + e]) : 0.f;
     }
   }
-  __device__ void done(int, int, bool) {}
   __device__ void row(int, int, int m, int n, bool live, float (&v)[8]) {
     if (!live) return;
     const float s = a.sx[m - a.m0];
@@ -151,7 +151,7 @@ struct EpiI8 {
     }
     T* p = a.y + (long long)m * a.N + n;
     if (a.whole) {
-      store_eight(p, v);
+      store_eight(p, v, a.past);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -181,8 +181,12 @@ int i8_product(const I8Call& c) {
   g.K = i8_pitch(c.K);
   g.lda = g.ldb = g.K;
   g.M = c.rows; g.N = c.N; g.slices = 1;
-  const typename EpiI8<T>::Args epi = {(T*)c.y, c.sx, c.scale, (const T*)c.bias, 0, c.N, c.act, c.N % 8 == 0 && vd_aligned(c.y, 16)};
+  const typename EpiI8<T>::Args epi = {(T*)c.y, c.sx, c.scale, (const T*)c.bias, 0, c.N, c.act, c.N % 8 == 0 && vd_aligned(c.y, 16),
+                                      (long long)c.rows * c.N * (long long)sizeof(T) >= kPastCaches};
   const long long t128 = (long long)vd_ceil_div(c.N, 128) * vd_ceil_div(c.rows, 128);
+#ifdef I8SHAPE
+  return launch_tile_gemm<true, true, true, I8SHAPE, EpiI8<T>>(c.ctx, VARDROP_K_LINEAR_I8, g, epi, c.s);
+#endif
   if (t128 >= 512) return launch_tile_gemm<true, true, true, Tile128, EpiI8<T>>(c.ctx, VARDROP_K_LINEAR_I8, g, epi, c.s);
   return launch_tile_gemm<true, true, true, Tile64, EpiI8<T>>(c.ctx, VARDROP_K_LINEAR_I8, g, epi, c.s);
 }
@@ -366,7 +370,7 @@ __global__ __launch_bounds__(256) void i8_few_kernel(const X* x, int rows, int K
 
 template <typename X, typename T>
 int i8_one_launch(const I8Call& c) {
-  const typename EpiI8<T>::Args a = {(T*)c.y, nullptr, c.scale, (const T*)c.bias, 0, c.N, c.act, c.N % 8 == 0 && vd_aligned(c.y, 16)};
+  const typename EpiI8<T>::Args a = {(T*)c.y, nullptr, c.scale, (const T*)c.bias, 0, c.N, c.act, c.N % 8 == 0 && vd_aligned(c.y, 16), 0};
   const X* x = (const X*)c.x;
   if (c.rows <= kFewRows && i8_pitch(c.K) <= kFewPitch) {
     const dim3 grid((unsigned)vd_ceil_div(c.N, 16));

@@ -77,6 +77,17 @@ __device__ inline intx16 tile_mfma(const Frag& a, const Frag& b, intx16 c) {
   return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(intx4, a.q), __builtin_bit_cast(intx4, b.q), c, 0, 0, 0);
 }
 
+// sum of the eight bf16 numbers of a fragment
+__device__ inline float eight_sum(const Frag& f) {
+  float lo = 0.f, hi = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    lo += __uint_as_float(f.w[e] << 16);
+    hi += __uint_as_float(f.w[e] & 0xffff0000u);
+  }
+  return lo + hi;
+}
+
 // The end of a tile: 32 rows x 32 NJ columns of a wavefront at a time through its own part of LDS (`smem`: 32 PITCH bytes a wavefront).
 // acc[i][j] element 4 q + e is row i * 32 + lane % 32, column j * 32 + 8 q + 4 (lane / 32) + e; back come eight columns a lane, the lanes of
 // a row beside each other.
@@ -131,12 +142,13 @@ __device__ __forceinline__ void tile_finish(const Sum (&acc)[S::MI][S::NJ], unsi
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
   }
-  epi.done(m0 / (MI * 32) + wm, n, n < N);
 }
 
 // AKC, BKC: operand contiguous along k.  Epi: `columns(n, N)` once, then `row(slice, k, m, n, live, v)` with eight sums of row m from
-// column n on, for every row of the tile (k counts a wavefront's); `live` is false outside the result, lanes of one row and block of 32 columns come together.  Last
-// `done(band, n, live)`: the wavefront's rows were those of this band of 32 MI rows; lanes 8 / NJ .. apart hold the same columns.
+// column n on, for every row of the tile (k counts a wavefront's); `live` is false outside the result, lanes of one row and block of 32 columns come together.
+// Epi::kSums (B not k-contiguous): column sums of B, from the fragments that are multiplied.  The tiles above each other share the stages
+// among them and their wavefronts above each other the steps, so that none is held up; what one has goes to `sums(piece, n, live, v)`,
+// tile_pieces() of them for a column.
 // t: the tile, n fastest, then m, then slice.
 template <bool I8, bool AKC, bool BKC, typename S, typename Epi>
 __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi::Args& args, int M, int K, int t) {
@@ -220,6 +232,10 @@ __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi:
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
 
+  float csum[NJ];
+  int next_sum = m0 / BM;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) csum[j] = 0.f;
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s)
     if (s < nk) issue(s, s);
@@ -260,7 +276,9 @@ __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi:
             }
           }
         };
-        auto multiply = [&](auto pending, int set) {
+        const bool summing = Epi::kSums && k == next_sum;
+        if (summing) next_sum += gy;
+        auto multiply = [&](auto pending, int set, int ks) {
           wait_lds_count<decltype(pending)::value>();
 #pragma unroll
           for (int i = 0; i < MI; ++i) tie(fa[set][i]);
@@ -270,23 +288,38 @@ __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi:
           for (int i = 0; i < MI; ++i)
 #pragma unroll
             for (int j = 0; j < NJ; ++j) acc[i][j] = tile_mfma(fb[set][j], fa[set][i], acc[i][j]);
+          if constexpr (Epi::kSums) {
+            if (summing && ks % S::WR == wm) {
+#pragma unroll
+              for (int j = 0; j < NJ; ++j) csum[j] += eight_sum(fb[set][j]);
+            }
+          }
           __builtin_amdgcn_sched_barrier(0);
         };
         read(Int<0>{}, 0);
         read(Int<1>{}, 1);
-        multiply(Int<OPK>{}, 0);
+        multiply(Int<OPK>{}, 0, 0);
         if constexpr (KS == 4) {
           read(Int<2>{}, 0);
-          multiply(Int<OPK>{}, 1);
+          multiply(Int<OPK>{}, 1, 1);
           read(Int<3>{}, 1);
-          multiply(Int<OPK>{}, 0);
+          multiply(Int<OPK>{}, 0, 2);
         }
-        multiply(Int<0>{}, 1);
+        multiply(Int<0>{}, 1, KS - 1);
       }
     }
   }
   __syncthreads();                                // every wavefront is done reading the last stage
   Epi epi{args};
+  if constexpr (Epi::kSums) {
+    static_assert(KS % S::WR == 0, "steps for every row of wavefronts");
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const float sum = csum[j] + __shfl_xor(csum[j], 32, 64);
+      const int n = n0 + wn * (NJ * 32) + j * 32 + col;
+      epi.sums((slice * gy + m0 / BM) * S::WR + wm, n, lane < 32 && n < g.N, sum);
+    }
+  }
   tile_finish<S, Epi>(acc, smem, epi, slice, M, g.N, m0, n0);
 }
 
@@ -300,6 +333,8 @@ __device__ __forceinline__ bool tile_dims(const TileArgs& g, int& M, int& K) {
   (g.n_role == 0 ? M : K) = g.n_mul * n;
   return true;
 }
+template <typename S>
+inline int tile_pieces(const TileArgs& g) { return g.slices * ((g.M + S::BM - 1) / S::BM) * S::WR; }
 template <typename S>
 __host__ __device__ inline long long tile_count(const TileArgs& g, int M) {
   return (long long)((g.N + S::BN - 1) / S::BN) * ((M + S::BM - 1) / S::BM) * g.slices;
