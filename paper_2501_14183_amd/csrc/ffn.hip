@@ -322,34 +322,7 @@ int check_sizes(int B, int n, int d, int f, int dtype) {
   if (dtype == VARDROP_BF16 && (d % 64 != 0 || f % 64 != 0)) return VARDROP_EUNSUPPORTED;
   return VARDROP_OK;
 }
-// ---- plans: which tile, how many slices.  What a tile of BM x BN over K costs beside others of its kind, in products of 32 x 32 x 1 of a
-// chip whose every place is taken; its start and end cost as much as kEnds of K.
-constexpr double kEnds = 250;
-struct ShapeCost {
-  int BM, BN, places;          // places: workgroups that are resident together on 256 compute units
-  double rate;                 // of the largest tile's
-};
-// Products whose rows are worked on take 256 x 128 as their largest, two workgroups a compute unit: while one is at its end the other
-// multiplies.  us, 256 x 256 -> 256 x 128: activation 240 -> 192 (65 536 x 768 x 1536), 103 -> 88 (27 584 x 512 x 2048), its gradient 233 -> 223 and 110 -> 97;
-// but dx 137 -> 161 and 53 -> 69.
-typedef TileShape<256, 128, 4, 2, 64, 3> TileWide;
-constexpr ShapeCost kShapes[3] = {{64, 128, 512, 0.62}, {128, 128, 512, 0.93}, {256, 256, 256, 1.0}};
-constexpr ShapeCost kRowShapes[3] = {{64, 128, 512, 0.62}, {128, 128, 512, 0.93}, {256, 128, 512, 1.0}};
-double tile_time(const ShapeCost& c, double K) { return c.BM * c.BN / 1024.0 * (K + kEnds) * c.places / 512.0 / c.rate; }
-long long tiles_of(const ShapeCost& c, long long M, int N) { return (M + c.BM - 1) / c.BM * vd_ceil_div(N, c.BN); }
-int product_shape(const ShapeCost (&shapes)[3], long long T, int N, int K) {
-  int best = 0;
-  double least = 0;
-  for (int i = 0; i < 3; ++i) {
-    const long long rounds = (tiles_of(shapes[i], T, N) + shapes[i].places - 1) / shapes[i].places;
-    const double t = rounds * tile_time(shapes[i], K);
-    if (i == 0 || t < least) {
-      least = t;
-      best = i;
-    }
-  }
-  return best;
-}
+// ---- the plan of the gradients' launch
 // The launch of dx (T x d over f) and of the weight gradients (2 d f over T in slices): time until the last place is done when the longer
 // tiles come first, and the sum of the slices behind it.
 constexpr int kMostSlices = 16, kLeastSlice = 256;
@@ -485,8 +458,6 @@ int launch_grads(const FfnCall& c, const TileArgs& gx, const EpiOut::Args& ax, c
                 a1, g2, a2)
 }
 #undef VD_FFN_LAUNCH
-// a call of CALL for the tile of kShapes, or with WIDE = TileWide of kRowShapes
-#define VD_BY_SHAPE(SHAPE, CALL, WIDE) ((SHAPE) == 0 ? CALL(Tile64) : (SHAPE) == 1 ? CALL(Tile128) : CALL(WIDE))
 
 template <int ACT>
 int fwd_bf16(const FfnCall& c, const void* x, const void* W1, const void* b1, const void* W2, const void* b2, void* y, uint8_t* kept, uint8_t* hc,

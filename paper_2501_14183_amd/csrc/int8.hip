@@ -183,12 +183,9 @@ int i8_product(const I8Call& c) {
   g.M = c.rows; g.N = c.N; g.slices = 1;
   const typename EpiI8<T>::Args epi = {(T*)c.y, c.sx, c.scale, (const T*)c.bias, 0, c.N, c.act, c.N % 8 == 0 && vd_aligned(c.y, 16),
                                       (long long)c.rows * c.N * (long long)sizeof(T) >= kPastCaches};
-  const long long t128 = (long long)vd_ceil_div(c.N, 128) * vd_ceil_div(c.rows, 128);
-#ifdef I8SHAPE
-  return launch_tile_gemm<true, true, true, I8SHAPE, EpiI8<T>>(c.ctx, VARDROP_K_LINEAR_I8, g, epi, c.s);
-#endif
-  if (t128 >= 512) return launch_tile_gemm<true, true, true, Tile128, EpiI8<T>>(c.ctx, VARDROP_K_LINEAR_I8, g, epi, c.s);
-  return launch_tile_gemm<true, true, true, Tile64, EpiI8<T>>(c.ctx, VARDROP_K_LINEAR_I8, g, epi, c.s);
+#define VD_CALL(S) launch_tile_gemm<true, true, true, S, EpiI8<T>>(c.ctx, VARDROP_K_LINEAR_I8, g, epi, c.s)
+  return VD_BY_SHAPE(product_shape(kRowShapes, c.rows, c.N, g.K / 2), VD_CALL, TileWide);
+#undef VD_CALL
 }
 
 // ---- quantisation and product in one launch, while a tile's rows of codes fit LDS beside the stages of the weight: every workgroup makes
@@ -452,7 +449,7 @@ extern "C" int vardrop_linear_i8(vardrop_ctx* ctx, const void* x, const float* s
                                  const float* scale, const void* bias, int act, void* y, int dtype, void* ws, size_t ws_bytes, void* stream) {
   if (!ctx || rows < 0 || K < 1 || N < 1 || !is_type(dtype) || (!is_type(x_dtype) && x_dtype != VARDROP_I8)) return VARDROP_EINVAL;
   if (act != VARDROP_ACT_NONE && act != VARDROP_ACT_RELU && act != VARDROP_ACT_GELU) return VARDROP_EINVAL;
-  if (K > kMaxI8K || (long long)vd_ceil_div(rows, 64) * vd_ceil_div(N, 128) >= (1ll << 31)) return VARDROP_EUNSUPPORTED;
+  if (K > kMaxI8K || (long long)vd_ceil_div(rows, 64) * vd_ceil_div(N, 64) >= (1ll << 31)) return VARDROP_EUNSUPPORTED;
   if ((x_dtype == VARDROP_I8) != (sx != nullptr) && rows > 0) return VARDROP_EINVAL;
   if (rows == 0) return VARDROP_OK;
   if (!x || !codes || !scale || !y || x == y) return VARDROP_EINVAL;

@@ -45,9 +45,44 @@ struct TileShape {
   static constexpr int simd = per_cu * WAVES / 4 > 0 ? per_cu * WAVES / 4 : 1;
 };
 
-typedef TileShape<64, 128, 2, 2, 128, 3> Tile64;
+typedef TileShape<64, 64, 2, 2, 128, 4> Tile64;
 typedef TileShape<128, 128, 2, 2, 128, 2> Tile128;
+typedef TileShape<256, 128, 4, 2, 64, 3> TileWide;
 typedef TileShape<256, 256, 2, 4, 128, 2> Tile256;
+
+// ---- which tile.  What a tile of BM x BN over K (of 2 bytes) costs beside others of its kind, in products of 32 x 32 x 1 of a
+// chip whose every place is taken; its start and end cost as much as kEnds of K.
+constexpr double kEnds = 250;
+struct ShapeCost {
+  int BM, BN, places;          // places: workgroups that are resident together on 256 compute units
+  double rate;                 // of the largest tile's
+};
+// Products whose rows are worked on take 256 x 128 as their largest, two workgroups a compute unit: while one is at its end the other
+// multiplies.  us, 256 x 256 -> 256 x 128: activation 240 -> 192 (65 536 x 768 x 1536), 103 -> 88 (27 584 x 512 x 2048), its gradient 233 -> 223 and 110 -> 97;
+// but dx 137 -> 161 and 53 -> 69.  8-bit products, 128 x 128 -> 256 x 128: 81 -> 72 (27 584 x 512 x 2048), 34.5 -> 28.2 (65 536 x 128 x 768).
+// Few rows take 64 x 64, four stages deep: us, 64 x 128 in three -> 64 x 64 in four: activation 8.0 -> 7.3 (2784 x 512 x 512), 7.4 -> 5.8 (300 x 512 x
+// 2048), dx there 6.2 -> 5.9 and 12.8 -> 9.5.
+constexpr ShapeCost kShapes[3] = {{64, 64, 512, 0.5}, {128, 128, 512, 0.93}, {256, 256, 256, 1.0}};
+constexpr ShapeCost kRowShapes[3] = {{64, 64, 512, 0.5}, {128, 128, 512, 0.93}, {256, 128, 512, 1.0}};
+inline double tile_time(const ShapeCost& c, double K) { return c.BM * c.BN / 1024.0 * (K + kEnds) * c.places / 512.0 / c.rate; }
+inline long long tiles_of(const ShapeCost& c, long long M, int N) { return (M + c.BM - 1) / c.BM * vd_ceil_div(N, c.BN); }
+inline int product_shape(const ShapeCost (&shapes)[3], long long T, int N, int K) {
+  int best = 0;
+  double least = 0;
+  for (int i = 0; i < 3; ++i) {
+    // (workgroups end at different times: the last round is seldom a whole one longer)
+    const double rounds = (double)tiles_of(shapes[i], T, N) / shapes[i].places;
+    const double t = (rounds <= 1 ? 1 : rounds + 0.3) * tile_time(shapes[i], K);
+    if (i == 0 || t < least) {
+      least = t;
+      best = i;
+    }
+  }
+  return best;
+}
+// a call of CALL for the tile of kShapes, or with WIDE = TileWide of kRowShapes
+#define VD_BY_SHAPE(SHAPE, CALL, WIDE) ((SHAPE) == 0 ? CALL(Tile64) : (SHAPE) == 1 ? CALL(Tile128) : CALL(WIDE))
+
 
 // Descriptor of the memory from p on, `bytes` long (none: every load gives zero).
 __device__ inline copy_src tile_source(const void* p, long long bytes) {
