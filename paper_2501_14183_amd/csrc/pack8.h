@@ -166,14 +166,4 @@ __device__ inline void from_float(bf16_t* p, float v) { *p = f2bf(v); }
 __device__ inline void from_float(float* p, float v) { *p = v; }
 
 }  // namespace
-
-// ---- element-wise passes (pack8.hip); rows = B * n, or with dn.dev B times what it holds (at most n).  Null pointers: not wanted
-// codes and exponents of x, and act(x) into `a` (which may be x), both of `dtype`; act VARDROP_ACT_NONE with a = nullptr: codes only
-int vd_pack8(vardrop_ctx*, int kid, const void* x, int B, int n, int d, int dtype, int act, void* codes, void* exps, void* a, hipStream_t s,
-             VdDevCount dn);
-// values of a checkpoint into x
-int vd_unpack8(vardrop_ctx*, int kid, const void* codes, const void* exps, int B, int n, int d, int dtype, void* x, hipStream_t s, VdDevCount dn);
-// dh = da * act'(h), a = act(h) with h from its checkpoint (fp32); dh may be da
-int vd_act_bwd_f32(vardrop_ctx*, int kid, const float* da, const void* codes, const void* exps, int B, int n, int d, int act, float* dh, float* a,
-                   hipStream_t s, VdDevCount dn);
 #endif  // VARDROP_PACK8_H

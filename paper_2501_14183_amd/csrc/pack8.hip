@@ -1,4 +1,4 @@
-// Activations in 8 bits (format: pack8.h): pack, unpack, and the element-wise half of an fp32 feed-forward block.
+// Activations in 8 bits (format: pack8.h): pack and unpack.
 //
 // Bound by memory: 2 or 4 bytes an element one way, 33/32 the other.
 #include "pack8.h"
@@ -6,9 +6,8 @@
 namespace {
 
 struct PackArgs {
-  const void* x;             // what is packed; the gradient of the activation backward
-  void* a;                   // activation (forward), values (unpack), activation (backward)
-  void* dh;
+  const void* x;             // what is packed
+  void* values;              // what is unpacked
   uint8_t* codes;
   uint8_t* exps;
   int B, n, d;
@@ -24,7 +23,7 @@ __device__ inline bool pack_rows(const PackArgs& p, long long& rows) {
 }
 
 // Whole blocks (d a multiple of 32): the tensor is one line of groups of eight, a lane each; four lanes are a block.
-template <typename T, int ACT, int U>
+template <typename T, int U>
 __global__ __launch_bounds__(256) void pack8_kernel(PackArgs p) {
   long long rows;
   if (!pack_rows(p, rows)) return;
@@ -44,31 +43,24 @@ __global__ __launch_bounds__(256) void pack8_kernel(PackArgs p) {
     for (int u = 0; u < U; ++u) {
       const long long i = at + u * 256 + threadIdx.x;
       const bool live = i < groups;              // (a block's four lanes agree: groups is a multiple of four)
-      if (p.codes) {
-        uint32_t e;
-        const u32x2 c = pack_eight(v[u], e);
-        if (live) *reinterpret_cast<u32x2*>(p.codes + i * 8) = c;
-        // four exponents of sixteen lanes leave as one word
-        const uint32_t word = e | ((uint32_t)__builtin_amdgcn_mov_dpp((int)e, 0x104, 0xf, 0xf, true) << 8) |
-                              ((uint32_t)__builtin_amdgcn_mov_dpp((int)e, 0x108, 0xf, 0xf, true) << 16) |
-                              ((uint32_t)__builtin_amdgcn_mov_dpp((int)e, 0x10c, 0xf, 0xf, true) << 24);
-        if ((i | 15) < groups) {
-          if ((threadIdx.x & 15) == 0) *reinterpret_cast<uint32_t*>(p.exps + (i >> 2)) = word;
-        } else if (live && (threadIdx.x & 3) == 0) {
-          p.exps[i >> 2] = (uint8_t)e;
-        }
-      }
-      if constexpr (ACT != kActNone) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[u][j] = act_value<ACT, true>(v[u][j]);
-        if (live) store_eight((T*)p.a + i * 8, v[u]);
+      uint32_t e;
+      const u32x2 c = pack_eight(v[u], e);
+      if (live) *reinterpret_cast<u32x2*>(p.codes + i * 8) = c;
+      // four exponents of sixteen lanes leave as one word
+      const uint32_t word = e | ((uint32_t)__builtin_amdgcn_mov_dpp((int)e, 0x104, 0xf, 0xf, true) << 8) |
+                            ((uint32_t)__builtin_amdgcn_mov_dpp((int)e, 0x108, 0xf, 0xf, true) << 16) |
+                            ((uint32_t)__builtin_amdgcn_mov_dpp((int)e, 0x10c, 0xf, 0xf, true) << 24);
+      if ((i | 15) < groups) {
+        if ((threadIdx.x & 15) == 0) *reinterpret_cast<uint32_t*>(p.exps + (i >> 2)) = word;
+      } else if (live && (threadIdx.x & 3) == 0) {
+        p.exps[i >> 2] = (uint8_t)e;
       }
     }
   }
 }
 
 // Any width: half a wavefront a block, a lane a channel.
-template <typename T, int ACT>
+template <typename T>
 __global__ __launch_bounds__(256) void pack8_any_kernel(PackArgs p) {
   long long rows;
   if (!pack_rows(p, rows)) return;
@@ -90,17 +82,12 @@ __global__ __launch_bounds__(256) void pack8_any_kernel(PackArgs p) {
     for (int u = 0; u < U; ++u) {
       const long long b = at + u * 8 + (threadIdx.x >> 5);
       const bool live = b < blocks && c[u] < p.d;
-      if (p.codes) {
-        uint32_t most = magnitude(v[u]);
+      uint32_t most = magnitude(v[u]);
 #pragma unroll
-        for (int m = 1; m < 32; m <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, m, 64));
-        const uint32_t e = pack_exponent(most);
-        if (live) p.codes[row[u] * p.d + c[u]] = (uint8_t)pack_code(e >= 248u ? pack_limit(v[u]) : v[u], pack_up(e));
-        if (live && l == 0) p.exps[b] = (uint8_t)e;
-      }
-      if constexpr (ACT != kActNone) {
-        if (live) from_float((T*)p.a + row[u] * p.d + c[u], act_value<ACT, true>(v[u]));
-      }
+      for (int m = 1; m < 32; m <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, m, 64));
+      const uint32_t e = pack_exponent(most);
+      if (live) p.codes[row[u] * p.d + c[u]] = (uint8_t)pack_code(e >= 248u ? pack_limit(v[u]) : v[u], pack_up(e));
+      if (live && l == 0) p.exps[b] = (uint8_t)e;
     }
   }
 }
@@ -127,14 +114,13 @@ __global__ __launch_bounds__(256) void unpack8_kernel(PackArgs p) {
       if (i < groups) {
         float v[8];
         unpack_eight(c[u], e[u], v);
-        store_eight((T*)p.a + i * 8, v);
+        store_eight((T*)p.values + i * 8, v);
       }
     }
   }
 }
 
-// Any width; with ACT: the activation's backward pass.
-template <typename T, int ACT>
+template <typename T>
 __global__ __launch_bounds__(256) void unpack8_any_kernel(PackArgs p) {
   long long rows;
   if (!pack_rows(p, rows)) return;
@@ -148,15 +134,7 @@ __global__ __launch_bounds__(256) void unpack8_any_kernel(PackArgs p) {
       const int c = (int)(b - row * nb) * kPackBlock + l;
       if (b >= blocks || c >= p.d) continue;
       const long long i = row * p.d + c;
-      const float h = (float)(int8_t)p.codes[i] * pack_step(p.exps[b]);
-      if constexpr (ACT == kActNone) {
-        from_float((T*)p.a + i, h);
-      } else {
-        float slope;
-        const float a = act_both<ACT, true>(h, slope);
-        from_float((T*)p.dh + i, to_float(((const T*)p.x)[i]) * slope);
-        from_float((T*)p.a + i, a);
-      }
+      from_float((T*)p.values + i, (float)(int8_t)p.codes[i] * pack_step(p.exps[b]));
     }
   }
 }
@@ -166,19 +144,19 @@ unsigned pack_grid(long long items, int per_block) {
   return (unsigned)(b > 4096 ? 4096 : b);
 }
 
-template <typename T, int ACT>
-int launch_pack(vardrop_ctx* ctx, int kid, const PackArgs& p, bool whole, long long rows, hipStream_t s) {
-  VdTimer timer(ctx, kid, s);
-  if (whole) VD_KERNEL(ctx, (pack8_kernel<T, ACT, 4>), dim3(pack_grid(rows * (p.d / 8), 1024)), dim3(256), 0, s, p);
-  else VD_KERNEL(ctx, (pack8_any_kernel<T, ACT>), dim3(pack_grid(rows * pack_blocks(p.d), 32)), dim3(256), 0, s, p);
+template <typename T>
+int launch_pack(vardrop_ctx* ctx, const PackArgs& p, long long rows, hipStream_t s) {
+  VdTimer timer(ctx, VARDROP_K_PACK8, s);
+  if (p.d % kPackBlock == 0 && vd_aligned(p.x, 16)) VD_KERNEL(ctx, (pack8_kernel<T, 4>), dim3(pack_grid(rows * (p.d / 8), 1024)), dim3(256), 0, s, p);
+  else VD_KERNEL(ctx, pack8_any_kernel<T>, dim3(pack_grid(rows * pack_blocks(p.d), 32)), dim3(256), 0, s, p);
   VD_LAUNCH_CHECK(ctx);
   return VARDROP_OK;
 }
 template <typename T>
-int launch_unpack(vardrop_ctx* ctx, int kid, const PackArgs& p, bool whole, long long rows, hipStream_t s) {
-  VdTimer timer(ctx, kid, s);
-  if (whole) VD_KERNEL(ctx, (unpack8_kernel<T, 4>), dim3(pack_grid(rows * (p.d / 8), 1024)), dim3(256), 0, s, p);
-  else VD_KERNEL(ctx, (unpack8_any_kernel<T, kActNone>), dim3(pack_grid(rows * pack_blocks(p.d), 32)), dim3(256), 0, s, p);
+int launch_unpack(vardrop_ctx* ctx, const PackArgs& p, long long rows, hipStream_t s) {
+  VdTimer timer(ctx, VARDROP_K_UNPACK8, s);
+  if (p.d % kPackBlock == 0 && vd_aligned(p.values, 16)) VD_KERNEL(ctx, (unpack8_kernel<T, 4>), dim3(pack_grid(rows * (p.d / 8), 1024)), dim3(256), 0, s, p);
+  else VD_KERNEL(ctx, unpack8_any_kernel<T>, dim3(pack_grid(rows * pack_blocks(p.d), 32)), dim3(256), 0, s, p);
   VD_LAUNCH_CHECK(ctx);
   return VARDROP_OK;
 }
@@ -191,53 +169,24 @@ int check_pack(vardrop_ctx* ctx, int B, int n, int d, int dtype, const void* x, 
   if (!saved || !vd_aligned(saved, 256)) return VARDROP_EWORKSPACE;
   return VARDROP_OK;
 }
+PackArgs pack_args(const void* x, void* values, const void* saved, int B, int n, int d, VdDevCount dn) {
+  uint8_t* codes = (uint8_t*)const_cast<void*>(saved);
+  return {x, values, codes, codes + pack_exponents_at((long long)B * n, d), B, n, d, dn.dev, dn.status};
+}
 int pack(vardrop_ctx* ctx, const void* x, int B, int n, int d, int dtype, void* saved, hipStream_t s, VdDevCount dn) {
   const int rc = check_pack(ctx, B, n, d, dtype, x, saved);
   if (rc || (long long)B * n == 0) return rc;
-  return vd_pack8(ctx, VARDROP_K_PACK8, x, B, n, d, dtype, VARDROP_ACT_NONE, saved, (char*)saved + pack_exponents_at((long long)B * n, d), nullptr, s, dn);
+  const PackArgs p = pack_args(x, nullptr, saved, B, n, d, dn);
+  return dtype == VARDROP_BF16 ? launch_pack<bf16_t>(ctx, p, (long long)B * n, s) : launch_pack<float>(ctx, p, (long long)B * n, s);
 }
 int unpack(vardrop_ctx* ctx, const void* saved, int B, int n, int d, int dtype, void* x, hipStream_t s, VdDevCount dn) {
   const int rc = check_pack(ctx, B, n, d, dtype, x, saved);
   if (rc || (long long)B * n == 0) return rc;
-  return vd_unpack8(ctx, VARDROP_K_UNPACK8, saved, (const char*)saved + pack_exponents_at((long long)B * n, d), B, n, d, dtype, x, s, dn);
+  const PackArgs p = pack_args(nullptr, x, saved, B, n, d, dn);
+  return dtype == VARDROP_BF16 ? launch_unpack<bf16_t>(ctx, p, (long long)B * n, s) : launch_unpack<float>(ctx, p, (long long)B * n, s);
 }
 
 }  // namespace
-
-int vd_pack8(vardrop_ctx* ctx, int kid, const void* x, int B, int n, int d, int dtype, int act, void* codes, void* exps, void* a, hipStream_t s,
-             VdDevCount dn) {
-  const long long rows = (long long)B * n;
-  PackArgs p = {};
-  p.x = x; p.a = a; p.codes = (uint8_t*)codes; p.exps = (uint8_t*)exps;
-  p.B = B; p.n = n; p.d = d; p.n_dev = dn.dev; p.status = dn.status;
-  const bool whole = d % kPackBlock == 0 && vd_aligned(x, 16) && vd_aligned(a, 16);
-  if (dtype == VARDROP_BF16) return launch_pack<bf16_t, kActNone>(ctx, kid, p, whole, rows, s);
-  if (act == VARDROP_ACT_RELU) return launch_pack<float, kActRelu>(ctx, kid, p, whole, rows, s);
-  if (act == VARDROP_ACT_GELU) return launch_pack<float, kActGelu>(ctx, kid, p, whole, rows, s);
-  return launch_pack<float, kActNone>(ctx, kid, p, whole, rows, s);
-}
-
-int vd_unpack8(vardrop_ctx* ctx, int kid, const void* codes, const void* exps, int B, int n, int d, int dtype, void* x, hipStream_t s, VdDevCount dn) {
-  PackArgs p = {};
-  p.a = x; p.codes = (uint8_t*)const_cast<void*>(codes); p.exps = (uint8_t*)const_cast<void*>(exps);
-  p.B = B; p.n = n; p.d = d; p.n_dev = dn.dev; p.status = dn.status;
-  const bool whole = d % kPackBlock == 0 && vd_aligned(x, 16);
-  return dtype == VARDROP_BF16 ? launch_unpack<bf16_t>(ctx, kid, p, whole, (long long)B * n, s)
-                               : launch_unpack<float>(ctx, kid, p, whole, (long long)B * n, s);
-}
-
-int vd_act_bwd_f32(vardrop_ctx* ctx, int kid, const float* da, const void* codes, const void* exps, int B, int n, int d, int act, float* dh, float* a,
-                   hipStream_t s, VdDevCount dn) {
-  PackArgs p = {};
-  p.x = da; p.dh = dh; p.a = a; p.codes = (uint8_t*)const_cast<void*>(codes); p.exps = (uint8_t*)const_cast<void*>(exps);
-  p.B = B; p.n = n; p.d = d; p.n_dev = dn.dev; p.status = dn.status;
-  const dim3 grid(pack_grid((long long)B * n * pack_blocks(d), 32));
-  VdTimer timer(ctx, kid, s);
-  if (act == VARDROP_ACT_RELU) VD_KERNEL(ctx, (unpack8_any_kernel<float, kActRelu>), grid, dim3(256), 0, s, p);
-  else VD_KERNEL(ctx, (unpack8_any_kernel<float, kActGelu>), grid, dim3(256), 0, s, p);
-  VD_LAUNCH_CHECK(ctx);
-  return VARDROP_OK;
-}
 
 extern "C" size_t vardrop_pack8_bytes(int B, int n, int d) {
   if (B < 0 || n < 0 || d < 1 || (long long)B * n >= (1ll << 31) || d > (1 << 20)) return 0;

@@ -25,6 +25,7 @@ struct TileArgs {
   const void *A, *B;
   long long lda, ldb;          // bytes from one row to the next
   int M, N, K;                 // elements; K of a k-contiguous operand is whole stages
+  long long planeA, planeB;    // bytes from one part of an operand to the next (Epi::kParts)
   int slices;                  // > 1: cut along k, one workgroup a slice
   // device-side token count (see vd_count): M (n_role 0) or K (n_role 1) is n_mul * n
   const int32_t* n_dev;
@@ -184,6 +185,9 @@ __device__ __forceinline__ void tile_finish(const Sum (&acc)[S::MI][S::NJ], unsi
 // Epi::kSums (B not k-contiguous): column sums of B, from the fragments that are multiplied.  The tiles above each other share the stages
 // among them and their wavefronts above each other the steps, so that none is held up; what one has goes to `sums(piece, n, live, v)`,
 // tile_pieces() of them for a column.
+// Epi::kParts (bf16 operands that stand for fp32 numbers): 6, both operands in three parts hi + mid + lo, each the nearest bf16 number to
+// what the ones before leave; 3, A in one part; 1, plain.  Every product of two parts is exact, and of the nine those are added up, the small
+// ones first, that are not below 2^-24 of the whole: hi lo, lo hi, mid mid, hi mid, mid hi, hi hi.
 // t: the tile, n fastest, then m, then slice.
 template <bool I8, bool AKC, bool BKC, typename S, typename Epi>
 __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi::Args& args, int M, int K, int t) {
@@ -210,7 +214,14 @@ __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi:
   const unsigned char* pb = (const unsigned char*)g.B + (BKC ? n0 * g.ldb + (long long)s0 * S::BKB : (long long)s0 * KU * g.ldb + n0 * 2ll);
   const long long ea = AKC ? (M - m0 - 1) * g.lda + (long long)K * ES - (long long)s0 * S::BKB : (K - s0 * KU - 1) * g.lda + (M - m0) * 2ll;
   const long long eb = BKC ? (g.N - n0 - 1) * g.ldb + (long long)K * ES - (long long)s0 * S::BKB : (K - s0 * KU - 1) * g.ldb + (g.N - n0) * 2ll;
-  const copy_src srcA = tile_source(pa, nk > 0 ? ea : 0), srcB = tile_source(pb, nk > 0 ? eb : 0);
+  constexpr int PARTS = Epi::kParts;
+  const int all = nk * PARTS;                           // stages over all pairs of parts
+  const auto part_a = [](int pair) { return PARTS == 6 ? (0x021010 >> (20 - 4 * pair)) & 3 : 0; };
+  const auto part_b = [](int pair) { return PARTS == 6 ? (0x201100 >> (20 - 4 * pair)) & 3 : 2 - pair; };
+  const auto source_a = [&](int pair) { return tile_source(pa + (PARTS == 6 ? part_a(pair) * g.planeA : 0), nk > 0 ? ea : 0); };
+  const auto source_b = [&](int pair) { return tile_source(pb + (PARTS > 1 ? part_b(pair) * g.planeB : 0), nk > 0 ? eb : 0); };
+  copy_src srcA = source_a(0), srcB = source_b(0);
+  int next_pair = 0, next_k = 0;                        // of the next stage to be copied
   uint32_t offA[IA], offB[IB];
 #pragma unroll
   for (int u = 0; u < IA; ++u) {
@@ -225,12 +236,22 @@ __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi:
     offB[u] = (uint32_t)row * (uint32_t)g.ldb + c * 16;
   }
   const uint32_t stepA = AKC ? (uint32_t)S::BKB : BK * (uint32_t)g.lda, stepB = BKC ? (uint32_t)S::BKB : BK * (uint32_t)g.ldb;
-  auto issue = [&](int k, int buf) {
+  auto issue = [&](int stage, int buf) {
     unsigned char* sp = smem + buf * STAGE + wave * 1024;
+    const int k = PARTS > 1 ? next_k : stage;
 #pragma unroll
     for (int u = 0; u < IA; ++u) dma16_buf(srcA, offA[u], k * stepA, sp + u * W * 1024);
 #pragma unroll
     for (int u = 0; u < IB; ++u) dma16_buf(srcB, offB[u], k * stepB, sp + A_BYTES + u * W * 1024);
+    if constexpr (PARTS > 1) {
+      if (++next_k == nk) {
+        next_k = 0;
+        if (++next_pair < PARTS) {
+          srcA = source_a(next_pair);
+          srcB = source_b(next_pair);
+        }
+      }
+    }
   };
   // ---- fragment addresses (LDS bytes relative to a stage): one for every step of a k-contiguous operand (blocks of 32 rows are a
   // fixed distance apart), one for every block of the other kind (steps are)
@@ -273,15 +294,15 @@ __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi:
   for (int j = 0; j < NJ; ++j) csum[j] = 0.f;
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s)
-    if (s < nk) issue(s, s);
-  for (int t0 = 0; t0 < nk; t0 += NS) {
+    if (s < all) issue(s, s);
+  for (int t0 = 0; t0 < all; t0 += NS) {
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
       const int k = t0 + s;
-      if (k < nk) {
-        wait_stages<NS - 2, LPS>(nk - 1 - k);     // stage k has landed once at most NS - 2 younger ones are in flight
+      if (k < all) {
+        wait_stages<NS - 2, LPS>(all - 1 - k);     // stage k has landed once at most NS - 2 younger ones are in flight
         __builtin_amdgcn_s_barrier();             // everyone has seen it land and is done with stage k - 1, whose buffer is next
-        if (k + NS - 1 < nk) issue(k + NS - 1, (s + NS - 1) % NS);
+        if (k + NS - 1 < all) issue(k + NS - 1, (s + NS - 1) % NS);
         const uint32_t so = s * STAGE;
         Frag fa[2][MI], fb[2][NJ];
         auto read = [&](auto step, int set) {
@@ -311,8 +332,11 @@ __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi:
             }
           }
         };
-        const bool summing = Epi::kSums && k == next_sum;
-        if (summing) next_sum += gy;
+        bool summing = Epi::kSums && k == next_sum;
+        if (summing) {
+          next_sum += gy;
+          if constexpr (PARTS == 6) summing = part_a(k / nk) == 0;        // (each part of B once)
+        }
         auto multiply = [&](auto pending, int set, int ks) {
           wait_lds_count<decltype(pending)::value>();
 #pragma unroll

@@ -92,5 +92,5 @@ def test_tensors_that_are_not_on_the_gpu_are_refused(lib):
 
 def test_kernel_ids_have_names(lib):
     names = [vd.vardrop_kernel_name(k) for k in range(64)]
-    for name in ("pack8", "unpack8", "ffn_up", "ffn_down", "ffn_dh", "ffn_grads", "ffn_act", "ffn_bias", "quantize", "linear_i8"):
+    for name in ("pack8", "unpack8", "ffn_up", "ffn_down", "ffn_dh", "ffn_grads", "ffn_split", "quantize", "linear_i8"):
         assert names.count(name) == 1

@@ -54,7 +54,10 @@ def kept(vd, ctx, saved, B, n, d, f):
 def check(vd, ctx, B, n, d, f, dtype, act, bias=True, grad="fp32", seed=0):
     t = make(seed, B, n, d, f, dtype, bias)
     g = on_device(t, B, n, dtype)
-    y, saved = vd.vardrop_ffn_fwd(ctx, g["x"], g["W1"], g["W2"], g["b1"], g["b2"], act=kind(vd, act))
+    size = vd.vardrop_ffn_saved_bytes(B, n, d, f)
+    room, buf = torch.full((B * n * d + 64,), 7.0, dtype=torch_dtype(dtype), device="cuda"), torch.full((size + 256,), 0xAB, dtype=torch.uint8, device="cuda")
+    y, saved = vd.vardrop_ffn_fwd(ctx, g["x"], g["W1"], g["W2"], g["b1"], g["b2"], act=kind(vd, act), out=room[:-64].view(B, n, d), saved=buf[:size])
+    assert bool((room[-64:] == 7.0).all()) and bool((buf[size:] == 0xAB).all())
     want, bound, h, eh = forward_bounds(t, dtype, act)
     assert_within("y", y, want, bound)
     again, none = vd.vardrop_ffn_fwd(ctx, g["x"], g["W1"], g["W2"], g["b1"], g["b2"], act=kind(vd, act), train=False)
@@ -64,7 +67,11 @@ def check(vd, ctx, B, n, d, f, dtype, act, bias=True, grad="fp32", seed=0):
     # half a step of the block's largest, whose own error may move the step by a factor of two
     most = np.maximum.reduceat(np.abs(h) + eh, np.arange(0, f, 32), axis=1)
     assert (np.abs(kh - h) <= eh + np.repeat(most, 32, axis=1)[:, :f] * 2.0 ** -7 * 1.005).all()
-    out = vd.vardrop_ffn_bwd(ctx, g["dy"], g["W1"], g["W2"], saved, act=kind(vd, act), bias_grads=True, grad_dtype=torch_dtype(grad))
+    gt = torch_dtype(grad)
+    rooms = [torch.full((k + 64,), 7.0, dtype=t_, device="cuda") for k, t_ in ((B * n * d, torch_dtype(dtype)), (d * f, gt), (d * f, gt), (f, gt), (d, gt))]
+    out = [r[:-64].view(s) for r, s in zip(rooms, ((B, n, d), (d, f), (f, d), (f,), (d,)))]
+    vd.vardrop_ffn_bwd(ctx, g["dy"], g["W1"], g["W2"], saved, act=kind(vd, act), out=out)
+    assert all(bool((r[-64:] == 7.0).all()) for r in rooms)
     want = backward_bounds(t, kx, kh, dtype, act, grad)
     for name, got in zip(NAMES, out):
         assert_within(name, got, *want[name])
@@ -78,7 +85,7 @@ def test_bf16(vd, ctx, B, n, d, f, act):
 
 
 @pytest.mark.parametrize("act", ["relu", "gelu"])
-@pytest.mark.parametrize("B,n,d,f", [(1, 1, 1, 1), (1, 1, 64, 128), (4, 10, 64, 128), (2, 33, 50, 97), (1, 65, 96, 31), (3, 111, 321, 65), (1, 600, 128, 256)])
+@pytest.mark.parametrize("B,n,d,f", [(1, 1, 1, 1), (1, 1, 64, 128), (4, 10, 64, 128), (2, 33, 50, 97), (1, 65, 96, 31), (3, 111, 321, 65), (1, 600, 128, 256), (1, 999, 35, 201), (2, 600, 200, 66)])
 def test_fp32(vd, ctx, B, n, d, f, act):
     check(vd, ctx, B, n, d, f, "fp32", act)
 
