@@ -117,6 +117,7 @@ enum {
   VARDROP_K_FFN_DH,          /* (dy W2^T) act'(h)                                           */
   VARDROP_K_FFN_GRADS,       /* dx, dW1, dW2 (K slices)                                     */
   VARDROP_K_FFN_SPLIT,       /* fp32: operands in parts, and the checkpoint of x            */
+  VARDROP_K_FFN_SMALL,       /* fp32: a small block forward in one launch                   */
   VARDROP_K_QUANTIZE,        /* rows or weights as 8-bit integers                           */
   VARDROP_K_LINEAR_I8,       /* product of 8-bit integers                                   */
   VARDROP_K_COUNT

@@ -83,7 +83,7 @@ extern "C" const char* vardrop_kernel_name(int kernel_id) {
       "sdpa_bwd_dq", "sdpa_bwd_dkv", "gemm_dw", "reduce_dw", "gemm_dxs", "scatter", "gemm_dw_dxs", "sdpa_bwd", "qkv_sdpa_fwd",
       "embed_rows", "gemm_embed", "gemm_dwe", "sdpa_bwd_dqkv", "embed_fused",
       "block_norm_fwd", "block_norm_bwd", "block_norm_vectors", "grad_norm", "clip", "adamw",
-      "pack8", "unpack8", "ffn_up", "ffn_down", "ffn_dh", "ffn_grads", "ffn_split", "quantize", "linear_i8"};
+      "pack8", "unpack8", "ffn_up", "ffn_down", "ffn_dh", "ffn_grads", "ffn_split", "ffn_small", "quantize", "linear_i8"};
   return (kernel_id >= 0 && kernel_id < VARDROP_K_COUNT) ? names[kernel_id] : nullptr;
 }
 

@@ -6,7 +6,7 @@
 // channels, so that no width is odd to the products; what the products hand to each other (act(h), dh) they write in parts themselves.  A
 // checkpoint's values are bf16 numbers, and x' has one part.  What three parts do not hold: bits below 2^-133; an infinity, or a magnitude
 // that rounds to one in bf16 (from 0x1.ffp127 on), counts as NaN.
-// Backward of 999 x 321 x 449, us: fp32 products with launches of their own for everything between 100 -> PLACEHOLDER.
+// Backward of 999 x 321 x 449, us: fp32 products with launches of their own for everything between 103 -> 50.
 #include "ffn.h"
 
 namespace {
@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256) void ffn_split_kernel(SplitArgs a) {
   const int pitch = padded(j.cols), per = pitch >> 3;
   const long long groups = (long long)j.all_rows * per;
   for (long long i = (long long)block * 256 + threadIdx.x; i < groups; i += (long long)j.blocks * 256) {
-    const int r = (int)(i / per), c = (int)(i - (long long)r * per) * 8;
+    const int r = groups <= 0x7fffffff ? (int)((uint32_t)i / (uint32_t)per) : (int)(i / per), c = (int)(i - (long long)r * per) * 8;
     float v[8];
     if (j.src) {
       load_row(j.src + (long long)r * j.cols, c, r < j.rows ? j.cols : 0, v);
@@ -220,6 +220,95 @@ struct EpiGradF32 {          // a weight gradient [M][N], or a slice's partial p
   }
 };
 
+// ---- a small block forward in one launch: a workgroup takes kSmallRows rows through both products, x and h in LDS (a channel's rows beside
+// each other, so that a weight meets all of them), a thread a column of the result, or a part of its sum where columns are fewer
+// than threads.
+constexpr int kSmallRows = 8, kSmallChannels = 512, kSmallWeights = 32768;
+struct SmallArgs {
+  const float *x, *W1, *b1, *W2, *b2;
+  float* y;
+  uint8_t *xc, *xe, *hc, *he;      // checkpoints; null: none
+  int B, n, d, f;
+  const int32_t* n_dev;
+  int32_t* status;
+};
+typedef float SmallRow[kSmallRows];
+// out[c][row] = bias[c] + sum_k in[k][row] W[k][c] for c < N; `part` has room for 256 columns' rows
+__device__ __forceinline__ void small_product(const SmallRow* in, const float* W, const float* bias, int K, int N, SmallRow* out, SmallRow* part) {
+  const int wide = min(256, (N + 63) / 64 * 64), groups = 256 / wide, g = threadIdx.x / wide, c0 = threadIdx.x % wide;
+  const int per = (K + groups - 1) / groups, k0 = min(K, g * per), k1 = g < groups ? min(K, k0 + per) : k0;
+  for (int c1 = 0; c1 < N; c1 += wide) {
+    const int c = c1 + c0;
+    float s[kSmallRows];
+#pragma unroll
+    for (int r = 0; r < kSmallRows; ++r) s[r] = 0.f;
+    if (c < N) {
+#pragma unroll 8
+      for (int k = k0; k < k1; ++k) {
+        const float w = W[(long long)k * N + c];
+#pragma unroll
+        for (int r = 0; r < kSmallRows; ++r) s[r] = fmaf(in[k][r], w, s[r]);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSmallRows; ++r) part[threadIdx.x][r] = s[r];
+    __syncthreads();
+    if (g == 0 && c < N) {
+      const float b = bias ? bias[c] : 0.f;
+#pragma unroll
+      for (int r = 0; r < kSmallRows; ++r) {
+        for (int i = 1; i < groups; ++i) s[r] += part[threadIdx.x + i * wide][r];
+        out[c][r] = s[r] + b;
+      }
+    }
+  }
+  __syncthreads();
+}
+// rows m0.. of `in`, packed: half a wavefront a block
+__device__ __forceinline__ void small_pack(const SmallRow* in, int m0, int rows, int d, uint8_t* codes, uint8_t* exps) {
+  const int nb = pack_blocks(d), l = threadIdx.x & 31;
+  for (int b = threadIdx.x >> 5; b < rows * nb; b += 8) {
+    const int r = b / nb, c = (b - r * nb) * kPackBlock + l;
+    const float v = c < d ? in[c][r] : 0.f;
+    uint32_t most = magnitude(v);
+#pragma unroll
+    for (int m = 1; m < 32; m <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, m, 64));
+    const uint32_t e = pack_exponent(most);
+    if (c < d) codes[(long long)(m0 + r) * d + c] = (uint8_t)pack_code(e >= 248u ? pack_limit(v) : v, pack_up(e));
+    if (l == 0) exps[(long long)(m0 + r) * nb + (b - r * nb)] = (uint8_t)e;
+  }
+}
+template <int ACT>
+__global__ __launch_bounds__(256) void ffn_small_kernel(SmallArgs a) {
+  __shared__ __attribute__((aligned(16))) SmallRow xs[kSmallChannels], hs[kSmallChannels], part[256];
+  int n;
+  if (!vd_count(a.n_dev, a.n, n, a.status)) return;
+  const int T = a.B * n, m0 = blockIdx.x * kSmallRows, rows = min(kSmallRows, T - m0);
+  if (rows <= 0) return;
+  for (int i = threadIdx.x; i < kSmallRows * a.d; i += 256) {
+    const int r = i / a.d, c = i - r * a.d;
+    xs[c][r] = r < rows ? a.x[(long long)(m0 + r) * a.d + c] : 0.f;
+  }
+  __syncthreads();
+  small_product(xs, a.W1, a.b1, a.d, a.f, hs, part);
+  if (a.xc) {
+    small_pack(xs, m0, rows, a.d, a.xc, a.xe);
+    small_pack(hs, m0, rows, a.f, a.hc, a.he);
+    __syncthreads();
+  }
+  for (int i = threadIdx.x; i < kSmallRows * a.f; i += 256) (&hs[0][0])[i] = act_value<ACT, true>((&hs[0][0])[i]);
+  __syncthreads();
+  small_product(hs, a.W2, a.b2, a.f, a.d, xs, part);
+  for (int i = threadIdx.x; i < rows * a.d; i += 256) {
+    const int r = i / a.d, c = i - r * a.d;
+    a.y[(long long)(m0 + r) * a.d + c] = xs[c][r];
+  }
+}
+bool is_small(const FfnCall& c) {
+  return c.d <= kSmallChannels && c.f <= kSmallChannels && c.d * c.f <= kSmallWeights && c.T <= (long long)kSmallRows * c.ctx->num_cus;
+}
+
 template <typename S, int ACT, bool KEEP>
 int launch_up(const FfnCall& c, const TileArgs& g, const typename EpiActF32<ACT, KEEP>::Args& e) {
   return launch_tile_gemm<false, true, false, S, EpiActF32<ACT, KEEP>>(c.ctx, VARDROP_K_FFN_UP, g, e, c.s);
@@ -283,6 +372,15 @@ TileArgs parts_product(const FfnCall& c, const void* A, const void* Bm, int K, i
 
 template <int ACT>
 int fwd(const FfnCall& c, const float* x, const float* W1, const float* b1, const float* W2, const float* b2, float* y, uint8_t* saved, char* ws) {
+  if (is_small(c)) {
+    uint8_t* hc = saved ? saved + pack_bytes(c.T, c.d) : nullptr;
+    const SmallArgs a = {x, W1, b1, W2, b2, y, saved, saved ? saved + pack_exponents_at(c.T, c.d) : nullptr, hc, saved ? hc + pack_exponents_at(c.T, c.f) : nullptr,
+                         c.B, c.n, c.d, c.f, c.dn.dev, c.dn.status};
+    VdTimer timer(c.ctx, VARDROP_K_FFN_SMALL, c.s);
+    VD_KERNEL(c.ctx, ffn_small_kernel<ACT>, dim3((unsigned)((c.T + kSmallRows - 1) / kSmallRows)), dim3(256), 0, c.s, a);
+    VD_LAUNCH_CHECK(c.ctx);
+    return VARDROP_OK;
+  }
   const WorkspaceF32 w = workspace_f32(c.T, c.d, c.f);
   const int D = padded(c.d), F = padded(c.f);
   SplitJob jx = {};
