@@ -3,12 +3,13 @@
 Per step, all on one stream and without a host synchronisation (the number of kept tokens stays on the device):
 
     hash -> sample -> embed the kept windows -> norm
-    -> layers x (attention -> post norm, gate, residual and the next norm in one call) -> loss
+    -> layers x (attention -> post norm, gate, residual and the next norm in one call; with --ffn the same around a feed-forward block,
+       whose activations wait for the backward pass in 8 bits) -> loss
     -> the same backwards -> global gradient norm -> AdamW with clipping
 
 The target is what a second encoder with other weights makes of the same windows, so the loss has a zero to go to.
 
-    python examples/train_encoder.py [--steps 200]
+    python examples/train_encoder.py [--steps 200] [--ffn 256]
 """
 import argparse
 import os
@@ -28,17 +29,23 @@ class Encoder:
 
     The residual stream is fp32, the blocks are bf16: pre norms LayerNorm, post norms RMSNorm with a learned gate."""
 
-    def __init__(self, ctx, B, L, n_max, d, H, layers, seed, train=True):
-        self.ctx, self.B, self.L, self.n_max, self.d, self.H, self.layers = ctx, B, L, n_max, d, H, layers
+    def __init__(self, ctx, B, L, n_max, d, H, layers, seed, train=True, ffn=0):
+        self.ctx, self.B, self.L, self.n_max, self.d, self.H, self.layers, self.ffn = ctx, B, L, n_max, d, H, layers, ffn
+        # what stands between two norms: a layer's attention, and with `ffn` channels inside its feed-forward block
+        self.blocks = [kind for _ in range(layers) for kind in (("attention", "ffn") if ffn else ("attention",))]
         g = torch.Generator(device="cuda").manual_seed(seed)
 
         def normal(*shape, scale, at=0.0):
             return torch.randn(*shape, generator=g, device="cuda") * scale + at
 
         p = {"We": normal(L, d, scale=L ** -0.5), "be": normal(d, scale=0.1), "w0": normal(d, scale=0.1, at=1.0), "b0": normal(d, scale=0.1)}
-        for k in range(layers):
-            for name in ("Wq", "Wk", "Wv", "Wo"):
-                p["%s%d" % (name, k)] = normal(d, d, scale=d ** -0.5)
+        for k, kind in enumerate(self.blocks):
+            if kind == "attention":
+                for name in ("Wq", "Wk", "Wv", "Wo"):
+                    p["%s%d" % (name, k)] = normal(d, d, scale=d ** -0.5)
+            else:
+                p["W1%d" % k], p["b1%d" % k] = normal(d, ffn, scale=d ** -0.5), normal(ffn, scale=0.1)
+                p["W2%d" % k], p["b2%d" % k] = normal(ffn, d, scale=ffn ** -0.5), normal(d, scale=0.1)
             p["wp%d" % k], p["gate%d" % k] = normal(d, scale=0.1, at=1.0), normal(d, scale=0.1, at=0.5)
             p["w%d" % (k + 1)], p["b%d" % (k + 1)] = normal(d, scale=0.1, at=1.0), normal(d, scale=0.1)
         self.low = {k: t.to(BF16) for k, t in p.items()}
@@ -50,11 +57,13 @@ class Encoder:
         lib = ctx._lib
         self.xs, self.x0 = tokens(BF16), tokens(F32)
         self.saved_embed = torch.empty(lib.vardrop_embed_saved_bytes(B, n_max, L, vd.BF16), dtype=torch.uint8, device="cuda")
-        saved = lib.vardrop_attn_saved_bytes(B, n_max, d, H, vd.BF16)
-        self.saved = [torch.empty(saved, dtype=torch.uint8, device="cuda") for _ in range(layers)]
-        self.f = [tokens(BF16) for _ in range(layers)]
+        sizes = {"attention": lib.vardrop_attn_saved_bytes(B, n_max, d, H, vd.BF16),
+                 "ffn": vd.vardrop_ffn_saved_bytes(B, n_max, d, ffn) if ffn else 0}
+        self.saved = [torch.empty(sizes[kind], dtype=torch.uint8, device="cuda") for kind in self.blocks]
+        self.f = [tokens(BF16) for _ in self.blocks]
         # (r, h, statistics) of every norm; the first has no branch and r = x0
-        self.norms = [(None if k == 0 else tokens(F32), tokens(BF16), torch.empty(B * n_max, 4, device="cuda")) for k in range(layers + 1)]
+        self.norms = [(None if k == 0 else tokens(F32), tokens(BF16), torch.empty(B * n_max, 4, device="cuda")) for k in range(len(self.blocks) + 1)]
+        self.ffn_ws = torch.empty(vd.vardrop_ffn_workspace_bytes(B, n_max, d, ffn, BF16), dtype=torch.uint8, device="cuda") if ffn else None
         if not train:
             return
         self.grads = {k: torch.zeros_like(t) for k, t in self.params.items()}
@@ -74,8 +83,28 @@ class Encoder:
     def attention(self, k):
         return [self.low["%s%d" % (name, k)] for name in ("Wq", "Wk", "Wv", "Wo")]
 
+    def block(self, k, n_dev):
+        """self.f[k] from the norm before it."""
+        h = self.norms[k][1]
+        if self.blocks[k] == "attention":
+            vd.vardrop_attn_fwd_dev(self.ctx, h, n_dev, self.n_max, *self.attention(k), self.H, self.f[k], self.saved[k])
+        else:
+            low = self.low
+            vd.vardrop_ffn_fwd(self.ctx, h, low["W1%d" % k], low["W2%d" % k], low["b1%d" % k], low["b2%d" % k], act=vd.ACT_GELU, saved=self.saved[k],
+                               ws=self.ffn_ws, out=self.f[k], n_dev=n_dev)
+
+    def block_backward(self, k, n_dev):
+        """self.dh and the gradients of block k's weights from self.df."""
+        g = self.grads
+        if self.blocks[k] == "attention":
+            vd.vardrop_attn_bwd_dev(self.ctx, self.df, self.norms[k][1], n_dev, self.n_max, *self.attention(k), self.H, self.saved[k],
+                                    self.ws, (self.dh, *[g["%s%d" % (name, k)] for name in ("Wq", "Wk", "Wv", "Wo")]))
+        else:
+            vd.vardrop_ffn_bwd(self.ctx, self.df, self.low["W1%d" % k], self.low["W2%d" % k], self.saved[k], act=vd.ACT_GELU, ws=self.ffn_ws,
+                               out=(self.dh, g["W1%d" % k], g["W2%d" % k], g["b1%d" % k], g["b2%d" % k]), n_dev=n_dev)
+
     def around(self, k):
-        """What the norm behind layer k - 1 takes: its own weight, and the post norm and gate of that layer."""
+        """What the norm behind block k - 1 takes: its own weight, and the post norm and gate of that block."""
         kw = dict(pre=vd.NORM_LAYER, w=self.low["w%d" % k])
         if k > 0:
             kw |= dict(post=vd.NORM_RMS, wp=self.low["wp%d" % (k - 1)], gate=self.low["gate%d" % (k - 1)], alpha=RES_SCALE,
@@ -89,8 +118,8 @@ class Encoder:
         self.x0.copy_(self.xs)
         vd.vardrop_block_norm_fwd(ctx, self.x0, b=self.low["b0"], out=self.norms[0], n_dev=n_dev, **self.around(0))
         res = self.x0
-        for k in range(self.layers):
-            vd.vardrop_attn_fwd_dev(ctx, self.norms[k][1], n_dev, n_max, *self.attention(k), self.H, self.f[k], self.saved[k])
+        for k in range(len(self.blocks)):
+            self.block(k, n_dev)
             vd.vardrop_block_norm_fwd(ctx, res, self.f[k], b=self.low["b%d" % (k + 1)], out=self.norms[k + 1], n_dev=n_dev,
                                       **self.around(k + 1))
             res = self.norms[k + 1][0]
@@ -99,13 +128,12 @@ class Encoder:
     def backward(self, dh, n_dev):
         """All gradients into self.grads, from that of the last norm's output."""
         ctx, n_max, g, dr = self.ctx, self.n_max, self.grads, None
-        for k in range(self.layers, 0, -1):
+        for k in range(len(self.blocks), 0, -1):
             r, _, stats = self.norms[k]
             out = (self.dr, self.df, g["w%d" % k], g["b%d" % k], g["wp%d" % (k - 1)], None, g["gate%d" % (k - 1)])
             vd.vardrop_block_norm_bwd(ctx, dr, dh, r, self.f[k - 1], stats, ws=self.ws, out=out, n_dev=n_dev, **self.around(k))
             dr, dh = self.dr, self.dh
-            vd.vardrop_attn_bwd_dev(ctx, self.df, self.norms[k - 1][1], n_dev, n_max, *self.attention(k - 1), self.H, self.saved[k - 1],
-                                    self.ws, (dh, *[g["%s%d" % (name, k - 1)] for name in ("Wq", "Wk", "Wv", "Wo")]))
+            self.block_backward(k - 1, n_dev)
         vd.vardrop_block_norm_bwd(ctx, dr, dh, self.x0, None, self.norms[0][2], ws=self.ws,
                                   out=(self.dr, None, g["w0"], g["b0"], None, None, None), n_dev=n_dev, **self.around(0))
         self.df.copy_(self.dr)
@@ -138,11 +166,11 @@ def windows(B, N, L, seed, table=None):
     return torch.sin(6.2831853 * t / period) + 0.5 * torch.sin(6.2831853 * t / 24.0) + 0.2 * torch.randn(B, N, L, generator=g, device="cuda")
 
 
-def train(steps=200, B=8, N=96, L=96, d=128, H=2, layers=2, gs=4, rate=2e-3, max_norm=1.0, say=None):
+def train(steps=200, B=8, N=96, L=96, d=128, H=2, layers=2, gs=4, rate=2e-3, max_norm=1.0, say=None, ffn=0):
     """-> losses of all steps (one host read, at the end)."""
     ctx = vd.Context(0)
-    student = Encoder(ctx, B, L, N, d, H, layers, seed=1)
-    teacher = Encoder(ctx, B, L, N, d, H, layers, seed=2, train=False)
+    student = Encoder(ctx, B, L, N, d, H, layers, seed=1, ffn=ffn)
+    teacher = Encoder(ctx, B, L, N, d, H, layers, seed=2, train=False, ffn=ffn)
     draw = torch.zeros(1, dtype=torch.int64, device="cuda")
     selection = tuple(torch.zeros(k, dtype=torch.int32, device="cuda") for k in (N, N, 2))
     rate_dev, status = torch.full((1,), rate, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
@@ -168,4 +196,6 @@ def train(steps=200, B=8, N=96, L=96, d=128, H=2, layers=2, gs=4, rate=2e-3, max
 if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     ap.add_argument("--steps", type=int, default=200)
-    train(ap.parse_args().steps, say=print)
+    ap.add_argument("--ffn", type=int, default=0, help="channels inside the feed-forward blocks (a multiple of 64); 0: attention alone")
+    args = ap.parse_args()
+    train(args.steps, say=print, ffn=args.ffn)
