@@ -1076,22 +1076,23 @@ def vardrop_linear_i8(ctx, x, codes, scale, bias=None, act=ACT_NONE, dtype=None,
         x, sx = x
         if sx.dtype is not torch.float32 or not sx.is_contiguous() or sx.get_device() != x.get_device() or sx.numel() != x.shape[0]:
             _refuse("sx", sx, x.shape[0], torch.float32)
-    dev, N, K = x.get_device(), scale.numel(), x.shape[-1]
+    shape, xt, dev, N = x.shape, x.dtype, x.get_device(), scale.numel()
+    K = shape[-1]
     pitch = _i8_pitch(K)
     rows = x.numel() // K if K else 0
-    if codes.dim() != 2 or codes.shape[1] != pitch:
-        raise TypeError("codes must be [N, %d] for rows of %d: got %s" % (pitch, K, list(codes.shape)))
+    if codes.shape != (N, pitch):
+        raise TypeError("codes must be [%d, %d] for rows of %d and %d scales: got %s" % (N, pitch, K, N, list(codes.shape)))
     if dtype is None:
-        dtype = out.dtype if out is not None else bias.dtype if bias is not None else torch.bfloat16 if given else x.dtype
+        dtype = out.dtype if out is not None else bias.dtype if bias is not None else torch.bfloat16 if given else xt
     if out is None:
         _own_buffers(stream, "vardrop_linear_i8", out=out)
-        out = torch.empty((rows, N) if given else (*x.shape[:-1], N), dtype=dtype, device=x.device)
+        out = torch.empty((rows, N) if given else (*shape[:-1], N), dtype=dtype, device=x.device)
     if ws is None and not given:
         _own_buffers(stream, "vardrop_linear_i8", ws=ws)
         ws = _room(vardrop_linear_i8_workspace_bytes(rows, K, N), x.device)
-    code = _CODES.get(x.dtype, -1) if not given else I8 if x.dtype is torch.int8 else -1
-    p_x = x.data_ptr() if x.is_contiguous() else _refuse("x", x, rows * K, x.dtype)
-    p_codes = (codes.data_ptr() if codes.dtype is torch.int8 and codes.numel() == N * pitch and codes.is_contiguous() and codes.get_device() == dev
+    code = _CODES.get(xt, -1) if not given else I8 if xt is torch.int8 else -1
+    p_x = x.data_ptr() if x.is_contiguous() else _refuse("x", x, rows * K, xt)
+    p_codes = (codes.data_ptr() if codes.dtype is torch.int8 and codes.is_contiguous() and codes.get_device() == dev
                else _refuse("codes", codes, N * pitch, torch.int8))
     p_scale = (scale.data_ptr() if scale.dtype is torch.float32 and scale.is_contiguous() and scale.get_device() == dev
                else _refuse("scale", scale, N, torch.float32))

@@ -33,7 +33,9 @@ namespace {
 
 // ---- the plan of the gradients' launch
 // The launch of dx (T x d over f) and of the weight gradients (2 d f over T in slices): time until the last place is done when the longer
-// tiles come first, and the sum of the slices behind it.
+// tiles come first, and the sum of the slices behind it.  Backward passes timed with every tile and number of slices, us, best -> by this plan:
+// 31.0 -> 31.0 (1000 x 512 x 2048), 26.0 -> 26.0 (2784 x 512 x 512), 40.9 -> 40.9 (8000 x 512 x 512), 54.5 -> 55.7 (6000 x 768 x 768), 301 -> 316 (27 584 x 512 x
+// 2048), 726 -> 731 (65 536 x 768 x 1536).
 constexpr int kMostSlices = 16, kLeastSlice = 256;
 struct GradPlan {
   int shape, slices;
@@ -67,7 +69,7 @@ inline GradPlan plan_grads(long long T, int d, int f) {
         }
         end = end > level ? end : level;
       }
-      if (s > 1) end += 2.0 * d * f * s * 2e-4 + 400;                          // (written and read at memory's rate; a launch)
+      if (s > 1) end += 2.0 * d * f * s * 1e-3 + 1300;                         // (written and read; what the last launch takes longer)
       if (least < 0 || end < least) {
         least = end;
         best = {i, s};

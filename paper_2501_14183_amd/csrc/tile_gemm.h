@@ -63,7 +63,7 @@ struct ShapeCost {
 // but dx 137 -> 161 and 53 -> 69.  8-bit products, 128 x 128 -> 256 x 128: 81 -> 72 (27 584 x 512 x 2048), 34.5 -> 28.2 (65 536 x 128 x 768).
 // Few rows take 64 x 64, four stages deep: us, 64 x 128 in three -> 64 x 64 in four: activation 8.0 -> 7.3 (2784 x 512 x 512), 7.4 -> 5.8 (300 x 512 x
 // 2048), dx there 6.2 -> 5.9 and 12.8 -> 9.5.
-constexpr ShapeCost kShapes[3] = {{64, 64, 512, 0.5}, {128, 128, 512, 0.93}, {256, 256, 256, 1.0}};
+constexpr ShapeCost kShapes[3] = {{64, 64, 512, 0.5}, {128, 128, 512, 0.85}, {256, 256, 256, 1.0}};
 constexpr ShapeCost kRowShapes[3] = {{64, 64, 512, 0.5}, {128, 128, 512, 0.93}, {256, 128, 512, 1.0}};
 inline double tile_time(const ShapeCost& c, double K) { return c.BM * c.BN / 1024.0 * (K + kEnds) * c.places / 512.0 / c.rate; }
 inline long long tiles_of(const ShapeCost& c, long long M, int N) { return (M + c.BM - 1) / c.BM * vd_ceil_div(N, c.BN); }
