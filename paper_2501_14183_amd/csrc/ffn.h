@@ -36,23 +36,24 @@ namespace {
 // tiles come first, and the sum of the slices behind it.  Backward passes timed with every tile and number of slices, us, best -> by this plan:
 // 31.0 -> 31.0 (1000 x 512 x 2048), 26.0 -> 26.0 (2784 x 512 x 512), 40.9 -> 40.9 (8000 x 512 x 512), 54.5 -> 55.7 (6000 x 768 x 768), 301 -> 316 (27 584 x 512 x
 // 2048), 726 -> 731 (65 536 x 768 x 1536).
-constexpr int kMostSlices = 16, kLeastSlice = 256;
+constexpr int kMostSlices = 16, kLeastSlice = 256;      // (tokens of a slice; in fp32, whose tokens count 3 and 6 times, a quarter)
 struct GradPlan {
   int shape, slices;
 };
-inline int most_slices(long long T) {
-  const long long s = T / kLeastSlice;
+inline int most_slices(long long T, int least = kLeastSlice) {
+  const long long s = T / least;
   return s < 1 ? 1 : (s > kMostSlices ? kMostSlices : (int)s);
 }
-inline GradPlan plan_grads(long long T, int d, int f) {
+// parts: pairs of parts of dx and, in the mean, of the weight gradients (Epi::kParts)
+inline GradPlan plan_grads(long long T, int d, int f, int least_slice = kLeastSlice, double parts_x = 1, double parts_w = 1) {
   GradPlan best = {0, 1};
   double least = -1;
   for (int i = 0; i < 3; ++i) {
     const ShapeCost& c = kShapes[i];
     const long long nx = tiles_of(c, T, d);
-    for (int s = 1; s <= most_slices(T); ++s) {
+    for (int s = 1; s <= most_slices(T, least_slice); ++s) {
       const long long nw = (tiles_of(c, d, f) + tiles_of(c, f, d)) * s;
-      const double tw = tile_time(c, (double)T / s), tx = tile_time(c, f);
+      const double tw = tile_time(c, parts_w * T / s), tx = tile_time(c, parts_x * f);
       const double tl = tw > tx ? tw : tx, ts = tw > tx ? tx : tw;
       const long long nl = tw > tx ? nw : nx, ns = tw > tx ? nx : nw;
       const long long full = nl / c.places, rest = nl % c.places;              // `rest` places have a long tile more than the others

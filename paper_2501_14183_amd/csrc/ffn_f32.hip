@@ -322,7 +322,7 @@ struct WorkspaceF32 {        // bytes from its start; every operand in three par
   size_t x, W1, W2, wide, act, kept, part, second, col, col2, total;
 };
 WorkspaceF32 workspace_f32(long long T, int d, int f) {
-  const size_t D = padded(d), F = padded(f), t = T, slices = most_slices(T);
+  const size_t D = padded(d), F = padded(f), t = T, slices = most_slices(T, kLeastSlice / 4);
   WorkspaceF32 w;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -436,7 +436,7 @@ int bwd(const FfnCall& c, const float* dy, const float* W1, const float* W2, con
 #undef VD_CALL
     if (rc) return rc;
   }
-  const GradPlan plan = plan_grads(c.T, D, F);
+  const GradPlan plan = plan_grads(c.T, D, F, kLeastSlice / 4, 6, 4.5);
   float *part = (float*)(ws + w.part), *second = (float*)(ws + w.second);
   fin.part_rows[0] = fin.pitch[1] = D;
   fin.part_rows[1] = fin.pitch[0] = F;
