@@ -550,8 +550,10 @@ int vardrop_unpack8_dev(vardrop_ctx* ctx, const void* saved, int B, const int32_
  *   dW1, dW2, db1, db2   element type grad_dtype: VARDROP_F32, or VARDROP_BF16 with VARDROP_BF16 tokens; overwritten; db NULL = skip
  *   ws               vardrop_ffn_workspace_bytes, 256-byte aligned; forward and backward, and all layers, may share one
  * VARDROP_BF16 multiplies on the matrix cores with fp32 accumulation (act(h) and dh are rounded to bf16 in between) and requires d and
- * f multiples of 64 and 16-byte aligned tensors (but db1, db2); VARDROP_F32 multiplies and sums in fp32, at any d and f.  B*n*d, B*n*f and
- * d*f < 2^31 (EUNSUPPORTED otherwise).  Outputs must not overlap inputs.  B*n == 0 is a no-op (weight gradients zero-filled).  The _dev
+ * f multiples of 64 and 16-byte aligned tensors (but db1, db2).  VARDROP_F32 takes any d and f, element aligned: a product is six exact
+ * products of rounded bf16 parts, summed in fp32; bits below 2^-133 are lost, and an infinity, or a magnitude that rounds to one in
+ * bf16, counts as NaN (a small forward, d f <= 32 768 and few tokens, multiplies in fp32 itself).  d, f <= 65 536; B*n*d, B*n*f and d*f < 2^31, in
+ * VARDROP_F32 with d and f up to multiples of 64 (EUNSUPPORTED otherwise).  Outputs must not overlap inputs.  B*n == 0 is a no-op (weight gradients zero-filled).  The _dev
  * forms read n on the device (see the general rules); the same n_max has to be given to the size queries, the forward and the
  * backward.  Sums run in an order that does not depend on scheduling. */
 size_t vardrop_ffn_saved_bytes(int B, int n, int d, int f);
@@ -587,7 +589,7 @@ int vardrop_ffn_bwd_dev(vardrop_ctx* ctx, const void* dy, int B, const int32_t* 
  *   bias    [N], `dtype`, NULL = none;  act any of the three;  y [rows][N], `dtype`
  *   ws      vardrop_linear_i8_workspace_bytes, 256-byte aligned; not needed with VARDROP_I8
  * Sums are exact 32-bit integers, scaled in fp32.  A row (or column of W) without a magnitude of 2^-100 or more counts as zeros, one
- * that holds an infinity or NaN makes its results NaN.  Any K up to 65536 (EUNSUPPORTED above) and any N; x and y need element
+ * that holds an infinity or NaN makes its results NaN.  Any K up to 65536, rows and N up to 2^30 (EUNSUPPORTED above); x and y need element
  * alignment only, and must not overlap.  rows == 0 is a no-op.
  */
 int vardrop_i8_pitch(int K);      /* bytes of a row of codes: K up to a multiple of 128, zeros behind K; 0 when out of range */

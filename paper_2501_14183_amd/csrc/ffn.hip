@@ -270,8 +270,9 @@ constexpr int kMostChannels = 65536;
 bool is_act(int act) { return act == VARDROP_ACT_RELU || act == VARDROP_ACT_GELU; }
 int check_sizes(int B, int n, int d, int f, int dtype) {
   if (B < 0 || n < 0 || d < 1 || f < 1 || (dtype != VARDROP_F32 && dtype != VARDROP_BF16)) return VARDROP_EINVAL;
-  const long long T = (long long)B * n;
-  if (T >= (1ll << 31) || T * d >= (1ll << 31) || T * f >= (1ll << 31) || (long long)d * f >= (1ll << 31)) return VARDROP_EUNSUPPORTED;
+  // (fp32 rows are padded to multiples of 64 channels in the workspace)
+  const long long T = (long long)B * n, D = dtype == VARDROP_F32 ? vd_align_up(d, 64) : d, F = dtype == VARDROP_F32 ? vd_align_up(f, 64) : f;
+  if (T >= (1ll << 31) || T * D >= (1ll << 31) || T * F >= (1ll << 31) || D * F >= (1ll << 31)) return VARDROP_EUNSUPPORTED;
   if (d > kMostChannels || f > kMostChannels) return VARDROP_EUNSUPPORTED;      // (a tile's rows are within 32 bits of each other)
   if (dtype == VARDROP_BF16 && (d % 64 != 0 || f % 64 != 0)) return VARDROP_EUNSUPPORTED;
   return VARDROP_OK;

@@ -10,6 +10,7 @@
 namespace {
 
 constexpr int kMaxI8K = 65536;                        // 127^2 K < 2^31
+constexpr int kMaxI8Rows = 1 << 30;
 constexpr float kLeastRow = 7.8886090522101181e-31f;  // 2^-100: rows below count as zeros (127 / max would not be finite for the smallest)
 
 __host__ __device__ inline int i8_pitch(int K) { return (K + 127) / 128 * 128; }
@@ -450,7 +451,7 @@ extern "C" int vardrop_linear_i8(vardrop_ctx* ctx, const void* x, const float* s
                                  const float* scale, const void* bias, int act, void* y, int dtype, void* ws, size_t ws_bytes, void* stream) {
   if (!ctx || rows < 0 || K < 1 || N < 1 || !is_type(dtype) || (!is_type(x_dtype) && x_dtype != VARDROP_I8)) return VARDROP_EINVAL;
   if (act != VARDROP_ACT_NONE && act != VARDROP_ACT_RELU && act != VARDROP_ACT_GELU) return VARDROP_EINVAL;
-  if (K > kMaxI8K || (long long)vd_ceil_div(rows, 64) * vd_ceil_div(N, 64) >= (1ll << 31)) return VARDROP_EUNSUPPORTED;
+  if (K > kMaxI8K || rows > kMaxI8Rows || N > kMaxI8Rows || (long long)vd_ceil_div(rows, 32) * vd_ceil_div(N, 64) >= (1ll << 31)) return VARDROP_EUNSUPPORTED;
   if ((x_dtype == VARDROP_I8) != (sx != nullptr) && rows > 0) return VARDROP_EINVAL;
   if (rows == 0) return VARDROP_OK;
   if (!x || !codes || !scale || !y || x == y) return VARDROP_EINVAL;

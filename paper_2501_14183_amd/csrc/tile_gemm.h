@@ -409,10 +409,15 @@ __global__ __launch_bounds__(S::THREADS, S::simd) void tile_gemm_kernel(TileArgs
   tile_gemm<I8, AKC, BKC, S, Epi>(g, args, M, K, xcd_contiguous(blockIdx.x, total));
 }
 
-// Raises the dynamic LDS limit of a kernel (a setting of a function on a device): `configured` remembers the device.
+// Raises the dynamic LDS limit of a kernel on the context's device, which need not be the current one; `configured` remembers the device.
 inline int tile_allow_lds(vardrop_ctx* ctx, const void* fn, int lds, int& configured) {
   if (lds <= 65536 || configured == ctx->device) return VARDROP_OK;
-  VD_HIP(ctx, hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+  int current = ctx->device;
+  VD_HIP(ctx, hipGetDevice(&current));
+  if (current != ctx->device) VD_HIP(ctx, hipSetDevice(ctx->device));
+  const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (current != ctx->device) (void)hipSetDevice(current);
+  VD_HIP(ctx, e);
   configured = ctx->device;
   return VARDROP_OK;
 }

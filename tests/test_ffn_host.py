@@ -53,6 +53,7 @@ def test_sizes(lib):
     assert lib.vardrop_linear_i8_workspace_bytes(3, 129, 7) == 768 + 256 and lib.vardrop_linear_i8_workspace_bytes(3, 70000, 7) == 0
     size = lib.vardrop_ffn_workspace_bytes
     assert size(1, 8, 64, 100, vd.BF16) == 0 and size(1, 8, 72, 64, vd.BF16) == 0 and size(1, 8, 72, 100, vd.F32) > 0
+    assert size(1, 8, 65536, 64, vd.F32) > 0 and size(1, 8, 65600, 64, vd.F32) == 0 and size(1 << 15, 1 << 10, 1, 1, vd.F32) == 0
     assert size(1, 8, 64, 64, vd.I8) == 0 and size(1 << 15, 1 << 15, 64, 64, vd.BF16) == 0
 
 

@@ -180,6 +180,35 @@ def test_a_count_on_the_device(vd, ctx, dtype, d, f):
             assert_within(name, got.view(-1, d)[:rows] if name == "dx" else got, *want[name])
 
 
+@pytest.mark.parametrize("dtype,n,d,f", [("bf16", 100, 64, 128), ("bf16", 1500, 128, 192), ("fp32", 70, 50, 70), ("fp32", 700, 64, 200)])
+def test_gradients_that_nobody_wants(vd, ctx, dtype, n, d, f):
+    """Any of dx, db1 and db2 may be missing; the others are the same."""
+    g = on_device(make(6, 1, n, d, f, dtype), 1, n, dtype)
+    saved = vd.vardrop_ffn_fwd(ctx, g["x"], g["W1"], g["W2"], g["b1"], g["b2"])[1]
+    full = vd.vardrop_ffn_bwd(ctx, g["dy"], g["W1"], g["W2"], saved, bias_grads=True)
+    for missing in ((0,), (3,), (4,), (3, 4), (0, 3, 4)):
+        out = tuple(None if k in missing else torch.empty_like(t) for k, t in enumerate(full))
+        vd.vardrop_ffn_bwd(ctx, g["dy"], g["W1"], g["W2"], saved, out=out)
+        assert all(o is None or torch.equal(o, t) for o, t in zip(out, full)), missing
+
+
+def test_offsets_past_32_bits(vd, ctx):
+    """Tokens whose activations, their checkpoints and both gradients lie up to 4 GB into their buffers: the last rows are those of a call of their own."""
+    n, d, f, last = 500_000, 64, 4224, 300
+    x = torch.randn(1, n, d, device="cuda", generator=torch.Generator("cuda").manual_seed(1)).bfloat16()
+    W1, W2 = torch.randn(d, f, device="cuda").mul_(d ** -0.5).bfloat16(), torch.randn(f, d, device="cuda").mul_(f ** -0.5).bfloat16()
+    y, saved = vd.vardrop_ffn_fwd(ctx, x, W1, W2)
+    dx, dW1, dW2, _, db2 = vd.vardrop_ffn_bwd(ctx, x, W1, W2, saved, bias_grads=True)
+    tail = x[:, -last:].contiguous()
+    y2, saved2 = vd.vardrop_ffn_fwd(ctx, tail, W1, W2)
+    assert torch.equal(y[:, -last:], y2)
+    assert torch.equal(dx[:, -last:], vd.vardrop_ffn_bwd(ctx, tail, W1, W2, saved2)[0])
+    # (eight numbers at a time in one chain at the most: n / 8 additions of error 2^-24)
+    want = x.double().sum((0, 1))
+    assert bool(((db2.double() - want).abs() <= n / 8 * 2.0 ** -24 * x.double().abs().sum((0, 1))).all())
+    assert bool(torch.isfinite(dW1).all()) and bool(torch.isfinite(dW2).all())
+
+
 def test_no_tokens(vd, ctx):
     for dt in (torch.bfloat16, torch.float32):
         W1, W2 = torch.ones(64, 128, dtype=dt, device="cuda"), torch.ones(128, 64, dtype=dt, device="cuda")
