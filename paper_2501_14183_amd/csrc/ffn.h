@@ -44,12 +44,13 @@ inline int most_slices(long long T, int least = kLeastSlice) {
   const long long s = T / least;
   return s < 1 ? 1 : (s > kMostSlices ? kMostSlices : (int)s);
 }
-// parts: pairs of parts of dx and, in the mean, of the weight gradients (Epi::kParts)
-inline GradPlan plan_grads(long long T, int d, int f, int least_slice = kLeastSlice, double parts_x = 1, double parts_w = 1) {
+// parts: pairs of parts of dx and, in the mean, of the weight gradients (tile_pairs)
+template <int SHAPES>
+inline GradPlan plan_grads(const ShapeCost (&shapes)[SHAPES], long long T, int d, int f, int least_slice = kLeastSlice, double parts_x = 1, double parts_w = 1) {
   GradPlan best = {0, 1};
   double least = -1;
-  for (int i = 0; i < 3; ++i) {
-    const ShapeCost& c = kShapes[i];
+  for (int i = 0; i < SHAPES; ++i) {
+    const ShapeCost& c = shapes[i];
     const long long nx = tiles_of(c, T, d);
     for (int s = 1; s <= most_slices(T, least_slice); ++s) {
       const long long nw = (tiles_of(c, d, f) + tiles_of(c, f, d)) * s;
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(S::THREADS, S::simd) void ffn_grads_kernel(TileArgs
   if (!tile_dims(gx, Mx, Kx) || !tile_dims(g1, M1, K1) || !tile_dims(g2, M2, K2)) return;
   const int nx = gx.A ? (int)tile_count<S>(gx, Mx) : 0, n1 = (int)tile_count<S>(g1, M1), nw = n1 + (int)tile_count<S>(g2, M2);
   if ((int)blockIdx.x >= nx + nw) return;
-  const bool w_first = K1 / g1.slices * Epi1::kParts > Kx * EpiX::kParts;
+  const bool w_first = (long long)(K1 / g1.slices) * tile_pairs<Epi1>() > (long long)Kx * tile_pairs<EpiX>();
   const int first = w_first ? nw : nx, xcd = blockIdx.x & 7, slot = blockIdx.x >> 3;
   const int of_first = (first >> 3) + (xcd < (first & 7) ? 1 : 0), from = xcd_range_start(xcd, first);
   const bool in_first = slot < of_first;

@@ -20,7 +20,7 @@ __device__ inline void bias_eight(const bf16_t* b, int n, int N, float (&v)[8]) 
 
 struct EpiOut {
   static constexpr bool kFetch = false, kSums = false;
-  static constexpr int kParts = 1;              // C = sums + bias, bf16
+  static constexpr int kPartsA = 1, kPartsB = 1;  // C = sums + bias, bf16
   struct Args {
     bf16_t* C;
     const bf16_t* bias;
@@ -38,7 +38,7 @@ struct EpiOut {
 template <int ACT, bool KEEP>
 struct EpiAct {
   static constexpr bool kFetch = false, kSums = false;
-  static constexpr int kParts = 1;              // h = sums + bias, packed with KEEP; a = act(h)
+  static constexpr int kPartsA = 1, kPartsB = 1;  // h = sums + bias, packed with KEEP; a = act(h)
   struct Args {
     bf16_t* C;
     const bf16_t* bias;
@@ -73,7 +73,7 @@ struct ActBwdArgs {
 template <int ACT, int MI, int NJ>
 struct EpiActBwd {
   static constexpr bool kFetch = true, kSums = false;
-  static constexpr int kParts = 1;           // sums = da; dh = da act'(h'), a = act(h')
+  static constexpr int kPartsA = 1, kPartsB = 1;  // sums = da; dh = da act'(h'), a = act(h')
   typedef ActBwdArgs Args;
   Args a;
   u32x2 codes[2 * MI * NJ];
@@ -102,7 +102,7 @@ struct EpiActBwd {
 
 struct EpiGrad {
   static constexpr bool kFetch = false, kSums = true;
-  static constexpr int kParts = 1;             // weight gradients: the result in the type of the gradients, or a slice's fp32 partial product
+  static constexpr int kPartsA = 1, kPartsB = 1;  // weight gradients: the result in the type of the gradients, or a slice's fp32 partial product
   struct Args {
     void* C;
     float* part;
@@ -368,7 +368,7 @@ int bwd_bf16(const FfnCall& c, const void* dy, const void* W1, const void* W2, c
 #undef VD_CALL
     if (rc) return rc;
   }
-  const GradPlan plan = plan_grads(c.T, c.d, c.f);
+  const GradPlan plan = plan_grads(kShapes, c.T, c.d, c.f);
   const bool split = plan.slices > 1, low = grad_dtype == VARDROP_BF16;
   if (split) {
     fin.part[0] = part;

@@ -6,7 +6,7 @@
 // channels, so that no width is odd to the products; what the products hand to each other (act(h), dh) they write in parts themselves.  A
 // checkpoint's values are bf16 numbers, and x' has one part.  What three parts do not hold: bits below 2^-133; an infinity, or a magnitude
 // that rounds to one in bf16 (from 0x1.ffp127 on), counts as NaN.
-// Backward of 999 x 321 x 449, us: fp32 products with launches of their own for everything between 103 -> 50.
+// Backward of 999 x 321 x 449, us: fp32 products with launches of their own for everything between 103 -> 42.
 #include "ffn.h"
 
 namespace {
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(256) void ffn_split_kernel(SplitArgs a) {
 // ---- what is done to the rows of a product (as in ffn.hip)
 struct EpiOutF32 {           // C [rows][N] = sums + bias
   static constexpr bool kFetch = false, kSums = false;
-  static constexpr int kParts = 6;
+  static constexpr int kPartsA = 3, kPartsB = 3;
   struct Args {
     float* C;
     const float* bias;
@@ -136,7 +136,7 @@ struct EpiOutF32 {           // C [rows][N] = sums + bias
 template <int ACT, bool KEEP>
 struct EpiActF32 {           // h = sums + bias, packed with KEEP; a = act(h) in parts, zeros behind the last channel
   static constexpr bool kFetch = false, kSums = false;
-  static constexpr int kParts = 6;
+  static constexpr int kPartsA = 3, kPartsB = 3;
   struct Args {
     bf16_t* act;
     long long plane;
@@ -174,7 +174,7 @@ struct ActBwdF32Args {
 template <int ACT, int MI, int NJ>
 struct EpiActBwdF32 {        // sums = da; dh = da act'(h'), a = act(h'), both in parts
   static constexpr bool kFetch = true, kSums = false;
-  static constexpr int kParts = 6;
+  static constexpr int kPartsA = 3, kPartsB = 3;
   typedef ActBwdF32Args Args;
   Args a;
   u32x2 codes[2 * MI * NJ];
@@ -204,7 +204,7 @@ struct EpiActBwdF32 {        // sums = da; dh = da act'(h'), a = act(h'), both i
 template <int PARTS>
 struct EpiGradF32 {          // a weight gradient [M][N], or a slice's partial product [slice][part_rows][pitch]
   static constexpr bool kFetch = false, kSums = true;
-  static constexpr int kParts = PARTS;
+  static constexpr int kPartsA = PARTS, kPartsB = 3;
   struct Args {
     float *C, *part, *sums;
     int M, N, whole;         // M, N: the result's; the sums are [padded][padded]
@@ -394,24 +394,24 @@ int fwd(const FfnCall& c, const float* x, const float* W1, const float* b1, cons
   if (rc) return rc;
   const TileArgs up = parts_product(c, ws + w.x, ws + w.W1, D, F, F, (long long)D * F);
   bf16_t* a = (bf16_t*)(ws + w.wide);
-  const int past = c.past(F, 6), shape = product_shape(kRowShapes, c.T, F, 6 * D);
+  const int past = c.past(F, 6), shape = product_shape(kPartShapes, c.T, F, 6 * D);
   if (saved) {
     uint8_t* hc = saved + pack_bytes(c.T, c.d);
     const typename EpiActF32<ACT, true>::Args e = {a, c.T * F, b1, hc, hc + pack_exponents_at(c.T, c.f), c.f, past};
 #define VD_CALL(S) launch_up<S, ACT, true>(c, up, e)
-    rc = VD_BY_SHAPE(shape, VD_CALL, TileWide);
+    rc = VD_BY_PARTS(shape, VD_CALL);
 #undef VD_CALL
   } else {
     const typename EpiActF32<ACT, false>::Args e = {a, c.T * F, b1, nullptr, nullptr, c.f, past};
 #define VD_CALL(S) launch_up<S, ACT, false>(c, up, e)
-    rc = VD_BY_SHAPE(shape, VD_CALL, TileWide);
+    rc = VD_BY_PARTS(shape, VD_CALL);
 #undef VD_CALL
   }
   if (rc) return rc;
   const TileArgs down = parts_product(c, a, ws + w.W2, F, D, D, (long long)D * F);
   const EpiOutF32::Args e = {y, b2, c.d, c.d % 8 == 0 && vd_aligned(y, 16), c.past(c.d, 4)};
 #define VD_CALL(S) launch_tile_gemm<false, true, false, S, EpiOutF32>(c.ctx, VARDROP_K_FFN_DOWN, down, e, c.s)
-  return VD_BY_SHAPE(product_shape(kShapes, c.T, D, 6 * F), VD_CALL, Tile256);
+  return VD_BY_PARTS(product_shape(kPartShapes, c.T, D, 6 * F), VD_CALL);
 #undef VD_CALL
 }
 
@@ -432,11 +432,11 @@ int bwd(const FfnCall& c, const float* dy, const float* W1, const float* W2, con
     const TileArgs g = parts_product(c, g0, ws + w.W2, D, F, D, (long long)D * F);
     const ActBwdF32Args e = {dh, a, c.T * F, hc, hc + pack_exponents_at(c.T, c.f), c.f, c.past(F, 6)};
 #define VD_CALL(S) launch_dh<S, ACT>(c, g, e)
-    rc = VD_BY_SHAPE(product_shape(kRowShapes, c.T, F, 6 * D), VD_CALL, TileWide);
+    rc = VD_BY_PARTS(product_shape(kPartShapes, c.T, F, 6 * D), VD_CALL);
 #undef VD_CALL
     if (rc) return rc;
   }
-  const GradPlan plan = plan_grads(c.T, D, F, kLeastSlice / 4, 6, 4.5);
+  const GradPlan plan = plan_grads(kPartShapes, c.T, D, F, kLeastSlice / 4, 6, 4.5);
   float *part = (float*)(ws + w.part), *second = (float*)(ws + w.second);
   fin.part_rows[0] = fin.pitch[1] = D;
   fin.part_rows[1] = fin.pitch[0] = F;
@@ -452,10 +452,10 @@ int bwd(const FfnCall& c, const float* dy, const float* W1, const float* W2, con
   g1.planeB = g2.planeA = c.T * F * 2;
   g2.planeB = c.T * D * 2;
   const EpiOutF32::Args ax = {dx, nullptr, c.d, c.d % 8 == 0 && vd_aligned(dx, 16), c.past(c.d, 4)};
-  const EpiGradF32<3>::Args a1 = {dW1, (float*)fin.part[0], fin.col[0], c.d, c.f, c.f % 8 == 0 && vd_aligned(dW1, 16)};
-  const EpiGradF32<6>::Args a2 = {dW2, (float*)fin.part[1], fin.col[1], c.f, c.d, c.d % 8 == 0 && vd_aligned(dW2, 16)};
-#define VD_CALL(S) launch_grads<S, EpiOutF32, EpiGradF32<3>, EpiGradF32<6>>(c, gx, ax, g1, a1, g2, a2, fin.pieces)
-  return VD_BY_SHAPE(plan.shape, VD_CALL, Tile256);
+  const EpiGradF32<1>::Args a1 = {dW1, (float*)fin.part[0], fin.col[0], c.d, c.f, c.f % 8 == 0 && vd_aligned(dW1, 16)};
+  const EpiGradF32<3>::Args a2 = {dW2, (float*)fin.part[1], fin.col[1], c.f, c.d, c.d % 8 == 0 && vd_aligned(dW2, 16)};
+#define VD_CALL(S) launch_grads<S, EpiOutF32, EpiGradF32<1>, EpiGradF32<3>>(c, gx, ax, g1, a1, g2, a2, fin.pieces)
+  return VD_BY_PARTS(plan.shape, VD_CALL);
 #undef VD_CALL
 }
 

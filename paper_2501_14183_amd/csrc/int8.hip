@@ -123,7 +123,7 @@ __device__ inline float i8_act(float v, int act) {
 template <typename T>
 struct EpiI8 {
   static constexpr bool kFetch = false, kSums = false;
-  static constexpr int kParts = 1;
+  static constexpr int kPartsA = 1, kPartsB = 1;
   struct Args {
     T* y;
     const float *sx, *sw;      // sx[0] is row m0's

@@ -93,26 +93,45 @@ __device__ inline float slope_factor(float u) {
 // |x|, at most 5.5 (NaN stays)
 __device__ inline float tail_argument(float x) { return __builtin_elementwise_minimum(__builtin_fabsf(x), 5.5f); }
 enum { kActNone = VARDROP_ACT_NONE, kActRelu = VARDROP_ACT_RELU, kActGelu = VARDROP_ACT_GELU };
-// `exact`: with the library's erf, for fp32 results
-template <int ACT, bool EXACT>
+// For results in fp32: Q = exp(-u^2 / 2) R(t), t = 1 / (1 + u / 4), R a polynomial of degree 9 fitted over 0 <= u <= 14 (1.5e-8 of Q; from 14 on
+// u Q is below 2^-140); u phi comes from the same exponential.  Value and derivative are off by at most 2 and 7 times 2^-24 (1 + u).  With the
+// library's erfc and exp the gradient of the activation of 999 x 321 x 449 took 15.8 us, and not 13.6.
+__device__ inline float fine_tail(float u, float& power) {
+  const float t = __builtin_amdgcn_rcpf(fmaf(u, 0.25f, 1.f));
+  power = fast_exp2(u * u * -0.72134752044448170f);
+  float p = 0.03394695743918419f;
+  p = fmaf(p, t, -0.19617852568626404f);
+  p = fmaf(p, t, 0.3950040936470032f);
+  p = fmaf(p, t, -0.3334725499153137f);
+  p = fmaf(p, t, 0.3044894337654114f);
+  p = fmaf(p, t, -0.02038533240556717f);
+  p = fmaf(p, t, 0.12156835198402405f);
+  p = fmaf(p, t, 0.09482017159461975f);
+  p = fmaf(p, t, 0.10022900998592377f);
+  return power * fmaf(p, t, -2.1600530089926906e-05f);
+}
+__device__ inline float fine_argument(float x) { return __builtin_elementwise_minimum(__builtin_fabsf(x), 14.f); }
+// `fine`: for fp32 results
+template <int ACT, bool FINE>
 __device__ inline float act_value(float x) {
   if constexpr (ACT == kActNone) return x;
   if constexpr (ACT == kActRelu) return x < 0.f ? 0.f : x;              // (NaN stays)
-  if constexpr (EXACT) return x * 0.5f * erfcf(x * -0.70710678118654752f);
-  const float u = tail_argument(x);
-  return fmaf(-u, tail_of(u), __builtin_elementwise_maximum(x, 0.f));
+  float power;
+  const float u = FINE ? fine_argument(x) : tail_argument(x);
+  return fmaf(-u, FINE ? fine_tail(u, power) : tail_of(u), __builtin_elementwise_maximum(x, 0.f));
 }
 // value and derivative
-template <int ACT, bool EXACT>
+template <int ACT, bool FINE>
 __device__ inline float act_both(float x, float& slope) {
   if constexpr (ACT == kActRelu) {
     slope = x > 0.f ? 1.f : (x <= 0.f ? 0.f : x);
     return x < 0.f ? 0.f : x;
   }
-  if constexpr (EXACT) {
-    const float below = 0.5f * erfcf(x * -0.70710678118654752f);
-    slope = fmaf(x * 0.39894228040f, expf(-0.5f * x * x), below);
-    return x * below;
+  if constexpr (FINE) {
+    float power;
+    const float u = fine_argument(x), q = fine_tail(u, power), s = fmaf(u * -0.39894228040143268f, power, q);
+    slope = x > 0.f ? 1.f - s : s;
+    return fmaf(-u, q, __builtin_elementwise_maximum(x, 0.f));
   }
   const float u = tail_argument(x), q = tail_of(u);
   const float t = fmaf(-slope_factor(u), q, 0.5f);

@@ -1,12 +1,12 @@
 // Matrix products whose results are worked on before they are stored: the feed-forward block (ffn.hip) and the 8-bit integer
 // products (int8.hip).
 //
-//   C = A B, tiles of BM x 128, four wavefronts of (BM / 2) x 64 each; fp32 (bf16 operands) or int32 (8-bit operands) sums.
+//   C = A B in tiles of a shape (TileShape); fp32 sums of bf16 operands, int32 sums of 8-bit ones.
 //
-// Both operands are copied straight into LDS, two or three stages deep, one barrier a stage; every wavefront copies its share and
-// computes.  A stage is 128 bytes of k for an operand that is contiguous along k ([M][K], [N][K]), 64 k-rows for a bf16
-// operand that is contiguous the other way ([K][M], [K][N]; read through the transposing LDS read).  In bytes both types are
-// the same kernel: v_mfma_f32_32x32x16_bf16 and v_mfma_i32_32x32x32_i8 take 16 bytes of k a lane.
+// Both operands are copied straight into LDS, two to four stages deep, one barrier a stage; every wavefront copies its share and
+// multiplies 32 x 32 blocks.  A stage is 64 or 128 bytes of k for an operand that is contiguous along k ([M][K], [N][K]), as many k-rows
+// as these bytes hold of bf16 for one that is contiguous the other way ([K][M], [K][N]; read through the transposing LDS read).  In bytes
+// both types are the same kernel: v_mfma_f32_32x32x16_bf16 and v_mfma_i32_32x32x32_i8 take 16 bytes of k a lane.
 // What lies outside a matrix (rows past M or N, k past K where K is a count of tokens) lies outside the range of its buffer
 // descriptor, whose loads give zero: there are no masks, and memory behind a tensor is not read.
 // The sums go through LDS once, by which each lane gets eight neighbouring columns of a row: what is done to a row there (Epi)
@@ -25,7 +25,7 @@ struct TileArgs {
   const void *A, *B;
   long long lda, ldb;          // bytes from one row to the next
   int M, N, K;                 // elements; K of a k-contiguous operand is whole stages
-  long long planeA, planeB;    // bytes from one part of an operand to the next (Epi::kParts)
+  long long planeA, planeB;    // bytes from one part of an operand to the next (Epi::kPartsA, kPartsB)
   int slices;                  // > 1: cut along k, one workgroup a slice
   // device-side token count (see vd_count): M (n_role 0) or K (n_role 1) is n_mul * n
   const int32_t* n_dev;
@@ -33,14 +33,15 @@ struct TileArgs {
   int n_max, n_mul, n_role;
 };
 
-// Shape of a tile and its workgroup: BM x BN, WR x WC wavefronts, BKB bytes of k a stage (of a k-contiguous operand), NS stages.
-template <int BM_, int BN_, int WR_, int WC_, int BKB_, int NS_>
+// Shape of a tile and its workgroup: BM x BN, WR x WC wavefronts, BKB bytes of k a stage (of a k-contiguous operand), NS stages, room for
+// PLANES parts of either operand in each.
+template <int BM_, int BN_, int WR_, int WC_, int BKB_, int NS_, int PLANES = 1>
 struct TileShape {
   static constexpr int BM = BM_, BN = BN_, WR = WR_, WC = WC_, BKB = BKB_, NS = NS_;
   static constexpr int WAVES = WR * WC, THREADS = WAVES * 64;
   static constexpr int MI = BM / WR / 32, NJ = BN / WC / 32;       // 32 x 32 blocks of a wavefront
   static constexpr int PITCH = NJ * 128 + 16;                      // LDS row of 32 x (32 NJ) sums
-  static constexpr int A_BYTES = BM * BKB, B_BYTES = BN * BKB, STAGE = A_BYTES + B_BYTES;
+  static constexpr int A_BYTES = BM * BKB, B_BYTES = BN * BKB, STAGE = PLANES * (A_BYTES + B_BYTES);
   static constexpr int ring = NS * STAGE, out = WAVES * 32 * PITCH, lds = ring > out ? ring : out;
   static constexpr int per_cu = (160 << 10) / lds;                 // workgroups of a compute unit
   static constexpr int simd = per_cu * WAVES / 4 > 0 ? per_cu * WAVES / 4 : 1;
@@ -50,6 +51,8 @@ typedef TileShape<64, 64, 2, 2, 128, 4> Tile64;
 typedef TileShape<128, 128, 2, 2, 128, 2> Tile128;
 typedef TileShape<256, 128, 4, 2, 64, 3> TileWide;
 typedef TileShape<256, 256, 2, 4, 128, 2> Tile256;
+typedef TileShape<64, 64, 2, 2, 64, 3, 3> Parts64;
+typedef TileShape<128, 128, 2, 4, 64, 3, 3> Parts128;
 
 // ---- which tile.  What a tile of BM x BN over K (of 2 bytes) costs beside others of its kind, in products of 32 x 32 x 1 of a
 // chip whose every place is taken; its start and end cost as much as kEnds of K.
@@ -64,13 +67,17 @@ struct ShapeCost {
 // Few rows take 64 x 64, four stages deep: us, 64 x 128 in three -> 64 x 64 in four: activation 8.0 -> 7.3 (2784 x 512 x 512), 7.4 -> 5.8 (300 x 512 x
 // 2048), dx there 6.2 -> 5.9 and 12.8 -> 9.5.
 constexpr ShapeCost kShapes[3] = {{64, 64, 512, 0.5}, {128, 128, 512, 0.85}, {256, 256, 256, 1.0}};
+// Operands in parts: 128 x 128 is the largest whose parts fit three deep.  us, 64 x 64 -> 128 x 128: activation 9.3 -> 18.6 (999 x 321 x 449), 19.7 -> 24.8 (4000 x 512 x
+// 512), 26.4 -> 24.5 (6000 x 512 x 512), 56.7 -> 52.0 (12 000 x 256 x 1024).
+constexpr ShapeCost kPartShapes[2] = {{64, 64, 512, 0.6}, {128, 128, 256, 1.0}};
 constexpr ShapeCost kRowShapes[3] = {{64, 64, 512, 0.5}, {128, 128, 512, 0.93}, {256, 128, 512, 1.0}};
 inline double tile_time(const ShapeCost& c, double K) { return c.BM * c.BN / 1024.0 * (K + kEnds) * c.places / 512.0 / c.rate; }
 inline long long tiles_of(const ShapeCost& c, long long M, int N) { return (M + c.BM - 1) / c.BM * vd_ceil_div(N, c.BN); }
-inline int product_shape(const ShapeCost (&shapes)[3], long long T, int N, int K) {
+template <int SHAPES>
+inline int product_shape(const ShapeCost (&shapes)[SHAPES], long long T, int N, int K) {
   int best = 0;
   double least = 0;
-  for (int i = 0; i < 3; ++i) {
+  for (int i = 0; i < SHAPES; ++i) {
     // (workgroups end at different times: the last round is seldom a whole one longer)
     const double rounds = (double)tiles_of(shapes[i], T, N) / shapes[i].places;
     const double t = (rounds <= 1 ? 1 : rounds + 0.3) * tile_time(shapes[i], K);
@@ -83,7 +90,7 @@ inline int product_shape(const ShapeCost (&shapes)[3], long long T, int N, int K
 }
 // a call of CALL for the tile of kShapes, or with WIDE = TileWide of kRowShapes
 #define VD_BY_SHAPE(SHAPE, CALL, WIDE) ((SHAPE) == 0 ? CALL(Tile64) : (SHAPE) == 1 ? CALL(Tile128) : CALL(WIDE))
-
+#define VD_BY_PARTS(SHAPE, CALL) ((SHAPE) == 0 ? CALL(Parts64) : CALL(Parts128))
 
 // Descriptor of the memory from p on, `bytes` long (none: every load gives zero).
 __device__ inline copy_src tile_source(const void* p, long long bytes) {
@@ -185,20 +192,25 @@ __device__ __forceinline__ void tile_finish(const Sum (&acc)[S::MI][S::NJ], unsi
 // Epi::kSums (B not k-contiguous): column sums of B, from the fragments that are multiplied.  The tiles above each other share the stages
 // among them and their wavefronts above each other the steps, so that none is held up; what one has goes to `sums(piece, n, live, v)`,
 // tile_pieces() of them for a column.
-// Epi::kParts (bf16 operands that stand for fp32 numbers): 6, both operands in three parts hi + mid + lo, each the nearest bf16 number to
-// what the ones before leave; 3, A in one part; 1, plain.  Every product of two parts is exact, and of the nine those are added up, the small
-// ones first, that are not below 2^-24 of the whole: hi lo, lo hi, mid mid, hi mid, mid hi, hi hi.
+// Epi::kPartsA, kPartsB (bf16 operands that stand for fp32 numbers): 3 and 3, both operands in three parts hi + mid + lo, each the nearest
+// bf16 number to what the ones before leave; 1 and 3, A in one part; 1 and 1, plain.  A stage holds all parts of its k.  Every product of
+// two parts is exact, and of the nine those are added up, the small ones of a step first, that are not below 2^-24 of the whole:
+// hi lo, mid mid, lo hi, hi mid, mid hi, hi hi.  (One pair of parts after the other, over all of k, copies and reads each part twice and meets
+// six times the barriers: products of 2002 x 512 x 1024 backward 104 us, and not 73; 27 584 x 512 x 2048 in 256 x 256 tiles 1458 and 1453.)
 // t: the tile, n fastest, then m, then slice.
 template <bool I8, bool AKC, bool BKC, typename S, typename Epi>
 __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi::Args& args, int M, int K, int t) {
   static_assert(!I8 || (AKC && BKC), "8-bit operands are contiguous along k");
   typedef typename TileSum<I8>::type Sum;
-  constexpr int BM = S::BM, BN = S::BN, MI = S::MI, NJ = S::NJ, NS = S::NS, A_BYTES = S::A_BYTES, STAGE = S::STAGE, W = S::WAVES;
+  constexpr int BM = S::BM, BN = S::BN, MI = S::MI, NJ = S::NJ, NS = S::NS, A_BYTES = S::A_BYTES, B_BYTES = S::B_BYTES, W = S::WAVES;
+  constexpr int PA = Epi::kPartsA, PB = Epi::kPartsB, STAGE = PA * A_BYTES + PB * B_BYTES;
+  static_assert(STAGE <= S::STAGE && (PA == 1 || PA == PB), "room for the parts");
   constexpr int BK = S::BKB / 2, KS = S::BKB / 32;                               // k-rows of a stage, steps of a stage
-  constexpr int IA = A_BYTES / (1024 * W), IB = S::B_BYTES / (1024 * W), LPS = IA + IB;   // 1 KB copies per wavefront and stage
-  constexpr int OPK = (AKC ? MI : 2 * MI) + (BKC ? NJ : 2 * NJ);                 // LDS reads per step
+  constexpr int IA = A_BYTES / (1024 * W), IB = B_BYTES / (1024 * W), LPS = PA * IA + PB * IB;   // 1 KB copies per wavefront, part and stage
+  constexpr int OPK = PA * (AKC ? MI : 2 * MI) + PB * (BKC ? NJ : 2 * NJ);       // LDS reads per step
+  constexpr int OPEN = OPK < 15 ? OPK : 15;                                       // (as many as the counter counts)
   constexpr int CHK = S::BKB / 16, CHA = AKC ? CHK : BM / 8, CHB = BKC ? CHK : BN / 8;    // 16-byte chunks of an LDS row
-  static_assert(IA * 1024 * W == A_BYTES && IB * 1024 * W == S::B_BYTES, "whole copies");
+  static_assert(IA * 1024 * W == A_BYTES && IB * 1024 * W == B_BYTES, "whole copies");
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int gx = (g.N + BN - 1) / BN, gy = (M + BM - 1) / BM;
   const int n0 = t % gx * BN, m0 = t / gx % gy * BM, slice = t / (gx * gy);
@@ -214,14 +226,11 @@ __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi:
   const unsigned char* pb = (const unsigned char*)g.B + (BKC ? n0 * g.ldb + (long long)s0 * S::BKB : (long long)s0 * KU * g.ldb + n0 * 2ll);
   const long long ea = AKC ? (M - m0 - 1) * g.lda + (long long)K * ES - (long long)s0 * S::BKB : (K - s0 * KU - 1) * g.lda + (M - m0) * 2ll;
   const long long eb = BKC ? (g.N - n0 - 1) * g.ldb + (long long)K * ES - (long long)s0 * S::BKB : (K - s0 * KU - 1) * g.ldb + (g.N - n0) * 2ll;
-  constexpr int PARTS = Epi::kParts;
-  const int all = nk * PARTS;                           // stages over all pairs of parts
-  const auto part_a = [](int pair) { return PARTS == 6 ? (0x021010 >> (20 - 4 * pair)) & 3 : 0; };
-  const auto part_b = [](int pair) { return PARTS == 6 ? (0x201100 >> (20 - 4 * pair)) & 3 : 2 - pair; };
-  const auto source_a = [&](int pair) { return tile_source(pa + (PARTS == 6 ? part_a(pair) * g.planeA : 0), nk > 0 ? ea : 0); };
-  const auto source_b = [&](int pair) { return tile_source(pb + (PARTS > 1 ? part_b(pair) * g.planeB : 0), nk > 0 ? eb : 0); };
-  copy_src srcA = source_a(0), srcB = source_b(0);
-  int next_pair = 0, next_k = 0;                        // of the next stage to be copied
+  copy_src srcA[PA], srcB[PB];
+#pragma unroll
+  for (int p = 0; p < PA; ++p) srcA[p] = tile_source(pa + p * g.planeA, nk > 0 ? ea : 0);
+#pragma unroll
+  for (int p = 0; p < PB; ++p) srcB[p] = tile_source(pb + p * g.planeB, nk > 0 ? eb : 0);
   uint32_t offA[IA], offB[IB];
 #pragma unroll
   for (int u = 0; u < IA; ++u) {
@@ -238,20 +247,14 @@ __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi:
   const uint32_t stepA = AKC ? (uint32_t)S::BKB : BK * (uint32_t)g.lda, stepB = BKC ? (uint32_t)S::BKB : BK * (uint32_t)g.ldb;
   auto issue = [&](int stage, int buf) {
     unsigned char* sp = smem + buf * STAGE + wave * 1024;
-    const int k = PARTS > 1 ? next_k : stage;
 #pragma unroll
-    for (int u = 0; u < IA; ++u) dma16_buf(srcA, offA[u], k * stepA, sp + u * W * 1024);
+    for (int p = 0; p < PA; ++p)
 #pragma unroll
-    for (int u = 0; u < IB; ++u) dma16_buf(srcB, offB[u], k * stepB, sp + A_BYTES + u * W * 1024);
-    if constexpr (PARTS > 1) {
-      if (++next_k == nk) {
-        next_k = 0;
-        if (++next_pair < PARTS) {
-          srcA = source_a(next_pair);
-          srcB = source_b(next_pair);
-        }
-      }
-    }
+      for (int u = 0; u < IA; ++u) dma16_buf(srcA[p], offA[u], stage * stepA, sp + p * A_BYTES + u * W * 1024);
+#pragma unroll
+    for (int p = 0; p < PB; ++p)
+#pragma unroll
+      for (int u = 0; u < IB; ++u) dma16_buf(srcB[p], offB[u], stage * stepB, sp + PA * A_BYTES + p * B_BYTES + u * W * 1024);
   };
   // ---- fragment addresses (LDS bytes relative to a stage): one for every step of a k-contiguous operand (blocks of 32 rows are a
   // fixed distance apart), one for every block of the other kind (steps are)
@@ -272,12 +275,12 @@ __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi:
   if constexpr (BKC) {
     const int rb = wn * (NJ * 32) + col;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) addrB[ks] = lds0 + A_BYTES + rb * S::BKB + (((2 * ks + half) ^ swz_kc<BK>(rb)) * 16);
+    for (int ks = 0; ks < KS; ++ks) addrB[ks] = lds0 + PA * A_BYTES + rb * S::BKB + (((2 * ks + half) ^ swz_kc<BK>(rb)) * 16);
   } else {
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       const int c = wn * (NJ * 32) + j * 32 + mn;
-      addrB[j] = lds0 + A_BYTES + krow * (BN * 2) + (((c >> 3) ^ swz_nc<BN>(krow)) * 16) + ((c >> 2) & 1) * 8;
+      addrB[j] = lds0 + PA * A_BYTES + krow * (BN * 2) + (((c >> 3) ^ swz_nc<BN>(krow)) * 16) + ((c >> 2) & 1) * 8;
     }
   }
   Sum acc[MI][NJ];
@@ -294,75 +297,94 @@ __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi:
   for (int j = 0; j < NJ; ++j) csum[j] = 0.f;
 #pragma unroll
   for (int s = 0; s < NS - 1; ++s)
-    if (s < all) issue(s, s);
-  for (int t0 = 0; t0 < all; t0 += NS) {
+    if (s < nk) issue(s, s);
+  for (int t0 = 0; t0 < nk; t0 += NS) {
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
       const int k = t0 + s;
-      if (k < all) {
-        wait_stages<NS - 2, LPS>(all - 1 - k);     // stage k has landed once at most NS - 2 younger ones are in flight
+      if (k < nk) {
+        wait_stages<NS - 2, LPS>(nk - 1 - k);     // stage k has landed once at most NS - 2 younger ones are in flight
         __builtin_amdgcn_s_barrier();             // everyone has seen it land and is done with stage k - 1, whose buffer is next
-        if (k + NS - 1 < all) issue(k + NS - 1, (s + NS - 1) % NS);
+        if (k + NS - 1 < nk) issue(k + NS - 1, (s + NS - 1) % NS);
         const uint32_t so = s * STAGE;
-        Frag fa[2][MI], fb[2][NJ];
-        auto read = [&](auto step, int set) {
-          constexpr int ks = decltype(step)::value;
-          if constexpr (AKC) {
-            const uint32_t p = addrA[AKC ? ks : 0] + so;
-            lds_read16_at<0>(fa[set][0].q, p);
-            if constexpr (MI > 1) lds_read16_at<32 * S::BKB>(fa[set][MI > 1 ? 1 : 0].q, p);
-            if constexpr (MI > 2) lds_read16_at<64 * S::BKB>(fa[set][MI > 2 ? 2 : 0].q, p);
-            if constexpr (MI > 3) lds_read16_at<96 * S::BKB>(fa[set][MI > 3 ? 3 : 0].q, p);
-          } else {
+        Frag fa[2][PA][MI], fb[2][PB][NJ];
+        auto read_part = [&](auto step, auto part, int set) {
+          constexpr int ks = decltype(step)::value, p = decltype(part)::value;
+          if constexpr (p < PA) {
+            Frag(&f)[MI] = fa[set][p < PA ? p : 0];
+            if constexpr (AKC) {
+              const uint32_t at = addrA[AKC ? ks : 0] + so;
+              lds_read16_at<p * A_BYTES>(f[0].q, at);
+              if constexpr (MI > 1) lds_read16_at<p * A_BYTES + 32 * S::BKB>(f[MI > 1 ? 1 : 0].q, at);
+              if constexpr (MI > 2) lds_read16_at<p * A_BYTES + 64 * S::BKB>(f[MI > 2 ? 2 : 0].q, at);
+              if constexpr (MI > 3) lds_read16_at<p * A_BYTES + 96 * S::BKB>(f[MI > 3 ? 3 : 0].q, at);
+            } else {
 #pragma unroll
-            for (int i = 0; i < MI; ++i) {
-              lds_read8_tr<ks * 16 * BM * 2>(fa[set][i].d[0], addrA[i] + so);
-              lds_read8_tr<ks * 16 * BM * 2 + 4 * BM * 2>(fa[set][i].d[1], addrA[i] + so);
+              for (int i = 0; i < MI; ++i) {
+                lds_read8_tr<p * A_BYTES + ks * 16 * BM * 2>(f[i].d[0], addrA[i] + so);
+                lds_read8_tr<p * A_BYTES + ks * 16 * BM * 2 + 4 * BM * 2>(f[i].d[1], addrA[i] + so);
+              }
             }
           }
-          if constexpr (BKC) {
-            const uint32_t p = addrB[BKC ? ks : 0] + so;
-            lds_read16_at<0>(fb[set][0].q, p);
-            if constexpr (NJ > 1) lds_read16_at<32 * S::BKB>(fb[set][NJ > 1 ? 1 : 0].q, p);
-          } else {
+          if constexpr (p < PB) {
+            Frag(&f)[NJ] = fb[set][p < PB ? p : 0];
+            if constexpr (BKC) {
+              const uint32_t at = addrB[BKC ? ks : 0] + so;
+              lds_read16_at<p * B_BYTES>(f[0].q, at);
+              if constexpr (NJ > 1) lds_read16_at<p * B_BYTES + 32 * S::BKB>(f[NJ > 1 ? 1 : 0].q, at);
+            } else {
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-              lds_read8_tr<ks * 16 * BN * 2>(fb[set][j].d[0], addrB[j] + so);
-              lds_read8_tr<ks * 16 * BN * 2 + 4 * BN * 2>(fb[set][j].d[1], addrB[j] + so);
+              for (int j = 0; j < NJ; ++j) {
+                lds_read8_tr<p * B_BYTES + ks * 16 * BN * 2>(f[j].d[0], addrB[j] + so);
+                lds_read8_tr<p * B_BYTES + ks * 16 * BN * 2 + 4 * BN * 2>(f[j].d[1], addrB[j] + so);
+              }
             }
           }
         };
-        bool summing = Epi::kSums && k == next_sum;
-        if (summing) {
-          next_sum += gy;
-          if constexpr (PARTS == 6) summing = part_a(k / nk) == 0;        // (each part of B once)
-        }
+        auto read = [&](auto step, int set) {
+          read_part(step, Int<0>{}, set);
+          read_part(step, Int<1>{}, set);
+          read_part(step, Int<2>{}, set);
+        };
+        const bool summing = Epi::kSums && k == next_sum;
+        if (summing) next_sum += gy;
         auto multiply = [&](auto pending, int set, int ks) {
           wait_lds_count<decltype(pending)::value>();
 #pragma unroll
-          for (int i = 0; i < MI; ++i) tie(fa[set][i]);
+          for (int p = 0; p < PA; ++p)
 #pragma unroll
-          for (int j = 0; j < NJ; ++j) tie(fb[set][j]);
+            for (int i = 0; i < MI; ++i) tie(fa[set][p][i]);
 #pragma unroll
-          for (int i = 0; i < MI; ++i)
+          for (int p = 0; p < PB; ++p)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) acc[i][j] = tile_mfma(fb[set][j], fa[set][i], acc[i][j]);
+            for (int j = 0; j < NJ; ++j) tie(fb[set][p][j]);
+          // pairs of parts whose places add up to 2, 1, 0
+#pragma unroll
+          for (int both = PB - 1; both >= 0; --both)
+#pragma unroll
+            for (int p = 0; p <= both && p < PA; ++p)
+#pragma unroll
+              for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) acc[i][j] = tile_mfma(fb[set][both - p][j], fa[set][p][i], acc[i][j]);
           if constexpr (Epi::kSums) {
             if (summing && ks % S::WR == wm) {
 #pragma unroll
-              for (int j = 0; j < NJ; ++j) csum[j] += eight_sum(fb[set][j]);
+              for (int p = PB - 1; p >= 0; --p)
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) csum[j] += eight_sum(fb[set][p][j]);
             }
           }
           __builtin_amdgcn_sched_barrier(0);
         };
         read(Int<0>{}, 0);
         read(Int<1>{}, 1);
-        multiply(Int<OPK>{}, 0, 0);
+        multiply(Int<OPEN>{}, 0, 0);
         if constexpr (KS == 4) {
           read(Int<2>{}, 0);
-          multiply(Int<OPK>{}, 1, 1);
+          multiply(Int<OPEN>{}, 1, 1);
           read(Int<3>{}, 1);
-          multiply(Int<OPK>{}, 0, 2);
+          multiply(Int<OPEN>{}, 0, 2);
         }
         multiply(Int<0>{}, 1, KS - 1);
       }
@@ -382,6 +404,8 @@ __device__ __forceinline__ void tile_gemm(const TileArgs& g, const typename Epi:
   tile_finish<S, Epi>(acc, smem, epi, slice, M, g.N, m0, n0);
 }
 
+// products of two parts that one of fp32 numbers takes
+template <typename Epi> constexpr int tile_pairs() { return Epi::kPartsA > 1 ? 6 : Epi::kPartsB; }
 // A product's dimensions with a device-side count resolved; false: the count is invalid.
 __device__ __forceinline__ bool tile_dims(const TileArgs& g, int& M, int& K) {
   M = g.M;

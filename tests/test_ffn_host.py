@@ -43,6 +43,29 @@ def test_the_fits_of_gelu():
     assert 5.5 * tail[-1] <= 1.1e-7 and abs(s[-1]) <= 6e-7
 
 
+def test_the_fine_fit_of_gelu():
+    """Its error over every argument, with t and the exponential off by one step of fp32 either way: below the 8 2^-24 (1 + |x|) that the tests of the fp32 block count."""
+    text = open(os.path.join(ROOT, "paper_2501_14183_amd", "csrc", "pack8.h")).read()
+    body = re.search(r"inline float fine_tail\(float u, float& power\) \{(.*?)\n\}", text, re.S).group(1)
+    c = [np.float32(v) for v in re.findall(r"(-?\d+\.\d+(?:e-\d+)?)f", body)]
+    assert c[0] == 0.25 and abs(c[1] + 0.5 / np.log(2)) < 1e-7 and len(c) == 12
+    f, x = np.float32, np.linspace(-20, 20, 400001).astype(np.float32)
+    w = x.astype(np.float64)
+    u = np.minimum(np.abs(x), f(14))
+    phi, cdf = np.exp(-0.5 * w * w) / np.sqrt(2 * np.pi), o.cdf(w)
+    for step in (-1, 0, 1):
+        t = f(1.0 / f(u.astype(np.float64) * 0.25 + 1.0))
+        t = np.nextafter(t, f(9 * step)) if step else t
+        power = f(np.exp2((u * u * c[1]).astype(np.float64)))
+        power = np.nextafter(power, f(9 * step)) if step else power
+        q = f(power * horner(c[2:], t))
+        value = f(np.maximum(w, 0.0) - u.astype(np.float64) * q)
+        s = f(f(u * f(-0.39894228040143268)).astype(np.float64) * power + q)
+        slope = np.where(x > 0, f(1.0 - s.astype(np.float64)), s)
+        assert (np.abs(value - w * cdf) / (1 + np.abs(w))).max() <= 2 * 2.0 ** -24
+        assert (np.abs(slope - cdf - w * phi) / (1 + np.abs(w))).max() <= 7 * 2.0 ** -24
+
+
 def test_sizes(lib):
     assert lib.vardrop_pack8_bytes(1, 1, 1) == 512 and lib.vardrop_pack8_bytes(2, 4, 64) == 512 + 256
     assert lib.vardrop_pack8_bytes(3, 5, 33) == 512 + 256 and lib.vardrop_pack8_bytes(0, 4, 64) == 0
