@@ -192,7 +192,7 @@ int i8_product(const I8Call& c) {
 
 // ---- quantisation and product in one launch, while a tile's rows of codes fit LDS beside the stages of the weight: every workgroup makes
 // the codes of its own 32 rows (16 lanes a row), which the workgroups of the other columns make again.  32 and not 64 rows: twice the
-// workgroups, half the rows for each to wait for.
+// workgroups, half the rows for each to wait for.  A chain too: launch, rows, their codes, four stages, the end; 862 x 512 x 720 7.4 us (86 TOPS).
 template <typename X>
 __device__ inline void load_some(const X* row, int k, int K, bool whole, float (&v)[8]) {
   if (whole && k + 8 <= K) {
@@ -203,12 +203,12 @@ __device__ inline void load_some(const X* row, int k, int K, bool whole, float (
   }
 }
 typedef TileShape<32, 128, 1, 4, 128, 3> I8Shape;
-constexpr int kI8Ring = I8Shape::NS * I8Shape::B_BYTES;
+constexpr int kFusedPitch = 512, kI8Ring = I8Shape::NS * I8Shape::B_BYTES;
 inline int i8_fused_lds(int K) { return kI8Ring + 256 + I8Shape::BM * i8_pitch(K); }
-template <typename X, typename T, int J>
+template <typename X, typename T>
 __global__ __launch_bounds__(256, 2) void i8_fused_kernel(const X* x, int rows, int K, int N, const uint8_t* codes, typename EpiI8<T>::Args args, int whole_x) {
   typedef I8Shape S;
-  constexpr int NS = S::NS, LPS = S::B_BYTES / 4096;
+  constexpr int NS = S::NS, LPS = S::B_BYTES / 4096, J = kFusedPitch / 128;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   float* sx = reinterpret_cast<float*>(smem + kI8Ring);
   unsigned char* tile = smem + kI8Ring + 256;             // [stage][32 rows][128 bytes], swizzled
@@ -314,9 +314,9 @@ __global__ __launch_bounds__(256, 2) void i8_fused_kernel(const X* x, int rows, 
   tile_finish<S, EpiI8<T>>(acc, smem, epi, 0, rows, N, m0, n0);
 }
 
-// ---- up to eight rows: a workgroup makes their codes and takes 16 columns, 16 lanes each, with the byte dot product; it is as long as
-// reading a few rows of weights takes.
-constexpr int kFewRows = 8, kFewPitch = 2048;
+// ---- up to four rows: a workgroup makes their codes and takes 16 columns, 16 lanes each, with the byte dot product.  Its time is a chain: launch,
+// rows twice, weights, sums; 1 x 512 x 512 4.3 us.
+constexpr int kFewRows = 4, kFewPitch = 1024;
 template <typename X, typename T, int R>
 __global__ __launch_bounds__(256) void i8_few_kernel(const X* x, int rows, int K, int N, const uint8_t* codes, typename EpiI8<T>::Args a) {
   __shared__ __attribute__((aligned(16))) uint8_t q[R][kFewPitch];
@@ -375,30 +375,28 @@ int i8_one_launch(const I8Call& c) {
     const dim3 grid((unsigned)vd_ceil_div(c.N, 16));
     VdTimer timer(c.ctx, VARDROP_K_LINEAR_I8, c.s);
     if (c.rows == 1) VD_KERNEL(c.ctx, (i8_few_kernel<X, T, 1>), grid, dim3(256), 0, c.s, x, c.rows, c.K, c.N, c.codes, a);
-    else if (c.rows <= 4) VD_KERNEL(c.ctx, (i8_few_kernel<X, T, 4>), grid, dim3(256), 0, c.s, x, c.rows, c.K, c.N, c.codes, a);
-    else VD_KERNEL(c.ctx, (i8_few_kernel<X, T, 8>), grid, dim3(256), 0, c.s, x, c.rows, c.K, c.N, c.codes, a);
+    else VD_KERNEL(c.ctx, (i8_few_kernel<X, T, kFewRows>), grid, dim3(256), 0, c.s, x, c.rows, c.K, c.N, c.codes, a);
     VD_LAUNCH_CHECK(c.ctx);
     return VARDROP_OK;
   }
   const int lds = i8_fused_lds(c.K), whole = c.K % 8 == 0 && vd_aligned(x, 16);
   const dim3 grid((unsigned)(vd_ceil_div(c.N, 128) * vd_ceil_div(c.rows, 32)));
-  static int narrow = -1, wide = -1;
-  const bool small = i8_pitch(c.K) <= 512;
-  const int rc = small ? tile_allow_lds(c.ctx, (const void*)i8_fused_kernel<X, T, 4>, i8_fused_lds(512), narrow)
-                       : tile_allow_lds(c.ctx, (const void*)i8_fused_kernel<X, T, 8>, i8_fused_lds(1024), wide);
+  static int configured = -1;
+  const int rc = tile_allow_lds(c.ctx, (const void*)i8_fused_kernel<X, T>, i8_fused_lds(kFusedPitch), configured);
   if (rc) return rc;
   VdTimer timer(c.ctx, VARDROP_K_LINEAR_I8, c.s);
-  if (small) VD_KERNEL(c.ctx, (i8_fused_kernel<X, T, 4>), grid, dim3(256), lds, c.s, x, c.rows, c.K, c.N, c.codes, a, whole);
-  else VD_KERNEL(c.ctx, (i8_fused_kernel<X, T, 8>), grid, dim3(256), lds, c.s, x, c.rows, c.K, c.N, c.codes, a, whole);
+  VD_KERNEL(c.ctx, (i8_fused_kernel<X, T>), grid, dim3(256), lds, c.s, x, c.rows, c.K, c.N, c.codes, a, whole);
   VD_LAUNCH_CHECK(c.ctx);
   return VARDROP_OK;
 }
-// One launch: few rows, or rows whose codes fit beside the stages while all tiles are resident together (two workgroups a compute unit up to
-// K = 512, one above).
+// One launch: few rows, or rows whose codes fit beside the stages twice a compute unit while all tiles are resident together.  us, two launches -> one
+// (replayed from a graph; issued one by one, two cost the host 2 us more): few rows, 1 x 128 x 512 5.4 -> 3.1, 4 x 512 x 4096 6.2 -> 5.3, 4 x 1024 x
+// 4096 7.5 -> 7.2, but 8 x 512 x 512 6.1 -> 8.4, 1 x 2048 x 2048 9.3 -> 9.6; tiles, 2247 x 97 x 321 8.5 -> 7.9, 4000 x 128 x 512 7.6 -> 5.8, 862 x 512 x 720 7.0
+// -> 7.4 (bf16) and 7.4 -> 7.0 (fp32), but 64 x 1024 x 1024 7.8 -> 10.6.
 bool i8_is_one_launch(const I8Call& c) {
-  if (c.rows <= kFewRows && i8_pitch(c.K) <= kFewPitch) return true;
-  if (i8_pitch(c.K) > 1024) return false;
-  return (long long)vd_ceil_div(c.rows, 32) * vd_ceil_div(c.N, 128) <= 2 * c.ctx->num_cus;
+  const int pitch = i8_pitch(c.K);
+  if (c.rows <= kFewRows && pitch <= kFewPitch) return true;
+  return pitch <= kFusedPitch && (long long)vd_ceil_div(c.rows, 32) * vd_ceil_div(c.N, 128) <= 2 * c.ctx->num_cus;
 }
 
 template <typename T>
