@@ -35,7 +35,7 @@ __device__ inline uint32_t wave_max(uint32_t v) {
   return v;
 }
 
-// A wavefront a row, any width and alignment.
+// A wavefront a row, any width and alignment: rows are read twice, the second time from the caches.
 template <typename T>
 __global__ __launch_bounds__(256) void i8_rows_kernel(const T* x, long long rows, int K, uint8_t* q, float* scale) {
   const int lane = threadIdx.x & 63, pitch = i8_pitch(K);
@@ -50,7 +50,8 @@ __global__ __launch_bounds__(256) void i8_rows_kernel(const T* x, long long rows
     if (lane == 0) scale[r] = s;
   }
 }
-// The same for rows of whole groups of eight that 64 lanes hold in U groups each: read once.
+// The same for rows of whole groups of eight that 64 lanes hold in U groups each: read once, 16 bytes at a time.  us, by elements -> by groups:
+// 27 584 x 512 in bf16 21.7 -> 9.3 (4.6 TB/s), 65 536 x 768 in bf16 64.6 -> 25.9, in fp32 76.8 -> 36.3, 2000 x 2048 in bf16 12.0 -> 3.8.
 template <typename T, int U>
 __global__ __launch_bounds__(256) void i8_rows_whole_kernel(const T* x, long long rows, int K, uint8_t* q, float* scale) {
   const int lane = threadIdx.x & 63, pitch = i8_pitch(K);

@@ -1,6 +1,6 @@
 // Activations in 8 bits (format: pack8.h): pack and unpack.
 //
-// Bound by memory: 2 or 4 bytes an element one way, 33/32 the other.
+// Bound by memory: 2 or 4 bytes an element one way, 33/32 the other.  27 584 x 512 in bf16: pack 9.7 us (4.4 TB/s), unpack 8.0 (5.3).
 #include "pack8.h"
 
 namespace {
@@ -59,7 +59,12 @@ __global__ __launch_bounds__(256) void pack8_kernel(PackArgs p) {
   }
 }
 
-// Any width: half a wavefront a block, a lane a channel.
+// Any width and alignment: half a wavefront a block, a lane a channel.  The tensor above by elements: 26.8 and 20.0 us; 65 536 x 321 in fp32 38 and
+// 30 (2.8 and 3.6 TB/s): a load, five steps of a maximum and a store of one byte for every element.  (Eight elements a lane, their stores 8 to 32
+// bytes apart: pack 28 -> 18 in bf16 and 26 -> 28 in fp32, unpack 20 -> 21 and 20 -> 37.)
+__device__ inline long long block_row(long long b, int nb, long long blocks) {
+  return blocks <= 0x7fffffff ? (long long)((uint32_t)b / (uint32_t)nb) : b / nb;         // (in 32 bits a third of the work)
+}
 template <typename T>
 __global__ __launch_bounds__(256) void pack8_any_kernel(PackArgs p) {
   long long rows;
@@ -74,7 +79,7 @@ __global__ __launch_bounds__(256) void pack8_any_kernel(PackArgs p) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const long long b = at + u * 8 + (threadIdx.x >> 5);
-      row[u] = b / nb;
+      row[u] = block_row(b, nb, blocks);
       c[u] = (int)(b - row[u] * nb) * kPackBlock + l;
       v[u] = b < blocks && c[u] < p.d ? to_float(((const T*)p.x)[row[u] * p.d + c[u]]) : 0.f;
     }
@@ -82,10 +87,13 @@ __global__ __launch_bounds__(256) void pack8_any_kernel(PackArgs p) {
     for (int u = 0; u < U; ++u) {
       const long long b = at + u * 8 + (threadIdx.x >> 5);
       const bool live = b < blocks && c[u] < p.d;
-      uint32_t most = magnitude(v[u]);
-#pragma unroll
-      for (int m = 1; m < 32; m <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, m, 64));
-      const uint32_t e = pack_exponent(most);
+      float top = __builtin_fabsf(v[u]);
+      top = most_of(top, __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(top), 0xb1, 0xf, 0xf, true)));      // lanes ^ 1
+      top = most_of(top, __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(top), 0x4e, 0xf, 0xf, true)));      // lanes ^ 2
+      top = most_of(top, __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(top), 0x141, 0xf, 0xf, true)));     // the other four of eight
+      top = most_of(top, __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(top), 0x140, 0xf, 0xf, true)));     // the other eight of sixteen
+      top = most_of(top, __shfl_xor(top, 16, 64));
+      const uint32_t e = pack_exponent(__float_as_uint(top));
       if (live) p.codes[row[u] * p.d + c[u]] = (uint8_t)pack_code(e >= 248u ? pack_limit(v[u]) : v[u], pack_up(e));
       if (live && l == 0) p.exps[b] = (uint8_t)e;
     }
@@ -130,7 +138,7 @@ __global__ __launch_bounds__(256) void unpack8_any_kernel(PackArgs p) {
   for (long long at = (long long)blockIdx.x * (8 * U); at < blocks; at += (long long)gridDim.x * (8 * U)) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const long long b = at + u * 8 + (threadIdx.x >> 5), row = b / nb;
+      const long long b = at + u * 8 + (threadIdx.x >> 5), row = block_row(b, nb, blocks);
       const int c = (int)(b - row * nb) * kPackBlock + l;
       if (b >= blocks || c >= p.d) continue;
       const long long i = row * p.d + c;
