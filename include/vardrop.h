@@ -552,7 +552,7 @@ int vardrop_unpack8_dev(vardrop_ctx* ctx, const void* saved, int B, const int32_
  * VARDROP_BF16 multiplies on the matrix cores with fp32 accumulation (act(h) and dh are rounded to bf16 in between) and requires d and
  * f multiples of 64 and 16-byte aligned tensors (but db1, db2).  VARDROP_F32 takes any d and f, element aligned: a product is six exact
  * products of rounded bf16 parts, summed in fp32; bits below 2^-133 are lost, and an infinity, or a magnitude that rounds to one in
- * bf16, counts as NaN (a small forward, d f <= 32 768 and few tokens, multiplies in fp32 itself).  d, f <= 65 536; B*n*d, B*n*f and d*f < 2^31, in
+ * bf16, counts as NaN (a small forward, d f <= 8192 and few tokens, multiplies in fp32 itself).  d, f <= 65 536; B*n*d, B*n*f and d*f < 2^31, in
  * VARDROP_F32 with d and f up to multiples of 64 (EUNSUPPORTED otherwise).  Outputs must not overlap inputs.  B*n == 0 is a no-op (weight gradients zero-filled).  The _dev
  * forms read n on the device (see the general rules); the same n_max has to be given to the size queries, the forward and the
  * backward.  Sums run in an order that does not depend on scheduling. */

@@ -90,6 +90,12 @@ def test_fp32(vd, ctx, B, n, d, f, act):
     check(vd, ctx, B, n, d, f, "fp32", act)
 
 
+@pytest.mark.parametrize("B,n,d,f", [(3, 5500, 100, 130), (8, 1000, 130, 200), (1, 6001, 450, 500)])
+def test_fp32_many_tokens(vd, ctx, B, n, d, f):
+    """Large tiles in either direction, several slices of the weight gradients."""
+    check(vd, ctx, B, n, d, f, "fp32", "gelu")
+
+
 @pytest.mark.parametrize("B,n,d,f", [(1, 17, 64, 128), (2, 600, 128, 192)])
 def test_without_biases_and_with_gradients_in_bf16(vd, ctx, B, n, d, f):
     check(vd, ctx, B, n, d, f, "bf16", "gelu", bias=False, grad="bf16")
