@@ -578,7 +578,7 @@ int vardrop_ffn_bwd_dev(vardrop_ctx* ctx, const void* dy, int B, const int32_t* 
 /* ---------------------------------------------------------------------------------
  * Products in 8-bit integers, for a model that answers: a scale for each token and for each output channel.
  *
- *   scale_t = max|x_t| / 127,  code = x * (127 / max|x_t|) to the nearest whole number, ties to even     (fp32, a row of x at a time)
+ *   scale_t = max|x_t| / 127,  code = x * (127 * (1 / max|x_t|)) to the nearest whole number, ties to even   (each operation in fp32)
  *   y[t][c] = act(scale_t scale_c sum_k code_t[k] code_c[k] + bias[c])
  *
  *   x       [rows][K] of x_dtype VARDROP_F32 or VARDROP_BF16, quantised by the call (codes and scales in `ws`), or VARDROP_I8: codes

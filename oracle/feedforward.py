@@ -85,7 +85,7 @@ def integers(x):
             scale[r] = np.nan
         elif m >= np.float32(2.0 ** -100):
             scale[r] = m / np.float32(127)
-            codes[r] = np.rint(x[r] * (np.float32(127) / m))
+            codes[r] = np.rint(x[r] * (np.float32(127) * (np.float32(1) / m)))
     return codes, scale
 
 

@@ -1,6 +1,6 @@
 // Products in 8-bit integers with a scale for each token and each output channel, for a model that answers.
 //
-//   s_t = max |x_t| / 127,  q_t = round(x_t (127 / max |x_t|));  the same for the columns of W;  y = act(s_t s_c (q_t . q_c) + b_c)
+//   s_t = max |x_t| / 127,  q_t = round(x_t (127 (1 / max |x_t|)));  the same for the columns of W;  y = act(s_t s_c (q_t . q_c) + b_c)
 //
 // Integer products and sums are exact; what is rounded is the codes, and the result.  Codes lie along k in rows of whole 128-byte
 // stages, zeros behind the last, which is what the matrix instruction's tiles (tile_gemm.h) read.
@@ -11,16 +11,17 @@ namespace {
 
 constexpr int kMaxI8K = 65536;                        // 127^2 K < 2^31
 constexpr int kMaxI8Rows = 1 << 30;
-constexpr float kLeastRow = 7.8886090522101181e-31f;  // 2^-100: rows below count as zeros (127 / max would not be finite for the smallest)
+constexpr float kLeastRow = 7.8886090522101181e-31f;  // 2^-100: rows below count as zeros (1 / max would not be finite for the smallest)
 
 __host__ __device__ inline int i8_pitch(int K) { return (K + 127) / 128 * 128; }
 
-// scale and its reciprocal of a row whose largest magnitude has these bits; a row that holds an infinity or NaN gets NaN
+// scale and 127 / max of a row whose largest magnitude has these bits; a row that holds an infinity or NaN gets NaN.
+// (127 (1 / max), two roundings, is how array libraries divide a number by a tensor: who quantises weights with one gets the same codes.)
 __device__ inline void i8_scales(uint32_t most, float& scale, float& up) {
   const float m = __uint_as_float(most);
   const bool some = m >= kLeastRow;
   scale = most >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : (some ? m / 127.f : 0.f);
-  up = some && most < 0x7f800000u ? 127.f / m : 0.f;
+  up = some && most < 0x7f800000u ? 127.f * (1.f / m) : 0.f;
 }
 // (the product is rounded before it is rounded to a whole number: a fused one would break ties of its own)
 __device__ inline uint32_t i8_code(float v, float up) {
