@@ -19,8 +19,9 @@ struct FfnFinish {
   float* col[2];               // [pieces][pitch of the columns]; null: not wanted
   void* dW[2];
   void* db[2];
-  int rows[2], cols[2], pitch[2], part_rows[2], pieces[2];     // dW[z] is [rows][cols], a slice [part_rows][pitch]
+  int rows[2], cols[2], pitch[2], part_rows[2];     // dW[z] is [rows][cols], a slice [part_rows][pitch]
   int slices, bf16;
+  int B, tile_rows, pieces;    // db1 has a piece for every tile_rows of the B n tokens, db2 `pieces`
 };
 
 // the fp32 block (ffn_f32.hip); arguments are checked
@@ -133,9 +134,8 @@ __global__ __launch_bounds__(S::THREADS, S::simd) void ffn_grads_kernel(TileArgs
 
 template <typename S, typename EpiX, typename Epi1, typename Epi2>
 int launch_grads(const FfnCall& c, const TileArgs& gx, const typename EpiX::Args& ax, const TileArgs& g1, const typename Epi1::Args& a1, const TileArgs& g2,
-                 const typename Epi2::Args& a2, int (&pieces)[2]) {
-  pieces[0] = tile_pieces<S>(g1);
-  pieces[1] = tile_pieces<S>(g2);
+                 const typename Epi2::Args& a2, int& pieces) {
+  pieces = tile_pieces<S>(g2);
   VD_FFN_LAUNCH(VARDROP_K_FFN_GRADS, (ffn_grads_kernel<S, EpiX, Epi1, Epi2>), S, (gx.A ? tile_count<S>(gx, gx.M) : 0) + tile_count<S>(g1, g1.M) + tile_count<S>(g2, g2.M), gx, ax, g1,
                 a1, g2, a2)
 }

@@ -24,7 +24,7 @@ __device__ inline void bias_eight(const bf16_t* b, int n, int N, float (&v)[8]) 
 
 struct EpiOut {
   static constexpr bool kFetch = false, kSums = false;
-  static constexpr int kPartsA = 1, kPartsB = 1;  // C = sums + bias, bf16
+  static constexpr int kPartsA = 1, kPartsB = 1, kRowSums = 0;  // C = sums + bias, bf16
   struct Args {
     bf16_t* C;
     const bf16_t* bias;
@@ -42,7 +42,7 @@ struct EpiOut {
 template <int ACT, bool KEEP>
 struct EpiAct {
   static constexpr bool kFetch = false, kSums = false;
-  static constexpr int kPartsA = 1, kPartsB = 1;  // h = sums + bias, packed with KEEP; a = act(h)
+  static constexpr int kPartsA = 1, kPartsB = 1, kRowSums = 0;  // h = sums + bias, packed with KEEP; a = act(h)
   struct Args {
     bf16_t* C;
     const bf16_t* bias;
@@ -72,14 +72,16 @@ struct EpiAct {
 struct ActBwdArgs {
   bf16_t *dh, *act;
   const uint8_t *codes, *exps;
+  float* sums;                 // of dh over a tile's rows, before it is rounded; null: not wanted
   int N, past;
 };
 template <int ACT, int MI, int NJ>
 struct EpiActBwd {
   static constexpr bool kFetch = true, kSums = false;
-  static constexpr int kPartsA = 1, kPartsB = 1;  // sums = da; dh = da act'(h'), a = act(h')
+  static constexpr int kPartsA = 1, kPartsB = 1, kRowSums = 1;  // sums = da; dh = da act'(h'), a = act(h')
   typedef ActBwdArgs Args;
   Args a;
+  float total[8];
   u32x2 codes[2 * MI * NJ];
   uint32_t exps[2 * MI * NJ];
   __device__ void fetch(int k, int m, int n, bool live) {
@@ -87,7 +89,10 @@ struct EpiActBwd {
     codes[k] = *reinterpret_cast<const u32x2*>(a.codes + at);
     exps[k] = a.exps[at >> 5];
   }
-  __device__ void columns(int, int) {}
+  __device__ void columns(int, int) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) total[e] = 0.f;
+  }
   __device__ void row(int, int k, int m, int n, bool live, float (&v)[8]) {
     if (!live) return;
     const long long at = (long long)m * a.N + n;
@@ -98,15 +103,17 @@ struct EpiActBwd {
       float slope;
       h[e] = act_both<ACT, false>(h[e], slope);
       v[e] *= slope;
+      total[e] += v[e];
     }
     store_eight(a.dh + at, v, a.past);
     store_eight(a.act + at, h, a.past);
   }
 };
 
+template <bool SUMS>
 struct EpiGrad {
-  static constexpr bool kFetch = false, kSums = true;
-  static constexpr int kPartsA = 1, kPartsB = 1;  // weight gradients: the result in the type of the gradients, or a slice's fp32 partial product
+  static constexpr bool kFetch = false, kSums = SUMS;
+  static constexpr int kPartsA = 1, kPartsB = 1, kRowSums = 0;  // weight gradients: the result in the type of the gradients, or a slice's fp32 partial product
   struct Args {
     void* C;
     float* part;
@@ -246,7 +253,7 @@ __global__ __launch_bounds__(256) void ffn_finish_kernel(FfnFinish f, int blocks
   __shared__ float red[16][17];
   const int at = blockIdx.x - weights, b0 = f.col[0] ? (f.cols[0] + 15) / 16 : 0, z = at >= b0;
   const int c = threadIdx.x & 15, group = threadIdx.x >> 4, cols = z ? f.cols[1] : f.cols[0], pitch = z ? f.pitch[1] : f.pitch[0];
-  const int column = (at - z * b0) * 16 + c, pieces = z ? f.pieces[1] : f.pieces[0];
+  const int column = (at - z * b0) * 16 + c, pieces = z ? f.pieces : (f.B * n + f.tile_rows - 1) / f.tile_rows;
   const float* p = (z ? f.col[1] : f.col[0]) + min(column, cols - 1);
   float s = 0.f;
   int k = group;
@@ -298,8 +305,8 @@ FfnWorkspace ffn_workspace(long long T, int d, int f) {
   const size_t slices = most_slices(T);
   w.part = take(slices * d * f * 4);
   w.second = take(slices * d * f * 4);
-  w.col = take(slices * vd_ceil_div(d, 64) * 2 * f * 4);      // two pieces for each slice and row of tiles at most
-  w.col2 = take(slices * vd_ceil_div(f, 64) * 2 * d * 4);
+  w.col = take((T + 63) / 64 * f * 4);                        // a piece for each row of tiles at most
+  w.col2 = take(slices * vd_ceil_div(f, 64) * 2 * d * 4);     // two for each slice and row of tiles
   w.total = at;
   return w;
 }
@@ -318,7 +325,8 @@ int launch_up(const FfnCall& c, const TileArgs& g, const typename EpiAct<ACT, KE
   VD_FFN_LAUNCH(VARDROP_K_FFN_UP, (ffn_up_kernel<S, ACT, KEEP>), S, tile_count<S>(g, g.M) + p.pieces, g, e, p)
 }
 template <typename S, int ACT>
-int launch_dh(const FfnCall& c, const TileArgs& g, const ActBwdArgs& e, PieceArgs p) {
+int launch_dh(const FfnCall& c, const TileArgs& g, const ActBwdArgs& e, PieceArgs p, int& tile_rows) {
+  tile_rows = S::BM;
   p.pieces = pieces_8(c.T * c.d / 8, S::THREADS);
   VD_FFN_LAUNCH(VARDROP_K_FFN_DH, (ffn_dh_kernel<S, ACT>), S, tile_count<S>(g, g.M) + p.pieces, g, e, p)
 }
@@ -366,8 +374,8 @@ int bwd_bf16(const FfnCall& c, const void* dy, const void* W1, const void* W2, c
     p.values = xv; p.codes = const_cast<uint8_t*>(saved); p.exps = const_cast<uint8_t*>(saved) + pack_exponents_at(c.T, c.d);
     p.B = c.B; p.n = c.n; p.d = c.d; p.n_dev = c.dn.dev;
     const TileArgs g = rows_product(c, dy, W2, c.d, c.f, c.d, true);
-    const ActBwdArgs e = {dh, a, hc, hc + pack_exponents_at(c.T, c.f), c.f, c.past(c.f, 2)};
-#define VD_CALL(S) launch_dh<S, ACT>(c, g, e, p)
+    const ActBwdArgs e = {dh, a, hc, hc + pack_exponents_at(c.T, c.f), db1 ? col : nullptr, c.f, c.past(c.f, 2)};
+#define VD_CALL(S) launch_dh<S, ACT>(c, g, e, p, fin.tile_rows)
     const int rc = VD_BY_SHAPE(product_shape(kRowShapes, c.T, c.f, c.d), VD_CALL, TileWide);
 #undef VD_CALL
     if (rc) return rc;
@@ -384,9 +392,9 @@ int bwd_bf16(const FfnCall& c, const void* dy, const void* W1, const void* W2, c
   const TileArgs gx = dx && c.T > 0 ? rows_product(c, dh, W1, c.f, c.d, c.f, false) : TileArgs{};
   const TileArgs g1 = tokens_product(c, xv, dh, c.d, c.f, plan.slices), g2 = tokens_product(c, a, dy, c.f, c.d, plan.slices);
   const EpiOut::Args ax = {(bf16_t*)dx, nullptr, c.d, c.past(c.d, 2)};
-  const EpiGrad::Args a1 = {dW1, split ? part : nullptr, fin.col[0], c.d, c.f, low};
-  const EpiGrad::Args a2 = {dW2, split ? second : nullptr, fin.col[1], c.f, c.d, low};
-#define VD_CALL(S) launch_grads<S, EpiOut, EpiGrad, EpiGrad>(c, gx, ax, g1, a1, g2, a2, fin.pieces)
+  const EpiGrad<false>::Args a1 = {dW1, split ? part : nullptr, nullptr, c.d, c.f, low};
+  const EpiGrad<true>::Args a2 = {dW2, split ? second : nullptr, fin.col[1], c.f, c.d, low};
+#define VD_CALL(S) launch_grads<S, EpiOut, EpiGrad<false>, EpiGrad<true>>(c, gx, ax, g1, a1, g2, a2, fin.pieces)
   return VD_BY_SHAPE(plan.shape, VD_CALL, Tile256);
 #undef VD_CALL
 }
@@ -428,6 +436,8 @@ int backward(vardrop_ctx* ctx, const void* dy, int B, int n, int d, int f, int d
   const uint8_t* xc = (const uint8_t*)saved;
   FfnFinish fin = {};
   fin.slices = 1;
+  fin.B = B;
+  fin.tile_rows = 64;
   fin.rows[0] = fin.part_rows[0] = fin.cols[1] = fin.pitch[1] = d;
   fin.rows[1] = fin.part_rows[1] = fin.cols[0] = fin.pitch[0] = f;
   if (dtype == VARDROP_BF16) {

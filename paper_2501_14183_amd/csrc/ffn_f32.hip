@@ -117,7 +117,7 @@ __global__ __launch_bounds__(256) void ffn_split_kernel(SplitArgs a) {
 // ---- what is done to the rows of a product (as in ffn.hip)
 struct EpiOutF32 {           // C [rows][N] = sums + bias
   static constexpr bool kFetch = false, kSums = false;
-  static constexpr int kPartsA = 3, kPartsB = 3;
+  static constexpr int kPartsA = 3, kPartsB = 3, kRowSums = 0;
   struct Args {
     float* C;
     const float* bias;
@@ -137,7 +137,7 @@ struct EpiOutF32 {           // C [rows][N] = sums + bias
 template <int ACT, bool KEEP>
 struct EpiActF32 {           // h = sums + bias, packed with KEEP; a = act(h) in parts, zeros behind the last channel
   static constexpr bool kFetch = false, kSums = false;
-  static constexpr int kPartsA = 3, kPartsB = 3;
+  static constexpr int kPartsA = 3, kPartsB = 3, kRowSums = 0;
   struct Args {
     bf16_t* act;
     long long plane;
@@ -170,14 +170,16 @@ struct ActBwdF32Args {
   bf16_t *dh, *act;
   long long plane;
   const uint8_t *codes, *exps;
+  float* sums;                 // of dh over a tile's rows; null: not wanted
   int N, past;
 };
 template <int ACT, int MI, int NJ>
 struct EpiActBwdF32 {        // sums = da; dh = da act'(h'), a = act(h'), both in parts
   static constexpr bool kFetch = true, kSums = false;
-  static constexpr int kPartsA = 3, kPartsB = 3;
+  static constexpr int kPartsA = 3, kPartsB = 3, kRowSums = 1;
   typedef ActBwdF32Args Args;
   Args a;
+  float total[8];
   u32x2 codes[2 * MI * NJ];
   uint32_t exps[2 * MI * NJ];
   __device__ void fetch(int k, int m, int n, bool live) {
@@ -185,7 +187,10 @@ struct EpiActBwdF32 {        // sums = da; dh = da act'(h'), a = act(h'), both i
     codes[k] = load_codes(a.codes + (long long)r * a.N, n, a.N);
     exps[k] = n < a.N ? a.exps[(long long)r * pack_blocks(a.N) + (n >> 5)] : 1u;
   }
-  __device__ void columns(int, int) {}
+  __device__ void columns(int, int) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) total[e] = 0.f;
+  }
   __device__ void row(int, int k, int m, int n, bool live, float (&v)[8]) {
     if (!live) return;
     float h[8];
@@ -195,6 +200,7 @@ struct EpiActBwdF32 {        // sums = da; dh = da act'(h'), a = act(h'), both i
       float slope;
       h[e] = act_both<ACT, true>(h[e], slope);
       v[e] = n + e < a.N ? v[e] * slope : 0.f;
+      total[e] += v[e];
       h[e] = n + e < a.N ? h[e] : 0.f;
     }
     const long long at = (long long)m * padded(a.N) + n;
@@ -204,8 +210,8 @@ struct EpiActBwdF32 {        // sums = da; dh = da act'(h'), a = act(h'), both i
 };
 template <int PARTS>
 struct EpiGradF32 {          // a weight gradient [M][N], or a slice's partial product [slice][part_rows][pitch]
-  static constexpr bool kFetch = false, kSums = true;
-  static constexpr int kPartsA = PARTS, kPartsB = 3;
+  static constexpr bool kFetch = false, kSums = PARTS == 3;       // (db2; db1 comes with dh)
+  static constexpr int kPartsA = PARTS, kPartsB = 3, kRowSums = 0;
   struct Args {
     float *C, *part, *sums;
     int M, N, whole;         // M, N: the result's; the sums are [padded][padded]
@@ -317,7 +323,8 @@ int launch_up(const FfnCall& c, const TileArgs& g, const typename EpiActF32<ACT,
   return launch_tile_gemm<false, true, false, S, EpiActF32<ACT, KEEP>>(c.ctx, VARDROP_K_FFN_UP, g, e, c.s);
 }
 template <typename S, int ACT>
-int launch_dh(const FfnCall& c, const TileArgs& g, const ActBwdF32Args& e) {
+int launch_dh(const FfnCall& c, const TileArgs& g, const ActBwdF32Args& e, int& tile_rows) {
+  tile_rows = S::BM;
   return launch_tile_gemm<false, true, true, S, EpiActBwdF32<ACT, S::MI, S::NJ>>(c.ctx, VARDROP_K_FFN_DH, g, e, c.s);
 }
 
@@ -341,7 +348,7 @@ WorkspaceF32 workspace_f32(long long T, int d, int f) {
   w.kept = take(2 * t * D);                // x', one part
   w.part = take(slices * D * F * 4);
   w.second = take(slices * D * F * 4);
-  w.col = take(slices * (D / 64) * 2 * F * 4);
+  w.col = take((t + 63) / 64 * F * 4);
   w.col2 = take(slices * (F / 64) * 2 * D * 4);
   w.total = at;
   return w;
@@ -433,8 +440,8 @@ int bwd(const FfnCall& c, const float* dy, const float* W1, const float* W2, con
     int rc = split(c, jy, weight_job(W2, ws + w.W2, c.f, c.d), jx, dx ? weight_job(W1, ws + w.W1, c.d, c.f) : SplitJob{});
     if (rc) return rc;
     const TileArgs g = parts_product(c, g0, ws + w.W2, D, F, D, (long long)D * F);
-    const ActBwdF32Args e = {dh, a, c.T * F, hc, hc + pack_exponents_at(c.T, c.f), c.f, c.past(F, 6)};
-#define VD_CALL(S) launch_dh<S, ACT>(c, g, e)
+    const ActBwdF32Args e = {dh, a, c.T * F, hc, hc + pack_exponents_at(c.T, c.f), db1 ? (float*)(ws + w.col) : nullptr, c.f, c.past(F, 6)};
+#define VD_CALL(S) launch_dh<S, ACT>(c, g, e, fin.tile_rows)
     rc = VD_BY_PARTS(product_shape(kPartShapes, c.T, F, 6 * D), VD_CALL);
 #undef VD_CALL
     if (rc) return rc;
@@ -455,7 +462,7 @@ int bwd(const FfnCall& c, const float* dy, const float* W1, const float* W2, con
   g1.planeB = g2.planeA = c.T * F * 2;
   g2.planeB = c.T * D * 2;
   const EpiOutF32::Args ax = {dx, nullptr, c.d, c.d % 8 == 0 && vd_aligned(dx, 16), c.past(c.d, 4)};
-  const EpiGradF32<1>::Args a1 = {dW1, (float*)fin.part[0], fin.col[0], c.d, c.f, c.f % 8 == 0 && vd_aligned(dW1, 16)};
+  const EpiGradF32<1>::Args a1 = {dW1, (float*)fin.part[0], nullptr, c.d, c.f, c.f % 8 == 0 && vd_aligned(dW1, 16)};
   const EpiGradF32<3>::Args a2 = {dW2, (float*)fin.part[1], fin.col[1], c.f, c.d, c.d % 8 == 0 && vd_aligned(dW2, 16)};
 #define VD_CALL(S) launch_grads<S, EpiOutF32, EpiGradF32<1>, EpiGradF32<3>>(c, gx, ax, g1, a1, g2, a2, fin.pieces)
   return VD_BY_PARTS(plan.shape, VD_CALL);

@@ -125,7 +125,7 @@ __device__ inline float i8_act(float v, int act) {
 template <typename T>
 struct EpiI8 {
   static constexpr bool kFetch = false, kSums = false;
-  static constexpr int kPartsA = 1, kPartsB = 1;
+  static constexpr int kPartsA = 1, kPartsB = 1, kRowSums = 0;
   struct Args {
     T* y;
     const float *sx, *sw;      // sx[0] is row m0's

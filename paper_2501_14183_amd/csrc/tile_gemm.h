@@ -185,6 +185,27 @@ __device__ __forceinline__ void tile_finish(const Sum (&acc)[S::MI][S::NJ], unsi
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
   }
+  if constexpr (Epi::kRowSums != 0) {
+    if (!epi.a.sums) return;
+    // lanes of the same columns, then the wavefronts above each other
+#pragma unroll
+    for (int u = LPR; u < 64; u <<= 1)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) epi.total[e] += __shfl_xor(epi.total[e], u, 64);
+    float* all = reinterpret_cast<float*>(smem);
+    __syncthreads();
+    if (lane < LPR) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) all[wm * S::BN + n - n0 + e] = epi.total[e];
+    }
+    __syncthreads();
+    for (int t = threadIdx.x; t < S::BN; t += S::THREADS) {
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < S::WR; ++w) sum += all[w * S::BN + t];
+      if (n0 + t < N) epi.a.sums[(long long)(m0 / S::BM) * N + n0 + t] = sum;
+    }
+  }
 }
 
 // AKC, BKC: operand contiguous along k.  Epi: `columns(n, N)` once, then `row(slice, k, m, n, live, v)` with eight sums of row m from
@@ -192,6 +213,7 @@ __device__ __forceinline__ void tile_finish(const Sum (&acc)[S::MI][S::NJ], unsi
 // Epi::kSums (B not k-contiguous): column sums of B, from the fragments that are multiplied.  The tiles above each other share the stages
 // among them and their wavefronts above each other the steps, so that none is held up; what one has goes to `sums(piece, n, live, v)`,
 // tile_pieces() of them for a column.
+// Epi::kRowSums: what `row` adds up over the rows in total[8] goes to a.sums [tiles above each other][N].
 // Epi::kPartsA, kPartsB (bf16 operands that stand for fp32 numbers): 3 and 3, both operands in three parts hi + mid + lo, each the nearest
 // bf16 number to what the ones before leave; 1 and 3, A in one part; 1 and 1, plain.  A stage holds all parts of its k.  Every product of
 // two parts is exact, and of the nine those are added up, the small ones of a step first, that are not below 2^-24 of the whole:
