@@ -7,9 +7,9 @@
 // with x', h' what the checkpoints stand for.  bf16: the element-wise work is done on the products' sums before they are
 // stored (tile_gemm.h): h never exists outside a tile, dy W2^T neither.
 // Two launches forward and three backward.  Large calls are bound by the products' loops, which wait for their operands' copies, and where the rows
-// are worked on by vector work: 65 536 x 768 x 1536, us, h and a 240 (640 TFLOP/s), y 142 (1090), dh and a 278 (560), dx, dW1 and dW2 445 (1040).
-// Short calls are chains of dependent launches, each of which takes 4 us and its tiles' stages one after the other: 2784 x 512 x 512 8.3, 6.7,
-// 8.3, 13.1 and 4.0 for the sums.
+// are worked on by vector work: 65 536 x 768 x 1536, us, h and a 240 (640 TFLOP/s), y 142 (1090), dh and a 278 (560), dx, dW1 and dW2 441 (1050).
+// Short calls are chains of dependent launches, each of which takes 4 us and its tiles' stages one after the other: 2784 x 512 x 512 8.2, 6.3,
+// 9.0, 12.4 and 3.9 for the sums.
 #include "ffn.h"
 
 namespace {
