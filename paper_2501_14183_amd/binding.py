@@ -1070,16 +1070,16 @@ def vardrop_linear_i8(ctx, x, codes, scale, bias=None, act=ACT_NONE, dtype=None,
     """y = act(x W + bias) from 8-bit integers, with (codes, scale) of W from vardrop_quantize_weight -> y [..., N].
 
     x [..., K] float32 or bfloat16, or the pair of vardrop_quantize_rows (then y is [rows, N]).  y is of type `dtype`: that of `out`, of
-    the bias or of x where it is not given.  ws: uint8 workspace for rows that the call quantises."""
+    the bias or of x (bfloat16 for a pair) where it is not given.  ws: uint8 workspace for rows that the call quantises."""
     given = type(x) is tuple
     if given:
         x, sx = x
-        if sx.dtype is not torch.float32 or not sx.is_contiguous() or sx.get_device() != x.get_device() or sx.numel() != x.shape[0]:
-            _refuse("sx", sx, x.shape[0], torch.float32)
     shape, xt, dev, N = x.shape, x.dtype, x.get_device(), scale.numel()
     K = shape[-1]
     pitch = _i8_pitch(K)
     rows = x.numel() // K if K else 0
+    if given and (sx.dtype is not torch.float32 or sx.numel() != rows or not sx.is_contiguous() or sx.get_device() != dev):
+        _refuse("sx", sx, rows, torch.float32)
     if codes.shape != (N, pitch):
         raise TypeError("codes must be [%d, %d] for rows of %d and %d scales: got %s" % (N, pitch, K, N, list(codes.shape)))
     if dtype is None:
