@@ -1078,6 +1078,8 @@ def vardrop_linear_i8(ctx, x, codes, scale, bias=None, act=ACT_NONE, dtype=None,
     K = shape[-1]
     pitch = _i8_pitch(K)
     rows = x.numel() // K if K else 0
+    if given and K != pitch:
+        raise TypeError("rows of codes must be of whole pitches, as vardrop_quantize_rows makes them: got %s" % list(shape))
     if given and (sx.dtype is not torch.float32 or sx.numel() != rows or not sx.is_contiguous() or sx.get_device() != dev):
         _refuse("sx", sx, rows, torch.float32)
     if codes.shape != (N, pitch):

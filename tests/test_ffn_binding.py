@@ -59,3 +59,12 @@ def test_codes_of_any_rank_have_a_scale_for_each_row(shape, rows):
     product_of_codes(ctx, q, gpu(rows), rows)
     (name, args), = ctx._lib.calls
     assert name == "vardrop_linear_i8" and args[3:5] == (rows, 128)
+
+
+@pytest.mark.parametrize("K", [1, 96, 127, 129, 250])
+def test_rows_of_codes_that_end_before_the_pitch_are_refused(K):
+    """The kernels read whole pitches of 128 bytes, behind the end of a buffer of shorter rows."""
+    ctx = Ctx()
+    with pytest.raises(TypeError):
+        product_of_codes(ctx, gpu(4, K, dtype=I8), gpu(4), 4, K=K)
+    assert ctx._lib.calls == []
