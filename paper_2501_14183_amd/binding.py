@@ -859,6 +859,16 @@ def _bytes(name, t, least, dev):
                     % (name, least, dev, t.dtype, list(t.shape), t.device))
 
 
+def _too_large(where):
+    """The library takes 32-bit sizes, to which ctypes would cut a larger one without a word."""
+    raise VarDropError(-4, where, ": a size does not fit 32 bits")
+
+
+def _asked(name, sizes, *rest):
+    """Bytes that the library's size query `name` answers; 0 for a size that its integers do not hold."""
+    return 0 if any(v >> 31 for v in sizes) else getattr(load_library(), name)(*sizes, *rest)
+
+
 def _room(nbytes, device):
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
 
@@ -866,12 +876,14 @@ def _room(nbytes, device):
 @functools.lru_cache(maxsize=4096)
 def vardrop_pack8_bytes(B, n, d):
     """Bytes of an 8-bit checkpoint of a [B, n, d] tensor (a multiple of 256)."""
-    return load_library().vardrop_pack8_bytes(B, n, d)
+    return _asked("vardrop_pack8_bytes", (B, n, d))
 
 
 def _packed(ctx, where, x, saved, need, dev, stream, n_dev, status):
     """vardrop_pack8 or vardrop_unpack8 with a checkpoint that is there; x: the tensor packed, or written."""
     B, n, d = x.shape
+    if (B | n | d) >> 31:
+        _too_large(where)
     dt = x.dtype
     p_x = x.data_ptr() if x.is_contiguous() else _refuse("x" if where == "vardrop_pack8" else "out", x, B * n * d, dt)
     p_saved = saved.data_ptr() if (saved.dtype is torch.uint8 and saved.numel() >= need and saved.is_contiguous()
@@ -908,13 +920,13 @@ def vardrop_unpack8(ctx, saved, out, stream=None, n_dev=None, status=None):
 @functools.lru_cache(maxsize=4096)
 def vardrop_ffn_saved_bytes(B, n, d, f):
     """Bytes of what vardrop_ffn_fwd keeps for the backward: the checkpoints of x [B, n, d] and of x W1 + b1 [B, n, f]."""
-    return load_library().vardrop_ffn_saved_bytes(B, n, d, f)
+    return _asked("vardrop_ffn_saved_bytes", (B, n, d, f))
 
 
 @functools.lru_cache(maxsize=4096)
 def vardrop_ffn_workspace_bytes(B, n, d, f, dtype):
     """Bytes of the workspace of vardrop_ffn_fwd and vardrop_ffn_bwd for tokens of a torch dtype."""
-    return load_library().vardrop_ffn_workspace_bytes(B, n, d, f, _CODES.get(dtype, -1))
+    return _asked("vardrop_ffn_workspace_bytes", (B, n, d, f), _CODES.get(dtype, -1))
 
 
 def _ffn_shapes(W1, W2, d):
@@ -935,6 +947,8 @@ def vardrop_ffn_fwd(ctx, x, W1, W2, b1=None, b2=None, act=ACT_GELU, train=True, 
     if W1.dim() != 2 or W1.shape[-1:] + (d,) != W2.shape or W1.shape[0] != d:
         _ffn_shapes(W1, W2, d)
     f = W1.shape[1]
+    if (B | n | d | f) >> 31:
+        _too_large("vardrop_ffn_fwd")
     if saved is not None and not train:
         raise TypeError("saved is for train=True")
     if out is None or ws is None or (train and saved is None):
@@ -979,6 +993,8 @@ def vardrop_ffn_bwd(ctx, dy, W1, W2, saved, act=ACT_GELU, bias_grads=False, grad
     if W1.dim() != 2 or W1.shape[-1:] + (d,) != W2.shape or W1.shape[0] != d:
         _ffn_shapes(W1, W2, d)
     f = W1.shape[1]
+    if (B | n | d | f) >> 31:
+        _too_large("vardrop_ffn_bwd")
     kw = d * f
     if out is None:
         _own_buffers(stream, "vardrop_ffn_bwd", out=out)
@@ -1023,11 +1039,13 @@ def vardrop_ffn_bwd(ctx, dy, W1, W2, saved, act=ACT_GELU, bias_grads=False, grad
 
 @functools.lru_cache(maxsize=4096)
 def _i8_pitch(K):
-    return load_library().vardrop_i8_pitch(K)
+    return _asked("vardrop_i8_pitch", (K,))
 
 
 def _quantized(ctx, where, t, rows, K, lines, out, stream):
     """vardrop_quantize_rows or vardrop_quantize_weight: codes of `lines` lines along K of t, and a scale each."""
+    if (K | lines) >> 31:
+        _too_large(where)
     dev, pitch = t.get_device(), _i8_pitch(K)
     if out is None:
         _own_buffers(stream, where, out=out)
@@ -1063,7 +1081,7 @@ def vardrop_quantize_weight(ctx, W, out=None, stream=None):
 @functools.lru_cache(maxsize=4096)
 def vardrop_linear_i8_workspace_bytes(rows, K, N):
     """Bytes of the workspace of vardrop_linear_i8 for rows that it quantises itself."""
-    return load_library().vardrop_linear_i8_workspace_bytes(rows, K, N)
+    return _asked("vardrop_linear_i8_workspace_bytes", (rows, K, N))
 
 
 def vardrop_linear_i8(ctx, x, codes, scale, bias=None, act=ACT_NONE, dtype=None, ws=None, out=None, stream=None):
@@ -1078,6 +1096,8 @@ def vardrop_linear_i8(ctx, x, codes, scale, bias=None, act=ACT_NONE, dtype=None,
     K = shape[-1]
     pitch = _i8_pitch(K)
     rows = x.numel() // K if K else 0
+    if (rows | K | N) >> 31:
+        _too_large("vardrop_linear_i8")
     if given and K != pitch:
         raise TypeError("rows of codes must be of whole pitches, as vardrop_quantize_rows makes them: got %s" % list(shape))
     if given and (sx.dtype is not torch.float32 or sx.numel() != rows or not sx.is_contiguous() or sx.get_device() != dev):

@@ -68,3 +68,58 @@ def test_rows_of_codes_that_end_before_the_pitch_are_refused(K):
     with pytest.raises(TypeError):
         product_of_codes(ctx, gpu(4, K, dtype=I8), gpu(4), 4, K=K)
     assert ctx._lib.calls == []
+
+
+MORE = 2 ** 32 + 3            # 3 in 32 bits
+
+
+def test_sizes_that_32_bits_cut_have_no_bytes():
+    for call, sizes in ((vd.vardrop_pack8_bytes, (1, 2, 64)), (vd.vardrop_ffn_saved_bytes, (1, 2, 64, 64)),
+                        (vd.vardrop_linear_i8_workspace_bytes, (2, 64, 64)),
+                        (lambda *s: vd.vardrop_ffn_workspace_bytes(*s, BF16), (1, 2, 64, 64)),
+                        (lambda *s: vd.vardrop_ffn_workspace_bytes(*s, F32), (1, 2, 64, 64))):
+        assert call(*sizes) > 0
+        for at in range(len(sizes)):
+            for more in (MORE, 2 ** 32 + 64, 2 ** 31, 2 ** 63 + 64, -1):
+                assert call(*sizes[:at], more, *sizes[at + 1:]) == 0
+
+
+def far(*shape, dtype=BF16):
+    """A tensor of that shape without memory."""
+    return torch.empty(*shape, dtype=dtype, device="meta").as_subclass(OnGpu)
+
+
+def far_calls():
+    room, saved = gpu(1 << 12, dtype=U8), gpu(1 << 12, dtype=U8)
+    block = dict(ws=room, stream=0)
+    return {
+        "pack8": lambda c: vd.vardrop_pack8(c, far(MORE, 1, 64), out=saved, stream=0),
+        "pack8, tokens": lambda c: vd.vardrop_pack8(c, far(1, MORE, 64), out=saved, stream=0),
+        "pack8, channels": lambda c: vd.vardrop_pack8(c, far(1, 1, MORE), out=saved, stream=0),
+        "pack8, none": lambda c: vd.vardrop_pack8(c, far(MORE, 0, 64), out=saved, stream=0),
+        "unpack8": lambda c: vd.vardrop_unpack8(c, saved, far(MORE, 1, 64), stream=0),
+        "ffn_fwd": lambda c: vd.vardrop_ffn_fwd(c, far(MORE, 1, 64), far(64, 64), far(64, 64), train=False, out=far(MORE, 1, 64), **block),
+        "ffn_fwd, tokens": lambda c: vd.vardrop_ffn_fwd(c, far(1, MORE, 64), far(64, 64), far(64, 64), saved=saved, out=far(1, MORE, 64), **block),
+        "ffn_fwd, channels": lambda c: vd.vardrop_ffn_fwd(c, far(1, 1, 64), far(64, 2 ** 32 + 64), far(2 ** 32 + 64, 64), train=False,
+                                                          out=far(1, 1, 64), **block),
+        "ffn_bwd": lambda c: vd.vardrop_ffn_bwd(c, far(MORE, 1, 64), far(64, 64), far(64, 64), saved, out=(None, far(64, 64), far(64, 64), None, None),
+                                                **block),
+        "quantize_rows": lambda c: vd.vardrop_quantize_rows(c, far(MORE, 64), out=(far(MORE, 128, dtype=I8), far(MORE, dtype=F32)), stream=0),
+        "quantize_rows, channels": lambda c: vd.vardrop_quantize_rows(c, far(1, MORE), out=(far(1, 128, dtype=I8), far(1, dtype=F32)), stream=0),
+        "quantize_weight": lambda c: vd.vardrop_quantize_weight(c, far(64, MORE), out=(far(MORE, 128, dtype=I8), far(MORE, dtype=F32)), stream=0),
+        "linear_i8": lambda c: vd.vardrop_linear_i8(c, far(MORE, 64), *weight(5, 64), ws=room, out=far(MORE, 5), stream=0),
+        "linear_i8, channels": lambda c: vd.vardrop_linear_i8(c, far(1, MORE), *weight(5, 64), ws=room, out=far(1, 5), stream=0),
+        "linear_i8, results": lambda c: vd.vardrop_linear_i8(c, far(1, 64), far(MORE, 128, dtype=I8), far(MORE, dtype=F32), ws=room, out=far(1, MORE),
+                                                             stream=0),
+        "linear_i8, codes": lambda c: vd.vardrop_linear_i8(c, (far(MORE, 128, dtype=I8), far(MORE, dtype=F32)), *weight(5, 128), out=far(MORE, 5),
+                                                           stream=0),
+    }
+
+
+@pytest.mark.parametrize("name", list(far_calls()))
+def test_calls_whose_sizes_32_bits_cut_are_refused(name):
+    """The library takes 32-bit sizes: a larger one has to be refused before it becomes another."""
+    ctx = Ctx()
+    with pytest.raises(vd.VarDropError) as e:
+        far_calls()[name](ctx)
+    assert e.value.code == -4 and ctx._lib.calls == []
