@@ -423,7 +423,7 @@ extern "C" int vardrop_i8_pitch(int K) { return K < 1 || K > kMaxI8K ? 0 : i8_pi
 
 extern "C" int vardrop_quantize_rows(vardrop_ctx* ctx, const void* x, int rows, int K, int dtype, void* codes, float* scale, void* stream) {
   if (!ctx || rows < 0 || K < 1 || !is_type(dtype)) return VARDROP_EINVAL;
-  if (K > kMaxI8K) return VARDROP_EUNSUPPORTED;
+  if (K > kMaxI8K || rows > kMaxI8Rows) return VARDROP_EUNSUPPORTED;
   if (rows == 0) return VARDROP_OK;
   if (!x || !codes || !scale || !vd_aligned(x, element(dtype)) || !vd_aligned(codes, 16) || !vd_aligned(scale, 4)) return VARDROP_EINVAL;
   if (dtype == VARDROP_BF16) return quantize<bf16_t>(ctx, (const bf16_t*)x, rows, K, (uint8_t*)codes, scale, (hipStream_t)stream);
@@ -432,7 +432,7 @@ extern "C" int vardrop_quantize_rows(vardrop_ctx* ctx, const void* x, int rows, 
 
 extern "C" int vardrop_quantize_weight(vardrop_ctx* ctx, const void* W, int K, int N, int dtype, void* codes, float* scale, void* stream) {
   if (!ctx || K < 1 || N < 1 || !is_type(dtype)) return VARDROP_EINVAL;
-  if (K > kMaxI8K) return VARDROP_EUNSUPPORTED;
+  if (K > kMaxI8K || N > kMaxI8Rows) return VARDROP_EUNSUPPORTED;
   if (!W || !codes || !scale || !vd_aligned(W, element(dtype)) || !vd_aligned(codes, 16) || !vd_aligned(scale, 4)) return VARDROP_EINVAL;
   VdTimer timer(ctx, VARDROP_K_QUANTIZE, (hipStream_t)stream);
   const dim3 grid((unsigned)vd_ceil_div(N, 32));
@@ -443,7 +443,7 @@ extern "C" int vardrop_quantize_weight(vardrop_ctx* ctx, const void* W, int K, i
 }
 
 extern "C" size_t vardrop_linear_i8_workspace_bytes(int rows, int K, int N) {
-  if (rows < 0 || K < 1 || N < 1 || K > kMaxI8K) return 0;
+  if (rows < 0 || K < 1 || N < 1 || K > kMaxI8K || rows > kMaxI8Rows || N > kMaxI8Rows) return 0;
   return vd_align_up((size_t)rows * i8_pitch(K), 256) + vd_align_up((size_t)rows * 4, 256);
 }
 

@@ -123,3 +123,16 @@ def test_calls_whose_sizes_32_bits_cut_are_refused(name):
     with pytest.raises(vd.VarDropError) as e:
         far_calls()[name](ctx)
     assert e.value.code == -4 and ctx._lib.calls == []
+
+
+def test_more_rows_of_codes_than_the_products_take_are_refused():
+    """2^30 rows, or channels, as vardrop_linear_i8 takes them; the address of a context is looked at before anything behind it."""
+    lib, most = vd.load_library(), 1 << 30
+    context = torch.zeros(64, dtype=U8).data_ptr()
+    for rows in (most + 1, 2 ** 31 - 1):
+        assert lib.vardrop_quantize_rows(context, None, rows, 8, vd.F32, None, None, None) == -4
+        assert lib.vardrop_quantize_weight(context, None, 8, rows, vd.F32, None, None, None) == -4
+        assert lib.vardrop_linear_i8_workspace_bytes(rows, 8, 8) == 0 and lib.vardrop_linear_i8_workspace_bytes(8, 8, rows) == 0
+    assert lib.vardrop_quantize_rows(context, None, most, 8, vd.F32, None, None, None) == -1
+    assert lib.vardrop_quantize_weight(context, None, 8, most, vd.F32, None, None, None) == -1
+    assert lib.vardrop_linear_i8_workspace_bytes(most, 8, most) == most * 128 + most * 4
