@@ -24,6 +24,11 @@ BF16, F32 = torch.bfloat16, torch.float32
 RES_SCALE, BRANCH_SCALE = 1.0, 0.5
 
 
+def name(stem, k):
+    """Name of a weight of block (or norm) k.  Numbers from ten on stand behind an underscore: b1 of block 1 and b of norm 11 would be one name."""
+    return "%s%s%d" % (stem, "_" if k > 9 else "", k)
+
+
 class Encoder:
     """Weights in fp32 with the bf16 copies that the kernels read, and one step's buffers for up to n_max tokens a window.
 
@@ -39,15 +44,24 @@ class Encoder:
             return torch.randn(*shape, generator=g, device="cuda") * scale + at
 
         p = {"We": normal(L, d, scale=L ** -0.5), "be": normal(d, scale=0.1), "w0": normal(d, scale=0.1, at=1.0), "b0": normal(d, scale=0.1)}
+
+        def weight(stem, k, t):
+            assert name(stem, k) not in p, name(stem, k)
+            p[name(stem, k)] = t
+
         for k, kind in enumerate(self.blocks):
             if kind == "attention":
-                for name in ("Wq", "Wk", "Wv", "Wo"):
-                    p["%s%d" % (name, k)] = normal(d, d, scale=d ** -0.5)
+                for stem in ("Wq", "Wk", "Wv", "Wo"):
+                    weight(stem, k, normal(d, d, scale=d ** -0.5))
             else:
-                p["W1%d" % k], p["b1%d" % k] = normal(d, ffn, scale=d ** -0.5), normal(ffn, scale=0.1)
-                p["W2%d" % k], p["b2%d" % k] = normal(ffn, d, scale=ffn ** -0.5), normal(d, scale=0.1)
-            p["wp%d" % k], p["gate%d" % k] = normal(d, scale=0.1, at=1.0), normal(d, scale=0.1, at=0.5)
-            p["w%d" % (k + 1)], p["b%d" % (k + 1)] = normal(d, scale=0.1, at=1.0), normal(d, scale=0.1)
+                weight("W1", k, normal(d, ffn, scale=d ** -0.5))
+                weight("b1", k, normal(ffn, scale=0.1))
+                weight("W2", k, normal(ffn, d, scale=ffn ** -0.5))
+                weight("b2", k, normal(d, scale=0.1))
+            weight("wp", k, normal(d, scale=0.1, at=1.0))
+            weight("gate", k, normal(d, scale=0.1, at=0.5))
+            weight("w", k + 1, normal(d, scale=0.1, at=1.0))
+            weight("b", k + 1, normal(d, scale=0.1))
         self.low = {k: t.to(BF16) for k, t in p.items()}
         self.params = {k: t.float() for k, t in self.low.items()}
 
@@ -80,8 +94,16 @@ class Encoder:
         self.norm = torch.zeros(1, device="cuda")
         self.step_dev = torch.zeros(1, dtype=torch.int64, device="cuda")
 
-    def attention(self, k):
-        return [self.low["%s%d" % (name, k)] for name in ("Wq", "Wk", "Wv", "Wo")]
+    def attention(self, k, of=None):
+        """Wq, Wk, Wv, Wo of block k, or what `of` has for them."""
+        return [(of or self.low)[name(stem, k)] for stem in ("Wq", "Wk", "Wv", "Wo")]
+
+    def feed_forward(self, k, of=None):
+        """W1, W2, b1, b2 of block k, or what `of` has for them."""
+        return [(of or self.low)[name(stem, k)] for stem in ("W1", "W2", "b1", "b2")]
+
+    def norm_bias(self, k):
+        return self.low[name("b", k)]
 
     def block(self, k, n_dev):
         """self.f[k] from the norm before it."""
@@ -89,25 +111,23 @@ class Encoder:
         if self.blocks[k] == "attention":
             vd.vardrop_attn_fwd_dev(self.ctx, h, n_dev, self.n_max, *self.attention(k), self.H, self.f[k], self.saved[k])
         else:
-            low = self.low
-            vd.vardrop_ffn_fwd(self.ctx, h, low["W1%d" % k], low["W2%d" % k], low["b1%d" % k], low["b2%d" % k], act=vd.ACT_GELU, saved=self.saved[k],
-                               ws=self.ffn_ws, out=self.f[k], n_dev=n_dev)
+            vd.vardrop_ffn_fwd(self.ctx, h, *self.feed_forward(k), act=vd.ACT_GELU, saved=self.saved[k], ws=self.ffn_ws, out=self.f[k], n_dev=n_dev)
 
     def block_backward(self, k, n_dev):
         """self.dh and the gradients of block k's weights from self.df."""
         g = self.grads
         if self.blocks[k] == "attention":
             vd.vardrop_attn_bwd_dev(self.ctx, self.df, self.norms[k][1], n_dev, self.n_max, *self.attention(k), self.H, self.saved[k],
-                                    self.ws, (self.dh, *[g["%s%d" % (name, k)] for name in ("Wq", "Wk", "Wv", "Wo")]))
+                                    self.ws, (self.dh, *self.attention(k, g)))
         else:
-            vd.vardrop_ffn_bwd(self.ctx, self.df, self.low["W1%d" % k], self.low["W2%d" % k], self.saved[k], act=vd.ACT_GELU, ws=self.ffn_ws,
-                               out=(self.dh, g["W1%d" % k], g["W2%d" % k], g["b1%d" % k], g["b2%d" % k]), n_dev=n_dev)
+            vd.vardrop_ffn_bwd(self.ctx, self.df, *self.feed_forward(k)[:2], self.saved[k], act=vd.ACT_GELU, ws=self.ffn_ws,
+                               out=(self.dh, *self.feed_forward(k, g)), n_dev=n_dev)
 
     def around(self, k):
         """What the norm behind block k - 1 takes: its own weight, and the post norm and gate of that block."""
-        kw = dict(pre=vd.NORM_LAYER, w=self.low["w%d" % k])
+        kw = dict(pre=vd.NORM_LAYER, w=self.low[name("w", k)])
         if k > 0:
-            kw |= dict(post=vd.NORM_RMS, wp=self.low["wp%d" % (k - 1)], gate=self.low["gate%d" % (k - 1)], alpha=RES_SCALE,
+            kw |= dict(post=vd.NORM_RMS, wp=self.low[name("wp", k - 1)], gate=self.low[name("gate", k - 1)], alpha=RES_SCALE,
                        beta=BRANCH_SCALE)
         return kw
 
@@ -116,11 +136,11 @@ class Encoder:
         ctx, n_max = self.ctx, self.n_max
         vd.vardrop_embed_fwd_dev(ctx, x, sel, n_dev, n_max, self.low["We"], self.low["be"], self.xs, self.saved_embed)
         self.x0.copy_(self.xs)
-        vd.vardrop_block_norm_fwd(ctx, self.x0, b=self.low["b0"], out=self.norms[0], n_dev=n_dev, **self.around(0))
+        vd.vardrop_block_norm_fwd(ctx, self.x0, b=self.norm_bias(0), out=self.norms[0], n_dev=n_dev, **self.around(0))
         res = self.x0
         for k in range(len(self.blocks)):
             self.block(k, n_dev)
-            vd.vardrop_block_norm_fwd(ctx, res, self.f[k], b=self.low["b%d" % (k + 1)], out=self.norms[k + 1], n_dev=n_dev,
+            vd.vardrop_block_norm_fwd(ctx, res, self.f[k], b=self.norm_bias(k + 1), out=self.norms[k + 1], n_dev=n_dev,
                                       **self.around(k + 1))
             res = self.norms[k + 1][0]
         return self.norms[-1][1]
@@ -130,7 +150,7 @@ class Encoder:
         ctx, n_max, g, dr = self.ctx, self.n_max, self.grads, None
         for k in range(len(self.blocks), 0, -1):
             r, _, stats = self.norms[k]
-            out = (self.dr, self.df, g["w%d" % k], g["b%d" % k], g["wp%d" % (k - 1)], None, g["gate%d" % (k - 1)])
+            out = (self.dr, self.df, g[name("w", k)], g[name("b", k)], g[name("wp", k - 1)], None, g[name("gate", k - 1)])
             vd.vardrop_block_norm_bwd(ctx, dr, dh, r, self.f[k - 1], stats, ws=self.ws, out=out, n_dev=n_dev, **self.around(k))
             dr, dh = self.dr, self.dh
             self.block_backward(k - 1, n_dev)
