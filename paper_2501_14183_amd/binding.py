@@ -1004,6 +1004,8 @@ def vardrop_ffn_bwd(ctx, dy, W1, W2, saved, act=ACT_GELU, bias_grads=False, grad
 
         out = (torch.empty_like(dy), grad(True, d, f), grad(True, f, d), grad(bias_grads, f), grad(bias_grads, d))
     dx, dW1, dW2, db1, db2 = out
+    if dW1 is None or dW2 is None:
+        raise TypeError("vardrop_ffn_bwd writes dW1 and dW2: they cannot be missing")
     gt = dW1.dtype
     if ws is None:
         _own_buffers(stream, "vardrop_ffn_bwd", ws=ws)

@@ -136,3 +136,14 @@ def test_more_rows_of_codes_than_the_products_take_are_refused():
     assert lib.vardrop_quantize_rows(context, None, most, 8, vd.F32, None, None, None) == -1
     assert lib.vardrop_quantize_weight(context, None, 8, most, vd.F32, None, None, None) == -1
     assert lib.vardrop_linear_i8_workspace_bytes(most, 8, most) == most * 128 + most * 4
+
+
+def test_weight_gradients_that_are_missing_are_a_type_error():
+    ctx, W1, W2, saved, ws = Ctx(), gpu(64, 128), gpu(128, 64), gpu(1 << 14, dtype=U8), gpu(1 << 20, dtype=U8)
+    for missing in ((1,), (2,), (1, 2)):
+        out = [gpu(1, 4, 64), gpu(64, 128), gpu(128, 64), None, None]
+        for k in missing:
+            out[k] = None
+        with pytest.raises(TypeError):
+            vd.vardrop_ffn_bwd(ctx, gpu(1, 4, 64), W1, W2, saved, ws=ws, out=tuple(out), stream=0)
+    assert ctx._lib.calls == []
