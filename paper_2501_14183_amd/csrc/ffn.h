@@ -10,7 +10,7 @@ struct FfnCall {
   long long T;
   VdDevCount dn;
   hipStream_t s;
-  int past(int N, int bytes) const { return T * N * bytes >= 16 << 20; }
+  int past(int N, int bytes) const { return T * N * bytes >= kPastCaches; }
 };
 
 // What the last launch of a backward pass adds up, in an order of its own: slices of dW1 and dW2, pieces of db1 and db2.
