@@ -520,8 +520,9 @@ int vardrop_adamw_dev(vardrop_ctx* ctx, const vardrop_tensor_list* list, const f
  *   saved  vardrop_pack8_bytes(B, n, d), a multiple of 256, 256-byte aligned: a signed byte for every element, and an exponent byte for
  *          every block of 32 channels of a row (the last may be shorter).  An element stands for its byte times a power of two, the
  *          smallest (of at least 2^-126) with which the block's largest magnitude is, rounded, at most 127 steps; ties to even.  So it
- *          is off by at most half a step, 2^-7 of the block's largest, and what it stands for is a bf16 number.  A block with an
- *          infinity or NaN comes back as NaN; magnitudes from 127.5 * 2^121 on as 127 * 2^121.
+ *          is off by at most half a step, 1/127.5 of the block's largest, and what it stands for is a bf16 number.  Two exceptions: of
+ *          a block whose largest is below 63.75 * 2^-126 (off by up to 2^-127, which may be all of a value), and magnitudes from
+ *          127.5 * 2^121 on, which come back as 127 * 2^121 (off by less than a step).  A block with an infinity or NaN comes back as NaN.
  * vardrop_unpack8 writes what `saved` stands for; its `dtype` need not be that of the tensor packed.  Rows need element alignment
  * only; d <= 2^20, B*n < 2^31 (EUNSUPPORTED above).  B*n == 0 is a no-op.  The _dev forms read n on the device (see the general rules);
  * the same n_max has to be given to the size query and both calls.
@@ -549,7 +550,8 @@ int vardrop_unpack8_dev(vardrop_ctx* ctx, const void* saved, int B, const int32_
  *   dx               NULL = not wanted
  *   dW1, dW2, db1, db2   element type grad_dtype: VARDROP_F32, or VARDROP_BF16 with VARDROP_BF16 tokens; overwritten; db NULL = skip
  *   ws               vardrop_ffn_workspace_bytes, 256-byte aligned; forward and backward, and all layers, may share one
- * VARDROP_BF16 multiplies on the matrix cores with fp32 accumulation (act(h) and dh are rounded to bf16 in between) and requires d and
+ * VARDROP_BF16 multiplies on the matrix cores with fp32 accumulation (act(h) and dh are rounded to bf16 in between; GELU is a fit, off
+ * by at most 3.9e-6, 2.7e-5 of its tail h (1 - Phi(|h|)), and held at -1.0e-7 from h = -5.5 down; its derivative by 1.5e-5) and requires d and
  * f multiples of 64 and 16-byte aligned tensors (but db1, db2).  VARDROP_F32 takes any d and f, element aligned: a product is six exact
  * products of rounded bf16 parts, summed in fp32; bits below 2^-133 are lost, and an infinity, or a magnitude that rounds to one in
  * bf16, counts as NaN (a small forward, d f <= 8192 and few tokens, multiplies in fp32 itself).  d, f <= 65 536; B*n*d, B*n*f and d*f < 2^31, in
@@ -588,7 +590,7 @@ int vardrop_ffn_bwd_dev(vardrop_ctx* ctx, const void* dy, int B, const int32_t* 
  *           lays it out, once
  *   bias    [N], `dtype`, NULL = none;  act any of the three;  y [rows][N], `dtype`
  *   ws      vardrop_linear_i8_workspace_bytes, 256-byte aligned; not needed with VARDROP_I8
- * Sums are exact 32-bit integers, scaled in fp32.  A row (or column of W) without a magnitude of 2^-100 or more counts as zeros, one
+ * Sums are exact 32-bit integers, scaled in fp32; GELU with y in VARDROP_BF16 is the fit of the feed-forward block.  A row (or column of W) without a magnitude of 2^-100 or more counts as zeros, one
  * that holds an infinity or NaN makes its results NaN.  Any K up to 65536, rows and N up to 2^30 (EUNSUPPORTED above); x and y need element
  * alignment only, and must not overlap.  rows == 0 is a no-op.
  */

@@ -5,8 +5,10 @@
 // code * 2^(E - 127): the step is the smallest power of two (of at least 2^-126) of which the block's largest magnitude is, rounded,
 // at most 127 steps, and a code is the nearest whole number, ties to even.  A power of two, and not the largest value over 127,
 // because code * step then is a bf16 number: what the backward pass multiplies is the checkpoint itself, with no rounding of its
-// own.  It costs half a bit on average: a value is off by at most half a step, 2^-7 of the block's largest.  A block that holds an
-// infinity or NaN has E = 255 and stands for NaN.  Magnitudes from 127.5 * 2^121 on count as 127 * 2^121.
+// own.  It costs half a bit on average: a value is off by at most half a step, 1/127.5 of the block's largest (which is 63.75 to 127.5
+// steps).  Two exceptions: a block whose largest is below 63.75 * 2^-126 has the least step, and its values are off by up to 2^-127;
+// magnitudes from 127.5 * 2^121 on count as 127 * 2^121, off by less than a step.  A block that holds an infinity or NaN has E = 255 and
+// stands for NaN.
 #ifndef VARDROP_PACK8_H
 #define VARDROP_PACK8_H
 #include "bf16_mfma.h"
