@@ -1100,10 +1100,11 @@ def vardrop_linear_i8(ctx, x, codes, scale, bias=None, act=ACT_NONE, dtype=None,
     rows = x.numel() // K if K else 0
     if (rows | K | N) >> 31:
         _too_large("vardrop_linear_i8")
-    if given and K != pitch:
-        raise TypeError("rows of codes must be of whole pitches, as vardrop_quantize_rows makes them: got %s" % list(shape))
-    if given and (sx.dtype is not torch.float32 or sx.numel() != rows or not sx.is_contiguous() or sx.get_device() != dev):
-        _refuse("sx", sx, rows, torch.float32)
+    if given:
+        if K != pitch:
+            raise TypeError("rows of codes must be of whole pitches, as vardrop_quantize_rows makes them: got %s" % list(shape))
+        if sx.dtype is not torch.float32 or sx.numel() != rows or not sx.is_contiguous() or sx.get_device() != dev:
+            _refuse("sx", sx, rows, torch.float32)
     if codes.shape != (N, pitch):
         raise TypeError("codes must be [%d, %d] for rows of %d and %d scales: got %s" % (N, pitch, K, N, list(codes.shape)))
     if dtype is None:

@@ -267,3 +267,20 @@ def test_what_is_not_finite_reaches_every_sum_over_its_tokens(vd, ctx, kind, dt)
     for name in ("dW1", "dW2", "db1"):
         assert bool(torch.isnan(rest2[name]).all()), name
     assert torch.equal(rest2["db2"], rest["db2"]) and bool(torch.isfinite(rest["db2"]).all())
+
+
+@pytest.mark.parametrize("shape", [(6, 200), (2, 3, 200), (3, 1, 2, 200), (700, 200)])
+def test_given_codes_of_any_rank(vd, ctx, shape):
+    """Rows of codes viewed as a batch give the rows of the plain call."""
+    g = u.generator(8, *shape)
+    x, W = torch.randn(shape, generator=g, device="cuda"), torch.randn(shape[-1], 40, generator=g, device="cuda")
+    weight = vd.vardrop_quantize_weight(ctx, W)
+    q, s = vd.vardrop_quantize_rows(ctx, x)
+    want = vd.vardrop_linear_i8(ctx, x, *weight)
+    got = vd.vardrop_linear_i8(ctx, (q.view(*shape[:-1], -1), s), *weight, dtype=F32)
+    assert got.shape == (s.numel(), 40) and torch.equal(got, want.view(-1, 40))
+    with pytest.raises(TypeError):
+        vd.vardrop_linear_i8(ctx, (q[:, :100].contiguous(), s), *weight)
+    if len(shape) > 2:
+        with pytest.raises(TypeError):
+            vd.vardrop_linear_i8(ctx, (q.view(*shape[:-1], -1), s[:shape[0]]), *weight)
