@@ -93,12 +93,11 @@ def product(A, B, lost=(), one=False):
 CPU = (70, 66, 72)            # tokens, d, f
 
 
-@pytest.mark.parametrize("lost", [None, *PAIRS])
-@pytest.mark.parametrize("which", ["up", "down", "dh", "dx", "dW1", "dW2"])
+# (in dW1 a checkpoint's value has one part)
+@pytest.mark.parametrize("which,lost", [(which, pair) for which in ("up", "down", "dh", "dx", "dW1", "dW2") for pair in (None, *PAIRS)
+                                        if which != "dW1" or not pair or pair[0] == 0])
 def test_single_products_show_every_pair(which, lost):
     T, d, f = CPU
-    if which == "dW1" and lost is not None and lost[0] > 0:
-        pytest.skip("a checkpoint's value has one part")
     here = lambda name: (lost,) if which == name else ()
     if which in ("up", "down"):
         t = u.single_forward(T, d, f, 1, device="cpu")
