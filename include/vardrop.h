@@ -590,7 +590,7 @@ int vardrop_ffn_bwd_dev(vardrop_ctx* ctx, const void* dy, int B, const int32_t* 
  *           lays it out, once
  *   bias    [N], `dtype`, NULL = none;  act any of the three;  y [rows][N], `dtype`
  *   ws      vardrop_linear_i8_workspace_bytes, 256-byte aligned; not needed with VARDROP_I8
- * Sums are exact 32-bit integers, scaled in fp32; GELU with y in VARDROP_BF16 is the fit of the feed-forward block.  A row (or column of W) without a magnitude of 2^-100 or more counts as zeros, one
+ * Sums are exact 32-bit integers, scaled in fp32, by the token's scale first; GELU with y in VARDROP_BF16 is the fit of the feed-forward block.  A row (or column of W) without a magnitude of 2^-100 or more counts as zeros, one
  * that holds an infinity or NaN makes its results NaN.  Any K up to 65536, rows and N up to 2^30 (EUNSUPPORTED above); x and y need element
  * alignment only, and must not overlap.  rows == 0 is a no-op.
  */
